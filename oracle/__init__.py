@@ -12,6 +12,8 @@ Modules
                max-pool, role allocation (role-conditional, fair, No-X),
                per-role selection, compaction, decoding through the keep-set
                and the per-role mass diagnostics.
+``pages``      the paged 4-bit cache: the row format, the page bookkeeping as
+               sequential Python, decode over it.
 ``brute``      pure-Python loops over tiny inputs (an independent second
                reading used to pin ``reference``).
 
@@ -28,3 +30,4 @@ which group query heads into KV heads, have their own grouping pins.
 """
 
 from .reference import *  # noqa: F401,F403
+from .pages import *  # noqa: F401,F403

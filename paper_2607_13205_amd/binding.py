@@ -41,6 +41,13 @@ EXPORTED = (
     "kve_read_probe",
 )
 
+#: every symbol include/kve_pages.h declares (their Python side is pages.py)
+EXPORTED_PAGES = (
+    "kve_page_bytes", "kve_pages_workspace_size", "kve_pages_extend", "kve_pages_fork", "kve_pages_free",
+    "kve_pages_append", "kve_pages_compact", "kve_pages_select", "kve_pages_read",
+    "kve_decode_pages_workspace_size", "kve_decode_pages",
+)
+
 
 class Strides(ctypes.Structure):
     """kve_strides_t: element strides of a [layer, batch, head, token] view of
@@ -108,6 +115,18 @@ def _load():
         "kve_read_probe": (c_int, [c_void, c_size, c_int, c_void, c_int, c_void]),
         "kve_decode_attention": (c_int, [c_void, c_void, c_void, c_void, c_int] + [c_int] * 6 +
                                  [c_float, c_void, c_void, c_size, c_void]),
+        "kve_page_bytes": (c_size, [c_int] * 2),
+        "kve_pages_workspace_size": (c_size, [c_int] * 3),
+        "kve_pages_extend": (c_int, [c_void, c_void, c_void, c_int, c_void, c_void, c_void, c_size, c_void]),
+        "kve_pages_fork": (c_int, [c_void, c_void, c_void, c_int, c_void, c_void, c_void, c_size, c_void]),
+        "kve_pages_free": (c_int, [c_void, c_void, c_int, c_void]),
+        "kve_pages_append": (c_int, [c_void] * 4 + [c_int] * 3 + [c_void] * 5),
+        "kve_pages_compact": (c_int, [c_void] * 4 + [c_int] * 3 + [c_void, c_void, c_int] + [c_void] * 4),
+        "kve_pages_select": (c_int, [c_void, c_int, c_void, c_void, c_void, c_int, c_void, c_void, c_void]),
+        "kve_pages_read": (c_int, [c_void, c_int, c_int, c_int] + [c_void] * 6),
+        "kve_decode_pages_workspace_size": (c_size, [c_int] * 6),
+        "kve_decode_pages": (c_int, [c_void, c_int, c_void, c_int, c_int, c_int, c_void, c_float, c_void, c_void,
+                                     c_size, c_void]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

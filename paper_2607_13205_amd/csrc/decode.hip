@@ -12,13 +12,14 @@
 // exp2(x - m) with m raised only when a logit exceeds it by more than 64 (a
 // wave vote), so the common step needs no cross-lane maximum.  Each workgroup
 // writes (m, l, o) per head; a second kernel merges the splits.
+#include "kve_decode_merge.h"
 #include "kve_device.h"
 #include "kve_internal.h"
 
 namespace kve {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kMergeThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBlk = 32;  // key rows per wave step
 
@@ -63,22 +64,6 @@ struct QKFrag<float, D> {
         for (int st = 0; st < NSTEP; ++st) f[st] = 0.0f;
     }
 };
-
-__device__ __forceinline__ float xor_max32(float v) {
-#pragma unroll
-    for (int s = 1; s < 32; s <<= 1) v = fmaxf(v, __shfl_xor(v, s));
-    return v;
-}
-
-__device__ __forceinline__ float xor_sum32(float v) {
-#pragma unroll
-    for (int s = 1; s < 32; s <<= 1) v += __shfl_xor(v, s);
-    return v;
-}
-
-__device__ __forceinline__ float read_lane(float v, int lane) {
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
-}
 
 // One workgroup per (segment, split).  NH: query heads per KV head padded to
 // 4 or 8.  Head h of the wave's 32x32 product sits in register h % 4 of the
@@ -263,87 +248,6 @@ __global__ __launch_bounds__(kThreads) void decode_split(const T* __restrict__ q
     }
 }
 
-// Merge the splits of a (segment, head) row and normalise: WPR waves per row,
-// each a contiguous share of the splits, 64 at a time: lane s takes the
-// reference and denominator of split s, then the partial outputs are added
-// kAhead loads at a time.  What the merge costs is round trips to memory, not
-// bytes: a loop that loads split by split took 6.9 us for 13 splits of 128 rows.
-template <int D, int WPR>
-__global__ __launch_bounds__(kThreads) void decode_combine(const float* __restrict__ ws_o,
-                                                           const float2* __restrict__ ws_ml, int G, int nsplit,
-                                                           int n_rows, float* __restrict__ out) {
-    constexpr int CPT = D / kWave;  // columns per lane
-    constexpr int kAhead = 8;
-    __shared__ float s_m[kWaves], s_l[kWaves], s_o[kWaves][D];
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int r = blockIdx.x * (kWaves / WPR) + wv / WPR;
-    const int row = min(r, n_rows - 1);  // no early return: the workgroup has a barrier
-    const int seg = row / G, h = row - (row / G) * G;
-    const size_t base = (size_t)seg * nsplit;
-    const int part = wv % WPR;
-    const int s0 = nsplit * part / WPR, s1 = nsplit * (part + 1) / WPR;
-    float mx = -INFINITY, lt = 0.0f, ot[CPT];
-#pragma unroll
-    for (int c = 0; c < CPT; ++c) ot[c] = 0.0f;
-    for (int sb = s0; sb < s1; sb += kWave) {
-        const int n = min(kWave, s1 - sb);
-        const float2 ml = ws_ml[(base + sb + min(lane, n - 1)) * G + h];
-        const float m = lane < n ? ml.x : -INFINITY;
-        float mn = fmaxf(xor_max32(m), mx);
-        mn = fmaxf(mn, __shfl_xor(mn, 32));
-        if (mn == -INFINITY) continue;  // uniform: only empty splits so far
-        const float a = fast_exp2(m - mn), keep = fast_exp2(mx - mn);
-        const float l = xor_sum32(lane < n ? a * ml.y : 0.0f);
-        lt = fmaf(lt, keep, l + __shfl_xor(l, 32));
-#pragma unroll
-        for (int c = 0; c < CPT; ++c) ot[c] *= keep;
-        mx = mn;
-        for (int i = 0; i < n; i += kAhead) {
-            float o[kAhead][CPT];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const float* os = ws_o + ((base + sb + min(i + j, n - 1)) * G + h) * D + lane * CPT;
-#pragma unroll
-                for (int c = 0; c < CPT; ++c) o[j][c] = os[c];
-            }
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const float w = i + j < n ? read_lane(a, min(i + j, n - 1)) : 0.0f;
-#pragma unroll
-                for (int c = 0; c < CPT; ++c) ot[c] = fmaf(w, o[j][c], ot[c]);
-            }
-        }
-    }
-    if constexpr (WPR > 1) {
-        s_m[wv] = mx;
-        s_l[wv] = lt;
-#pragma unroll
-        for (int c = 0; c < CPT; ++c) s_o[wv][lane * CPT + c] = ot[c];
-        __syncthreads();
-        if (part != 0) return;
-        float m = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < WPR; ++w) m = fmaxf(m, s_m[wv + w]);
-        lt = 0.0f;
-#pragma unroll
-        for (int c = 0; c < CPT; ++c) ot[c] = 0.0f;
-        if (m != -INFINITY) {
-#pragma unroll
-            for (int w = 0; w < WPR; ++w) {
-                const float a = fast_exp2(s_m[wv + w] - m);
-                lt = fmaf(a, s_l[wv + w], lt);
-#pragma unroll
-                for (int c = 0; c < CPT; ++c) ot[c] = fmaf(a, s_o[wv + w][lane * CPT + c], ot[c]);
-            }
-        }
-    }
-    if (r < n_rows) {
-#pragma unroll
-        for (int c = 0; c < CPT; ++c) out[(size_t)r * D + lane * CPT + c] = lt > 0.0f ? ot[c] / lt : 0.0f;
-    }
-}
-
 template <typename T, int D, int NH>
 hipError_t run_decode(const void* q, const void* kc, const void* vc, const int32_t* count, int L, int B,
                       int Hq, int Hkv, int k_cap, float scale, float* out, void* ws, hipStream_t st) {
@@ -354,15 +258,7 @@ hipError_t run_decode(const void* q, const void* kc, const void* vc, const int32
     hipLaunchKernelGGL((decode_split<T, D, NH>), dim3((unsigned)((size_t)p.segs * p.nsplit)), dim3(kThreads), 0,
                        st, static_cast<const T*>(q), static_cast<const T*>(kc), static_cast<const T*>(vc), count,
                        p.G, k_cap, p.nsplit, p.split_keys, scale * kLog2e, wo, wml, out);
-    const int rows = p.segs * p.G;
-    // one split: nothing to merge.  Up to 16: one wave per row; more: four, which
-    // cut the chain of loads (kAhead splits per round trip) in four
-    if (p.nsplit > 16)
-        hipLaunchKernelGGL((decode_combine<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, wo, wml, p.G,
-                           p.nsplit, rows, out);
-    else if (p.nsplit > 1)
-        hipLaunchKernelGGL((decode_combine<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0,
-                           st, wo, wml, p.G, p.nsplit, rows, out);
+    launch_merge<D, false>(wo, wml, p.G, p.nsplit, p.segs * p.G, out, st);
     return hipGetLastError();
 }
 

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "kve_decode_plan.h"
+#include "kve_pages_plan.h"
 #include "kve_quest_plan.h"
 #include "kve_snap_plan.h"
 
@@ -89,5 +90,25 @@ hipError_t launch_read_probe(const void* buf, size_t bytes, int nontemporal, flo
 hipError_t launch_compact(const RowView& k, const RowView& v, int elem_bytes, const int32_t* idx,
                           const int32_t* count, int L, int B, int Hkv, int N, int d, int k_cap,
                           void* k_out, void* v_out, hipStream_t st);
+
+// The paged 4-bit cache (kve_pages.h); p.L layers per call.
+hipError_t launch_pages_extend(const PagePool& p, const int32_t* seq, const int32_t* add, int n, int32_t* start,
+                               int32_t* missing, void* ws, hipStream_t st);
+hipError_t launch_pages_fork(const PagePool& p, int d, const int32_t* src, const int32_t* dst, int n, int32_t* done,
+                             int32_t* missing, void* ws, hipStream_t st);
+hipError_t launch_pages_free(const PagePool& p, const int32_t* seq, int n, hipStream_t st);
+
+// k, v: views [L, B, Hkv, N, d].  idx null: rows 0 .. count[b] (count null: cap)
+// of each segment, else idx[l, b, j, 0 .. count[l, b, j]); cap entries per segment.
+hipError_t launch_pages_pack(const RowView& k, const RowView& v, int dtype, int d, int B, int N, const int32_t* idx,
+                             const int32_t* count, int cap, const int32_t* start, const int32_t* seq,
+                             const PagePool& p, hipStream_t st);
+hipError_t launch_pages_select(const PagePool& p, int d, int B, const int32_t* src, const int32_t* idx,
+                               const int32_t* count, int cap, const int32_t* dst, const int32_t* start,
+                               hipStream_t st);
+hipError_t launch_pages_read(const PagePool& p, int dtype, int d, int B, int T, const int32_t* seq,
+                             const int32_t* start, const int32_t* count, void* k_out, void* v_out, hipStream_t st);
+hipError_t launch_decode_pages(const void* q, int dtype, const PagePool& p, int d, int B, int Hq, int max_tokens,
+                               const int32_t* seq, float scale, float* out, void* ws, hipStream_t st);
 
 }  // namespace kve

@@ -1,0 +1,45 @@
+// The paged 4-bit cache: what its kernels and the C ABI share.  Plain C++.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kve_decode_plan.h"
+
+namespace kve {
+
+constexpr int kPageMin = 32, kPageMax = 1024;  // tokens per page, powers of two
+constexpr int kPagesMaxEntries = 1024;         // entries of one bookkeeping call: one per thread of its workgroup
+constexpr int kPagesMaxGroup = 16;             // query heads per KV head: the columns of a 16x16 product
+constexpr int kPagesRowsMin = 16;              // fewest rows per workgroup of a call on rows
+
+// The cache as kernels see it.  shift: log2 of the page size.
+struct PagePool {
+    char* pool;
+    int32_t *refs, *table, *held, *length;
+    int L, n_pages, Hkv, S, M, shift;
+};
+
+// Bytes of one page of one (layer, KV head): two codes per byte and a scale byte
+// per 32 channels, keys and values.  A multiple of 16 for every valid size.
+inline size_t page_block_bytes(int page, int d) { return (size_t)page * d / 16 * 17; }
+
+// Parts of a page of all KV heads of a layer that kve_pages_fork copies, one per workgroup.
+constexpr int kPagesCopyBytes = 16384;
+inline int pages_copy_blocks(int Hkv, int page, int d) {
+    return (int)((Hkv * page_block_bytes(page, d) + kPagesCopyBytes - 1) / kPagesCopyBytes);
+}
+
+// Workspace of extend and fork: one fork_plan entry per entry, then the free
+// pages found, at most as many as there are.
+inline size_t pages_workspace(int n_pages, int n) {
+    return align_up((size_t)n * 16) + align_up((size_t)n_pages * sizeof(int32_t));
+}
+
+// Plan of a decode over pages: max_tokens rows per segment in splits of whole
+// 128-row quanta, as over a dense cache.
+inline DecodePlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens, int d) {
+    return decode_plan(L, B, Hq, Hkv, max_tokens, d);
+}
+
+}  // namespace kve

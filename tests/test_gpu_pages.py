@@ -1,0 +1,574 @@
+"""The paged 4-bit cache on the GPU against its oracle: packed bytes, moved rows
+and bookkeeping bit for bit, decode within the dense decode's bound."""
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import oracle as O  # noqa: E402
+from tests.parity import check_decode, report  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def K():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2607_13205_amd.build import ensure_built
+    ensure_built()
+    import paper_2607_13205_amd as K
+    return K
+
+
+def dev(x, dtype=torch.int32):
+    return torch.as_tensor(np.ascontiguousarray(x)).to(dtype).cuda()
+
+
+def make(K, L, Hkv, d, page, n_pages, S, M, seed=0, garbage=True):
+    """An empty cache whose pool and table hold anything (scale bytes 255, NaN, among it)."""
+    g = np.random.default_rng(seed)
+    pool = g.integers(0, 256, (L, n_pages, Hkv, K.page_bytes(page, d)), dtype=np.uint8)
+    if garbage:
+        pool[..., page * d:] = g.choice([255, 0, 254, 127], pool[..., page * d:].shape)
+    z = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = dev(g.integers(-(1 << 31), 1 << 31, (S, M)))
+    return K.Pages(torch.from_numpy(pool).cuda(), z(n_pages), table, z(S), z(S), page, d)
+
+
+def book(pages):
+    return O.PageBook(*(getattr(pages, n).cpu().numpy() for n in ("refs", "table", "held", "length")), pages.page)
+
+
+def same_book(pages, b):
+    for n in ("refs", "held", "length"):
+        assert np.array_equal(getattr(pages, n).cpu().numpy(), getattr(b, n)), n
+    t = pages.table.cpu().numpy()
+    for s in range(b.S):
+        assert np.array_equal(t[s, :b.held[s]], b.table[s, :b.held[s]]), s
+
+
+def rows_of(pages, slot, upto=None):
+    """float64 keys and values [L, Hkv, length, d] of a slot, unpacked by the oracle."""
+    n = int(pages.length[slot]) if upto is None else upto
+    ids = pages.table[slot, :-(-n // pages.page)].cpu().numpy()
+    block = pages.pool.cpu().numpy()[:, ids].transpose(0, 2, 1, 3)
+    k, v = O.page_unpack(block, pages.page, pages.d)
+    return tuple(x.reshape(x.shape[:2] + (-1, pages.d))[:, :, :n] for x in (k, v))
+
+
+def normal(shape, dtype, seed, scale=1.0):
+    return (scale * torch.randn(shape, generator=torch.Generator().manual_seed(seed))).to(TORCH[dtype])
+
+
+# ---------------------------------------------------------------------------
+# the row format
+# ---------------------------------------------------------------------------
+
+def _hard_rows(dtype, d):
+    """Rows that meet every border of the format."""
+    r = np.random.default_rng(5)
+    rows = []
+    for _ in range(24):  # multiples of an eighth and a sixteenth of the unit: ties and the values next to them
+        rows.append(r.integers(-56, 57, d) / 8.0 * 2.0 ** r.integers(-40, 40))
+        rows.append(r.integers(-112, 113, d) / 16.0)
+    for _ in range(8):
+        rows.append(r.standard_normal(d) * 2.0 ** r.integers(-135, 125))
+        rows.append(r.standard_normal(d) * 2.0 ** r.integers(-30, 30, d))
+    rows += [np.zeros(d), np.full(d, -0.0), np.full(d, 3.38e38), np.full(d, 1e-44), np.full(d, 2.0 ** -126)]
+    for bad in (np.nan, np.inf, -np.inf):
+        x = r.standard_normal(d)
+        x[7] = bad
+        x[40] = -bad
+        rows.append(x)
+    x = torch.from_numpy(np.stack(rows)).to(TORCH[dtype])
+    if dtype == "f32":  # one step of float32 below and above the borders
+        t = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], dtype=torch.float32)
+        e = torch.cat([t, torch.nextafter(t, t * 0), torch.nextafter(t, t * 9), torch.tensor([6.0, 7.0, 6.9999995])])
+        x = torch.cat([x, torch.cat([e, e.new_full((8,), 6.0)]).repeat(d // 32)[None]])
+        x = torch.cat([x, x[-1:] * 2.0 ** 90, x[-1:] * 2.0 ** -120])
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_packed_bytes(K, dtype, d):
+    x = _hard_rows(dtype, d)
+    n, page = len(x), 32
+    pages = make(K, 1, 1, d, page, 5, 1, 4)
+    start, _ = K.pages_extend(pages, dev([n]))
+    before = pages.pool.cpu().numpy().copy()
+    k, v = x[None, None, None].cuda(), x.flip(0)[None, None, None].cuda()
+    K.pages_append(k, v, pages, start)
+    x = x.double().numpy()
+    M = -(-n // page)
+    pad = np.zeros((M * page - n, d))
+    want = O.page_pack(np.concatenate([x, pad]).reshape(M, page, d), np.concatenate([x[::-1], pad]).reshape(M, page, d))
+    written = torch.zeros_like(pages.pool, dtype=torch.bool)
+    for t in range(n):
+        _mark(written, pages, 0, 0, 0, t)
+    written = written.cpu().numpy()[0, :M, 0]
+    got, before = pages.pool.cpu().numpy()[0, :, 0], before[0, :, 0]
+    assert np.array_equal(got[:M][written], want[written])
+    assert np.array_equal(got[:M][~written], before[:M][~written]) and np.array_equal(got[M:], before[M:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_read_gives_every_code_and_scale(K, dtype, d):
+    """All 256 scale bytes times all sixteen codes, through pages_read."""
+    page = 256
+    block = np.zeros(K.page_bytes(page, d), dtype=np.uint8)
+    codes = (np.arange(d)[None] + np.arange(page)[:, None]) % 16
+    packed = (codes[:, 0::2] | codes[:, 1::2] << 4).astype(np.uint8)
+    half, ns = page * d // 2, page * d // 32
+    block[:half] = packed.reshape(-1)
+    block[half:2 * half] = packed[::-1].reshape(-1)
+    block[2 * half:2 * half + ns] = np.tile(np.arange(256), d // 32)
+    block[2 * half + ns:] = np.tile(np.arange(256)[::-1], d // 32)
+    z = dev([0])
+    pages = K.Pages(torch.from_numpy(block)[None, None, None].cuda(), z, dev([[0]]), dev([1]), dev([page]), page, d)
+    k, v = K.pages_read(pages, page, dtype=TORCH[dtype])
+    wk, wv = O.page_unpack(block, page, d)
+    big = float(torch.finfo(TORCH[dtype]).max)
+    for got, want in ((k, wk), (v, wv)):
+        want = np.where(np.abs(want) > big, np.copysign(np.inf, want), want)
+        assert np.array_equal(got[0, 0, 0].double().cpu().numpy(), want, equal_nan=True)
+
+
+# ---------------------------------------------------------------------------
+# rows
+# ---------------------------------------------------------------------------
+
+def _filled(K, L, Hkv, d, page, lengths, seed=0, spare=3, dtype="bf16", extra_slots=0):
+    """A cache with one sequence per length (slots in order), its rows normal numbers."""
+    S, n_pages = len(lengths) + extra_slots, sum(-(-n // page) for n in lengths) + spare
+    M = max(1, max(-(-n // page) for n in lengths) + 1)
+    pages = make(K, L, Hkv, d, page, n_pages, S, M, seed)
+    B, T = len(lengths), max(max(lengths), 1)
+    start, missing = K.pages_extend(pages, dev(lengths), seq=dev(range(B)))
+    assert start.tolist() == [0] * B and missing.item() == 0
+    k, v = normal((L, B, Hkv, T, d), dtype, seed + 1).cuda(), normal((L, B, Hkv, T, d), dtype, seed + 2).cuda()
+    K.pages_append(k, v, pages, start, n_new=dev(lengths), seq=dev(range(B)))
+    return pages, k, v
+
+
+CASES = [  # L, B, Hkv, N, d, page, cap, dtype
+    (1, 1, 1, 1, 64, 32, 1, "bf16"),
+    (2, 3, 2, 77, 128, 32, 50, "bf16"),
+    (1, 2, 3, 400, 64, 128, 300, "bf16"),
+    (1, 2, 2, 150, 128, 64, 149, "f32"),
+    (2, 1, 1, 333, 64, 1024, 200, "f32"),
+]
+
+
+@pytest.mark.parametrize("L,B,Hkv,N,d,page,cap,dtype", CASES)
+@pytest.mark.parametrize("major", ["head", "token"])
+def test_compact(K, L, B, Hkv, N, d, page, cap, dtype, major):
+    r = np.random.default_rng(N)
+    shape = (L, B, Hkv, N, d) if major == "head" else (L, B, N, Hkv, d)
+    k, v = normal(shape, dtype, 1).cuda(), normal(shape, dtype, 2).cuda()
+    if major == "token":
+        k, v = k.permute(0, 1, 3, 2, 4), v.permute(0, 1, 3, 2, 4)
+    S, M = B + 2, -(-(cap + 37) // page) + 1
+    pages = make(K, L, Hkv, d, page, B * M + 2, S, M, seed=3)
+    slots = r.permutation(S)[:B]
+    seq = dev(slots)
+    K.pages_extend(pages, dev(r.integers(0, 37, B)), seq=seq)       # some rows are there already
+    first = pages.length[seq.long()].clone()
+    start, _ = K.pages_extend(pages, dev([cap] * B), seq=seq)
+    assert torch.equal(start, first)
+    idx = np.stack([np.sort(r.permutation(N)[:cap]) for _ in range(L * B * Hkv)]).reshape(L, B, Hkv, cap)
+    count = np.full((L, B, Hkv), cap)
+    count[0, 0, 0] = max(0, cap - 3)
+    count[-1, -1, -1] = cap + 9                                      # more than the row holds: cut
+    if cap > 8:
+        idx[0, -1, 0, 2], idx[0, -1, 0, 5] = -1, N                   # skipped
+    before = pages.pool.clone()
+    K.pages_compact(k, v, dev(idx), dev(count), pages, start, seq=seq)
+    kn, vn = k.double().cpu().numpy(), v.double().cpu().numpy()
+    written = torch.zeros_like(before, dtype=torch.bool)
+    touched = (before != pages.pool)
+    for b in range(B):
+        gk, gv = rows_of(pages, int(slots[b]))
+        for l in range(L):
+            for j in range(Hkv):
+                for m in range(min(count[l, b, j], cap)):
+                    t = idx[l, b, j, m]
+                    if 0 <= t < N:
+                        at = int(start[b]) + m
+                        assert np.array_equal(gk[l, j, at], O.mx4_round(kn[l, b, j, t][None])[0])
+                        assert np.array_equal(gv[l, j, at], O.mx4_round(vn[l, b, j, t][None])[0])
+                        _mark(written, pages, int(slots[b]), l, j, at)
+    assert not (touched & ~written).any(), "bytes of other rows were written"
+
+
+def _mark(mask, pages, slot, l, j, at):
+    page, d = pages.page, pages.d
+    pg, t = int(pages.table[slot, at // page]), at % page
+    half, ns = page * d // 2, page * d // 32
+    for i in (0, 1):
+        mask[l, pg, j, i * half + t * d // 2:i * half + (t + 1) * d // 2] = True
+        mask[l, pg, j, 2 * half + i * ns + t:2 * half + (i + 1) * ns:page] = True
+
+
+def test_append_drops_what_has_no_place(K):
+    """Refused starts, positions without a page, page numbers outside the pool, slots outside: nothing is written there."""
+    L, Hkv, d, page = 1, 2, 64, 32
+    pages, k, v = _filled(K, L, Hkv, d, page, [40, 10, 33, 5], spare=4)
+    pages.table[2, 1] = 1 << 30
+    pages.table[3, 0] = -5
+    pages.held[1] = 1 << 30                                          # more than the table's row: cut to it
+    before = pages.pool.clone()
+    T = 70
+    x = normal((L, 5, Hkv, T, d), "bf16", 9).cuda()
+    K.pages_append(x, x, pages, dev([-1, 60, 20, 0, 0]), seq=dev([0, 1, 2, 3, 4]), n_new=dev([70, 2, 30, 30, 9]))
+    torch.cuda.synchronize()
+    changed = (before != pages.pool).any(-1)[0]                      # [n_pages, Hkv]
+    own = {int(pages.table[1, 1]) if 0 <= int(pages.table[1, 1]) < pages.c.n_pages else -1, int(pages.table[2, 0])}
+    assert {int(i) for i in changed.any(-1).nonzero().flatten()} <= own
+    K.pages_append(x[:, :2], x[:, :2], pages, dev([0, 0]), seq=dev([-3, 99]))
+    K.pages_append(x[:, :1], x[:, :1], pages, dev([0]), n_new=dev([-4]), seq=dev([0]))
+    K.pages_append(x[:, :1, :, :0], x[:, :1, :, :0], pages, dev([0]), seq=dev([0]))
+    assert torch.equal((before != pages.pool).any(-1)[0], changed)
+
+
+@pytest.mark.parametrize("L,B,Hkv,N,d,page,cap,dtype", CASES)
+def test_read_ranges(K, L, B, Hkv, N, d, page, cap, dtype):
+    r = np.random.default_rng(cap)
+    lengths = [N] + [int(r.integers(0, N + 1)) for _ in range(B)]
+    pages, k, v = _filled(K, L, Hkv, d, page, lengths, dtype=dtype)
+    want = [O.mx4_round(x.double().cpu().numpy()) for x in (k, v)]
+    n = len(lengths)
+    start = np.array([0] + [int(r.integers(-1, N + 2)) for _ in range(B)])
+    count = np.array([cap] + [int(r.integers(-1, cap + 2)) for _ in range(B)])
+    order = r.permutation(n)
+    outs = [torch.full((L, n, Hkv, cap, d), 7.0, dtype=TORCH[dtype], device="cuda") for _ in (0, 1)]
+    K.pages_read(pages, cap, seq=dev(order), start=dev(start[order]), count=dev(count[order]), k_out=outs[0],
+                 v_out=outs[1])
+    for got, w in zip(outs, want):
+        exp = np.full(got.shape, 7.0)
+        for i, s in enumerate(order):
+            m = min(int(count[s]), cap, lengths[s] - int(start[s]))
+            if start[s] >= 0 and m > 0:
+                exp[:, i, :, :m] = w[:, s, :, start[s]:start[s] + m]
+        assert np.array_equal(got.double().cpu().numpy(), exp)
+    # all slots, whole sequences; slots outside and invalid pages give nothing
+    k2, _ = K.pages_read(pages, N, dtype=TORCH[dtype])
+    for s in range(n):
+        assert np.array_equal(k2[:, s, :, :lengths[s]].double().cpu().numpy(), want[0][:, s, :, :lengths[s]])
+        assert not k2[:, s, :, lengths[s]:].any()
+    pages.table[0, 0] = pages.c.n_pages
+    k3, v3 = K.pages_read(pages, N, seq=dev([-1, n, 0]), dtype=TORCH[dtype])
+    assert not k3[:, :2].any() and not v3[:, :2].any() and not k3[:, 2, :, :page].any()
+    assert torch.equal(k3[:, 2, :, page:], k2[:, 0, :, page:])
+
+
+@pytest.mark.parametrize("L,B,Hkv,N,d,page,cap,dtype", CASES)
+def test_select(K, L, B, Hkv, N, d, page, cap, dtype):
+    r = np.random.default_rng(7 * N)
+    lengths = [N] * B
+    pages, k, v = _filled(K, L, Hkv, d, page, lengths, spare=B * (-(-cap // page)) + 1, extra_slots=B)
+    dst = dev(range(B, 2 * B))
+    start, missing = K.pages_extend(pages, dev([cap] * B), seq=dst)
+    assert missing.item() == 0
+    idx = np.stack([np.sort(r.permutation(N)[:cap]) for _ in range(L * B * Hkv)]).reshape(L, B, Hkv, cap)
+    count = np.full((L, B, Hkv), cap)
+    if cap > 8:
+        idx[0, 0, 0, 3], idx[0, 0, 0, 4], count[-1, -1, -1] = N, -7, cap - 4
+    K.pages_select(pages, dev(range(B)), dev(idx), dev(count), dst, start)
+    src = [rows_of(pages, b) for b in range(B)]
+    for b in range(B):
+        got = rows_of(pages, B + b)
+        for g, s in zip(got, src[b]):
+            for l in range(L):
+                for j in range(Hkv):
+                    m = np.arange(min(count[l, b, j], cap))
+                    m = m[(idx[l, b, j, m] >= 0) & (idx[l, b, j, m] < N)]
+                    assert np.array_equal(g[l, j, m], s[l, j, idx[l, b, j, m]])
+    for b in range(B):  # the sources are what they were
+        for s, x in zip(rows_of(pages, b), (k, v)):
+            assert np.array_equal(s, O.mx4_round(x[:, b].double().cpu().numpy()))
+
+
+# ---------------------------------------------------------------------------
+# bookkeeping
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("seed,S,M,page,n_pages", [(0, 12, 5, 32, 30), (1, 40, 7, 64, 90), (2, 200, 9, 32, 5000)])
+def test_bookkeeping_follows_the_oracle(K, seed, S, M, page, n_pages):
+    """Random extends, forks and frees with refusals of every kind, and the rows of forked tails."""
+    r = np.random.default_rng(seed)
+    pages = make(K, 2, 2, 64, page, n_pages, S, M, seed)
+    b = book(pages)
+    for step in range(60):
+        n = int(r.integers(1, S // 2))
+        seq = r.integers(-1, S + 1, n)
+        what = r.integers(0, 5)
+        if what < 3:
+            add = r.integers(-1, int(0.6 * M * page), n)
+            start, missing = K.pages_extend(pages, dev(add), seq=dev(seq))
+            want, lack = b.extend(seq, add)
+            assert start.tolist() == want and missing.item() == lack
+        elif what == 3:
+            dst = r.integers(-1, S + 1, n)
+            before = pages.pool.clone()
+            done, missing = K.pages_fork(pages, dev(seq), dev(dst))
+            want, lack, copies = b.fork(seq, dst)
+            assert done.tolist() == want and missing.item() == lack
+            keep = torch.ones(n_pages, dtype=torch.bool, device="cuda")
+            for a, o, rows in copies:
+                keep[o] = False
+                ka, va = O.page_unpack(before[:, a].cpu().numpy(), page, 64)
+                ko, vo = O.page_unpack(pages.pool[:, o].cpu().numpy(), page, 64)
+                assert np.array_equal(ka[:, :, :rows], ko[:, :, :rows], equal_nan=True)
+                assert np.array_equal(va[:, :, :rows], vo[:, :, :rows], equal_nan=True)
+            assert torch.equal(before[:, keep], pages.pool[:, keep])
+        else:
+            K.pages_free(pages, dev(seq[:max(1, n // 3)]))
+            b.free(seq[:max(1, n // 3)])
+        same_book(pages, b)
+    K.pages_free(pages)
+    assert not pages.refs.any() and not pages.held.any() and not pages.length.any()
+
+
+def test_many_entries_and_a_large_pool(K):
+    """1024 entries; free pages scattered over 300000, found in ascending order over many rounds."""
+    r = np.random.default_rng(11)
+    n_pages, S = 300_000, 1024
+    pages = make(K, 1, 1, 64, 32, n_pages, S, 4, garbage=False)
+    refs = (r.random(n_pages) < 0.99).astype(np.int32)
+    pages.refs.copy_(dev(refs))
+    b = book(pages)
+    add = r.integers(0, 100, S)
+    order = r.permutation(S)
+    start, missing = K.pages_extend(pages, dev(add), seq=dev(order))
+    want, lack = b.extend(order, add)
+    assert start.tolist() == want and missing.item() == lack
+    same_book(pages, b)
+
+
+def test_corrupt_bookkeeping_stays_in_bounds(K):
+    """Lengths, counts and page numbers that no call made: what the header promises, nothing else touched."""
+    pages, _, _ = _filled(K, 1, 1, 64, 32, [50, 50, 50], extra_slots=3)
+    pages.length.copy_(dev([1 << 30, -7, 50, 0, 0, 0]))
+    pages.held.copy_(dev([1 << 30, 2, -3, 0, 0, 0]))
+    pages.table[0].fill_(-(1 << 31))
+    refs = pages.refs.clone()
+    done, _ = K.pages_fork(pages, dev([0, 1, 2]), dev([3, 4, 5]))
+    assert done.tolist() == [1, 1, 1] and pages.length[3:].tolist() == [pages.c.M * 32, 0, 0]
+    assert torch.equal(pages.refs, refs)
+    q = normal((1, 6, 2, 64), "bf16", 1).cuda()
+    assert not K.decode_pages(q, pages).any()
+    K.pages_free(pages, dev([0, 2, 3]))
+    assert torch.equal(pages.refs, refs)
+    start, _ = K.pages_extend(pages, dev([1]), seq=dev([1]))
+    assert start.tolist() == [0]
+
+
+# ---------------------------------------------------------------------------
+# decode
+# ---------------------------------------------------------------------------
+
+def _decode_ref(q, k, v, G):
+    """float64 decode of one (layer, sample): q [Hq, d], k, v [Hkv, n, d]; (out, weighted magnitudes, largest logit)."""
+    out, mag, top = [], [], 0.0
+    for h in range(q.shape[0]):
+        kk, vv = k[h // G], v[h // G]
+        if kk.shape[0] == 0:
+            out.append(np.zeros(q.shape[1]))
+            mag.append(np.zeros(q.shape[1]))
+            continue
+        x = kk @ q[h] / np.sqrt(q.shape[1])
+        top = max(top, float(np.abs(x).max()))
+        w = np.exp(x - x.max())
+        w /= w.sum()
+        out.append(w @ vv)
+        mag.append(w @ np.abs(vv))
+    return np.stack(out), np.stack(mag), top
+
+
+DECODES = [  # Hkv, G, d, page, lengths, max_tokens, dtype, scale of the queries
+    (1, 1, 64, 32, [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65], None, "bf16", 1.0),
+    (2, 4, 128, 32, [0, 1, 31, 32, 33, 127, 128, 129, 300], None, "bf16", 1.0),
+    (2, 3, 128, 64, [5, 700, 1639], 1639, "bf16", 1.0),
+    (1, 8, 128, 1024, [4000, 1, 2047], None, "bf16", 1.0),
+    (1, 16, 128, 64, [333, 20], None, "bf16", 1.0),
+    (3, 5, 64, 128, [1000, 64, 0], None, "bf16", 1.0),
+    (1, 16, 64, 64, [190], None, "f32", 1.0),
+    (2, 4, 128, 64, [600, 31], None, "f32", 1.0),
+    (2, 4, 64, 32, [5003, 1200], None, "f32", 1.0),
+    (2, 4, 128, 64, [600, 90], None, "bf16", 40.0),     # logits of hundreds: the reference is raised again and again
+    (1, 7, 128, 64, [900, 90], None, "f32", 40.0),
+    (1, 2, 128, 64, [600], 350, "bf16", 1.0),           # fewer tokens than the sequence has
+    (1, 4, 128, 32, [70000, 3], None, "bf16", 1.0),     # many splits
+]
+
+
+@pytest.mark.parametrize("Hkv,G,d,page,lengths,most,dtype,qs", DECODES)
+def test_decode(K, Hkv, G, d, page, lengths, most, dtype, qs):
+    L, B, Hq = (2 if max(lengths) < 5000 else 1), len(lengths), Hkv * G
+    pages, _, _ = _filled(K, L, Hkv, d, page, lengths, seed=G, extra_slots=1)
+    r = np.random.default_rng(G)
+    order = r.permutation(B)
+    q = normal((L, B, Hq, d), dtype, 77, qs).cuda()
+    out = torch.full((L, B, Hq, d), float("nan"), device="cuda")
+    K.decode_pages(q, pages, max_tokens=most, seq=dev(order), out=out)
+    worst = 0.0
+    qn, on = q.double().cpu().numpy(), out.double().cpu().numpy()
+    for i, s in enumerate(order):
+        n = lengths[s] if most is None else min(lengths[s], most)
+        k, v = rows_of(pages, int(s), n)
+        for l in range(L):
+            want, mag, top = _decode_ref(qn[l, i], k[l], v[l], G)
+            worst = max(worst, check_decode(on[l, i], want, mag, top, f"length {n} layer {l}"))
+    report(f"paged decode worst err/bound g{G} d{d} {dtype} x{qs:g}", round(worst, 4))
+
+
+def test_decode_equals_decode_over_the_rows_read_back(K):
+    """The same rows dense in bf16: decode_attention gives the same to float32 rounding."""
+    lengths = [700, 64, 0, 333]
+    pages, _, _ = _filled(K, 1, 4, 128, 64, lengths)
+    k, v = K.pages_read(pages, 700)
+    q = normal((1, 4, 16, 128), "bf16", 3).cuda()
+    a = K.decode_pages(q, pages, max_tokens=700)
+    count = dev(lengths)[None, :, None].expand(1, 4, 4).contiguous()
+    b = K.decode_attention(q, k, v, count)
+    k64, v64 = k.double().cpu().numpy(), v.double().cpu().numpy()
+    for s, n in enumerate(lengths):
+        want, mag, top = _decode_ref(q[0, s].double().cpu().numpy(), k64[0, s, :, :n], v64[0, s, :, :n], 4)
+        check_decode(a[0, s].cpu().numpy(), want, mag, top)
+        check_decode(b[0, s].cpu().numpy(), want, mag, top)
+
+
+def test_decode_leaves_out_missing_pages_and_passes_nan_on(K):
+    L, Hkv, G, d, page = 1, 2, 4, 128, 32
+    lengths = [100, 100, 100, 100, 20]
+    pages, _, _ = _filled(K, L, Hkv, d, page, lengths)
+    q = normal((L, 5, Hkv * G, d), "bf16", 4).cuda()
+    pages.table[0, 1] = -1
+    pages.table[1, 0], pages.table[1, 3] = pages.c.n_pages, 1 << 30
+    pages.table[2, :4] = -1
+    k, v = rows_of(pages, 3)
+    half = page * d // 2
+    pages.pool[0, int(pages.table[3, 2]), 0, 2 * half + 5] = 255     # a key block of KV head 0
+    pages.pool[0, int(pages.table[4, 0]), 1, 2 * half + page * d // 32 + 3 * page + 7] = 255  # a value block of head 1
+    out = K.decode_pages(q, pages).double().cpu().numpy()[0]
+    qn = q.double().cpu().numpy()[0]
+    for s, keep in ((0, [0, 2, 3]), (1, [1, 2])):
+        ids = [int(pages.table[s, i]) for i in keep]
+        kk, vv = O.page_unpack(pages.pool.cpu().numpy()[0][ids].transpose(1, 0, 2), page, d)
+        n = sum(min(32, 100 - 32 * i) for i in keep)
+        kk, vv = kk.reshape(Hkv, -1, d)[:, :n], vv.reshape(Hkv, -1, d)[:, :n]
+        want, mag, top = _decode_ref(qn[s], kk, vv, G)
+        check_decode(out[s], want, mag, top)
+    assert not out[2].any()
+    assert np.isnan(out[3, :G]).all()
+    want, mag, top = _decode_ref(qn[3], k[0], v[0], G)
+    check_decode(out[3, G:], want[G:], mag[G:], top)
+    assert np.isfinite(out[4, :G]).all()
+    assert np.isnan(out[4, G:, 96:]).all() and np.isfinite(out[4, G:, :96]).all()
+    # slots outside read as empty
+    assert not K.decode_pages(q[:, :2], pages, seq=dev([-1, 5])).any()
+
+
+# ---------------------------------------------------------------------------
+# together
+# ---------------------------------------------------------------------------
+
+def _step(K, pages, k, v, q, seq, one, out, start, missing, ws_book, ws, most):
+    """One decode step: room for the new token, its rows, attention over all of them."""
+    K.pages_extend(pages, one, seq=seq, start=start, missing=missing, workspace=ws_book)
+    K.pages_append(k, v, pages, start, seq=seq)
+    K.decode_pages(q, pages, max_tokens=most, seq=seq, out=out, workspace=ws)
+
+
+def test_captured_decode_loop(K):
+    """A captured step replayed over 70 tokens (pages are taken on the way) equals the eager loop, and an eager step
+    on a second cache between the replays changes neither."""
+    L, B, Hkv, G, d, page, n0, steps = 2, 3, 2, 4, 128, 32, 50, 70
+    lengths = [n0, 1, 33]
+    qs = normal((steps, L, B, Hkv * G, d), "bf16", 1).cuda()
+    ks, vs = normal((steps, L, B, Hkv, 1, d), "bf16", 2).cuda(), normal((steps, L, B, Hkv, 1, d), "bf16", 3).cuda()
+
+    def fresh():
+        pages, _, _ = _filled(K, L, Hkv, d, page, lengths, spare=20)
+        table = torch.full((B, 6), -1, dtype=torch.int32, device="cuda")
+        table[:, :pages.c.M] = pages.table
+        pages = K.Pages(pages.pool, pages.refs, table, pages.held, pages.length, page, d)
+        most = 6 * page
+        bufs = dict(out=torch.zeros((L, B, Hkv * G, d), device="cuda"), start=dev([0] * B), missing=dev([0]),
+                    ws_book=torch.empty(K.pages_workspace_size(pages.c.n_pages, B, B), dtype=torch.uint8, device="cuda"),
+                    ws=torch.empty(K.decode_pages_workspace_size(L, B, Hkv * G, Hkv, most, d), dtype=torch.uint8,
+                                   device="cuda"), seq=dev([2, 0, 1]), one=dev([1] * B), most=most)
+        return pages, bufs
+
+    pages, bufs = fresh()
+    want = []
+    for i in range(steps):
+        _step(K, pages, ks[i], vs[i], qs[i], **bufs)
+        want.append(bufs["out"].clone())
+    end = [x.clone() for x in (pages.refs, pages.held, pages.length)]
+
+    pages, bufs = fresh()
+    other, obufs = fresh()
+    q, k, v = qs[0].clone(), ks[0].clone(), vs[0].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        _step(K, pages, k, v, q, **bufs)
+    for i in range(steps):
+        q.copy_(qs[i]); k.copy_(ks[i]); v.copy_(vs[i])
+        graph.replay()
+        if i % 9 == 0:
+            _step(K, other, ks[i], vs[i], qs[i], **obufs)
+            torch.cuda.synchronize()
+        assert torch.equal(bufs["out"], want[i]), i
+        assert bufs["missing"].item() == 0
+    for a, b in zip(end, (pages.refs, pages.held, pages.length)):
+        assert torch.equal(a, b)
+
+
+def test_calls_on_another_stream(K):
+    lengths = [700, 64]
+    pages, _, _ = _filled(K, 1, 2, 128, 64, lengths, extra_slots=2, spare=30)
+    q = normal((1, 2, 8, 128), "bf16", 3).cuda()
+    want = K.decode_pages(q, pages, seq=dev([0, 1]))
+    src, dst, one = dev([0, 1]), dev([2, 3]), dev([2])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())      # all inputs are made before this
+    done, _ = K.pages_fork(pages, src, dst, stream=s)
+    got = K.decode_pages(q, pages, seq=dst, stream=s)
+    k, _ = K.pages_read(pages, 700, seq=one, stream=s)
+    s.synchronize()
+    assert done.tolist() == [1, 1] and torch.equal(got, want)
+    assert np.array_equal(k[0, 0].double().cpu().numpy(), rows_of(pages, 0)[0][0])
+
+
+def test_forked_sequences_go_their_own_ways(K):
+    """Children share the parent's full pages, write behind them, and outlive it; freed pages are used again."""
+    L, Hkv, d, page = 2, 2, 64, 32
+    pages, k0, v0 = _filled(K, L, Hkv, d, page, [75], extra_slots=3, spare=6)
+    done, _ = K.pages_fork(pages, dev([0, 0]), dev([1, 2]))
+    assert done.tolist() == [1, 1]
+    x = normal((L, 3, Hkv, 40, d), "bf16", 8).cuda()
+    new = dev([1, 40, 23])
+    start, missing = K.pages_extend(pages, new, seq=dev([0, 1, 2]))
+    K.pages_append(x, x, pages, start, n_new=new, seq=dev([0, 1, 2]))
+    K.pages_free(pages, dev([0]))
+    y = normal((L, 1, Hkv, 64, d), "bf16", 9).cuda()
+    start, missing = K.pages_extend(pages, dev([64]), seq=dev([3]))   # takes what the parent left
+    assert missing.item() == 0
+    K.pages_append(y, y, pages, start, seq=dev([3]))
+    base = O.mx4_round(k0[:, 0].double().cpu().numpy())
+    more = O.mx4_round(x.double().cpu().numpy())
+    for slot, n in ((1, 40), (2, 23)):
+        k, _ = rows_of(pages, slot)
+        assert np.array_equal(k[:, :, :75], base) and np.array_equal(k[:, :, 75:], more[:, slot, :, :n])
+    assert np.array_equal(rows_of(pages, 3)[1], O.mx4_round(y[:, 0].double().cpu().numpy()))
+    K.pages_free(pages)
+    assert not pages.refs.any()

@@ -248,6 +248,20 @@ __global__ __launch_bounds__(kThreads) void decode_split(const T* __restrict__ q
     }
 }
 
+// Merge the splits of the (segment, head) rows: kMergeWaves / WPR rows per
+// workgroup, ws_o [segments * nsplit, G, D], ws_ml [segments * nsplit, G].
+template <int D, int WPR>
+__global__ __launch_bounds__(kThreads) void decode_combine(const float* __restrict__ ws_o,
+                                                           const float2* __restrict__ ws_ml, int G, int nsplit,
+                                                           int n_rows, float* __restrict__ out) {
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = blockIdx.x * (kWaves / WPR) + wv / WPR;
+    const int row = min(r, n_rows - 1);  // no early return: the workgroup has a barrier
+    const int seg = row / G, h = row - (row / G) * G;
+    const size_t base = (size_t)seg * nsplit * G + h;
+    merge_row<D, WPR, false>(ws_o + base * D, ws_ml + base, G, nsplit, r < n_rows, out + (size_t)row * D);
+}
+
 template <typename T, int D, int NH>
 hipError_t run_decode(const void* q, const void* kc, const void* vc, const int32_t* count, int L, int B,
                       int Hq, int Hkv, int k_cap, float scale, float* out, void* ws, hipStream_t st) {
@@ -258,7 +272,15 @@ hipError_t run_decode(const void* q, const void* kc, const void* vc, const int32
     hipLaunchKernelGGL((decode_split<T, D, NH>), dim3((unsigned)((size_t)p.segs * p.nsplit)), dim3(kThreads), 0,
                        st, static_cast<const T*>(q), static_cast<const T*>(kc), static_cast<const T*>(vc), count,
                        p.G, k_cap, p.nsplit, p.split_keys, scale * kLog2e, wo, wml, out);
-    launch_merge<D, false>(wo, wml, p.G, p.nsplit, p.segs * p.G, out, st);
+    const int rows = p.segs * p.G;
+    // one split: nothing to merge.  Up to 16: one wave per row; more: four, which
+    // cut the chain of loads (kAhead splits per round trip) in four
+    if (p.nsplit > 16)
+        hipLaunchKernelGGL((decode_combine<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, wo, wml, p.G,
+                           p.nsplit, rows, out);
+    else if (p.nsplit > 1)
+        hipLaunchKernelGGL((decode_combine<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0,
+                           st, wo, wml, p.G, p.nsplit, rows, out);
     return hipGetLastError();
 }
 

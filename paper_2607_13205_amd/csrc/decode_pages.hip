@@ -16,9 +16,16 @@
 // channel: the scaled conversion gives two channels of a token, and a byte
 // permutation pairs the tokens.
 //
+// With up to four heads per KV head the sixteen columns hold every head three
+// times, and each copy's lanes make another of the three parts of the weights: a
+// third of the second products, and fewer vector instructions, which are what
+// bounds the kernel beside the loads.  With up to eight they hold every head
+// twice: the first copy takes the top and the last part, the second the middle one.
+//
 // Split-K and the lazy softmax reference are those of the dense decode
 // (decode.hip): weights are exp2(x - m) with m raised only when a logit exceeds it
-// by more than 64.
+// by more than 64.  The denominators are one more row of the second product, a
+// row of ones.
 #include <type_traits>
 
 #include "kve_decode_merge.h"
@@ -32,9 +39,11 @@ namespace {
 constexpr int kThreads = kMergeThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBlk = 32;    // tokens per wave step
-constexpr int kHeads = kPagesMaxGroup;
+constexpr int kSplitTries = 4;
 
-typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+// Waves per SIMD that the registers are kept to, and so workgroups per compute unit.
+template <typename T, int D, int NH>
+constexpr int kPerSimd = D == 128 && (std::is_same<T, float>::value || NH > 8) ? 3 : 4;
 
 // Eight bf16, the high halves of eight floats.
 __device__ __forceinline__ bf16x8 high_halves(const uint32_t (&x)[8]) {
@@ -98,159 +107,370 @@ __device__ __forceinline__ void unpack_tokens(const uint32_t (&w)[8], const floa
     odd = __builtin_bit_cast(bf16x8, o);
 }
 
-// One workgroup per (segment, split); its waves take 32 tokens in turn.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void pages_split(const T* __restrict__ q, PagePool p,
-                                                        const int32_t* __restrict__ seq, int B, int G,
-                                                        int max_tokens, int nsplit, int split_keys, float sl2,
-                                                        float* __restrict__ ws_o, float2* __restrict__ ws_ml,
-                                                        float* __restrict__ out) {
-    constexpr int NP = std::is_same<T, float>::value ? 3 : 1;  // bf16 parts of a query
-    constexpr int NK = D / 32;                                 // products per 16 tokens: dwords of a lane's quarter row
-    constexpr int NC = D / 16;                                 // channels per lane of V^T
-    __shared__ float s_ml[kWaves][2][kHeads];
-    __shared__ float s_o[kWaves][kHeads][D];
-
-    const int seg = blockIdx.x / nsplit;
-    const int sp = blockIdx.x - seg * nsplit;
-    const int j = seg % p.Hkv, lb = seg / p.Hkv;
-    const int l = lb / B, b = lb - l * B;
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int c = lane & 15, quarter = lane >> 4;
+// Tokens that sample b has for a decode.
+__device__ __forceinline__ int tokens_of(const PagePool& p, const int32_t* seq, int b, int max_tokens) {
     const int slot = slot_of(seq, b, p.S);
-    const int n = slot < 0 ? 0 : min(length_of(p, slot), max_tokens);
-    const int k0 = sp * split_keys;
-    const int k1 = min(n, k0 + split_keys);
-    const int page = 1 << p.shift;
+    return slot < 0 ? 0 : min(length_of(p, slot), max_tokens);
+}
 
-    bf16x8 qf[NK][NP];
+__device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
-    for (int s = 0; s < NK; ++s) {
-        if constexpr (NP == 1) {
-            u32x4 x = zero16();
-            if (c < G) x = ld16(q + ((size_t)seg * G + c) * D + D / 4 * quarter + 8 * s);
-            qf[s][0] = __builtin_bit_cast(bf16x8, x);
-        } else {
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                x[i] = c < G ? (float)q[((size_t)seg * G + c) * D + D / 4 * quarter + 8 * s + i] : 0.0f;
-            split3(x, qf[s]);
-        }
+    for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+__device__ __forceinline__ int quanta_of(const PagePool& p, const int32_t* seq, int b, int B, int max_tokens) {
+    return b < B ? (tokens_of(p, seq, b, max_tokens) + kDecodeQuantum - 1) / kDecodeQuantum : 0;
+}
+
+// How the sequences are cut (PagesPlan): quanta per split, such that the splits
+// are at most `share`, or at most share + B where a few tries find no such size.
+// Every wave works it out for itself, 64 sequences at a time.
+__device__ __forceinline__ int split_quanta(const PagePool& p, const int32_t* seq, int B, int max_tokens, int share) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int q0 = quanta_of(p, seq, lane, B, max_tokens);  // the first 64: loaded once
+    long long total = __builtin_amdgcn_readfirstlane(wave_sum(q0));
+    for (int b0 = kWave; b0 < B; b0 += kWave)
+        total += __builtin_amdgcn_readfirstlane(wave_sum(quanta_of(p, seq, b0 + lane, B, max_tokens)));
+    int per = (int)max(1LL, (total + share - 1) / share);
+    for (int tries = 0; tries < kSplitTries; ++tries) {
+        int splits = __builtin_amdgcn_readfirstlane(wave_sum((q0 + per - 1) / per));
+        for (int b0 = kWave; b0 < B; b0 += kWave)
+            splits += __builtin_amdgcn_readfirstlane(
+                wave_sum((quanta_of(p, seq, b0 + lane, B, max_tokens) + per - 1) / per));
+        if (splits <= share) break;
+        per = max(per + 1, (int)((long long)per * splits / share));
     }
-    float m = -INFINITY, den = 0.0f;
-    f32x4 o[NC];
-#pragma unroll
-    for (int i = 0; i < NC; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    return per;
+}
 
-    for (int t0 = k0 + wv * kBlk; t0 < k1; t0 += kWaves * kBlk) {
-        const int pg = p.table[(size_t)slot * p.M + (t0 >> p.shift)];
-        if (pg < 0 || pg >= p.n_pages) continue;
-        const char* block = page_block<D>(p, l, pg, j);
-        const int tok = t0 & (page - 1);
-        const int left = k1 - t0;  // tokens of this step
+// Splits before and of a sequence.
+struct SplitRange {
+    int first, count;
+};
 
-        // keys: a quarter row per lane and tile, and the scales of eight tokens
-        uint32_t kw[2][NK];
+// The sequence that split x belongs to, or -1, and its range.  ranges: where not
+// null, every sequence's range is written there (by one wave).
+__device__ __forceinline__ int find_split(const PagePool& p, const int32_t* seq, int B, int max_tokens, int per,
+                                          int x, SplitRange& r, SplitRange* ranges) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int before = 0, found = -1;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+        const int n = (quanta_of(p, seq, b0 + lane, B, max_tokens) + per - 1) / per;
+        int inc = n;
 #pragma unroll
-        for (int tile = 0; tile < 2; ++tile) {
-            const char* row = block + (size_t)(tok + 8 * (c >> 2) + 4 * tile + (c & 3)) * (D / 2) + quarter * (D / 8);
-#pragma unroll
-            for (int s = 0; s < NK; ++s) kw[tile][s] = reinterpret_cast<const uint32_t*>(row)[s];
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int y = __shfl_up(inc, o);
+            if (lane >= o) inc += y;
         }
-        const char* scales = block + (size_t)page * D;
-        const u32x2 ks = *reinterpret_cast<const u32x2*>(scales + (size_t)(quarter * D / 128) * page + tok + 8 * (c >> 2));
-        // values: NC channels of eight tokens
-        uint32_t vw[8];
+        const int first = before + inc - n;
+        if (ranges != nullptr && b0 + lane < B) ranges[b0 + lane] = SplitRange{first, n};
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(x >= first && x < first + n);
+        if (mask != 0) {
+            const int at = __builtin_ctzll(mask);
+            r.first = __builtin_amdgcn_readlane(first, at);
+            r.count = __builtin_amdgcn_readlane(n, at);
+            found = b0 + at;
+            if (ranges == nullptr) return found;
+        }
+        before += __builtin_amdgcn_readlane(inc, kWave - 1);
+    }
+    return found;
+}
+
+// What a wave loads for 32 tokens: a quarter row per lane and tile of the keys
+// and their scales, NC channels of eight tokens of the values and theirs.
+// block: the page of this (layer, KV head); tok: the first token in it, both the
+// same for all lanes, whose own offsets do not change.
+template <int D>
+struct Step {
+    static constexpr int NK = D / 32;
+    uint32_t k[2][NK], v[8];
+    u32x2 ks, vs;
+
+    __device__ __forceinline__ void load_keys(const char* block, int tok, int shift) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int c = lane & 15, quarter = lane >> 4;
+        const char* keys = block + tok * (D / 2);
+        const char* scales = block + ((size_t)D << shift) + tok;
+        const uint32_t at = (8 * (c >> 2) + (c & 3)) * (D / 2) + quarter * (D / 8);
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+            for (int s = 0; s < NK; ++s)
+                k[tile][s] = reinterpret_cast<const uint32_t*>(keys + at + tile * 4 * (D / 2))[s];
+        ks = *reinterpret_cast<const u32x2*>(scales + (uint32_t)(((quarter * D / 128) << shift) + 8 * (c >> 2)));
+    }
+
+    __device__ __forceinline__ void load_values(const char* block, int tok, int shift) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int c = lane & 15, quarter = lane >> 4;
+        const char* values = block + ((size_t)(D / 2) << shift) + tok * (D / 2);
+        const char* scales = block + ((size_t)D << shift) + tok;
+        const uint32_t at = 8 * quarter * (D / 2) + c * (D / 32);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const char* row = block + (size_t)page * (D / 2) + (size_t)(tok + 8 * quarter + i) * (D / 2) + c * (D / 32);
             if constexpr (D == 128)
-                vw[i] = *reinterpret_cast<const uint32_t*>(row);
+                v[i] = *reinterpret_cast<const uint32_t*>(values + at + i * (D / 2));
             else
-                vw[i] = *reinterpret_cast<const uint16_t*>(row);
+                v[i] = *reinterpret_cast<const uint16_t*>(values + at + i * (D / 2));
         }
-        u32x2 vs = *reinterpret_cast<const u32x2*>(scales + (size_t)(D / 32 + c * (D / 16) / 32) * page + tok + 8 * quarter);
+        vs = *reinterpret_cast<const u32x2*>(scales +
+                                             (uint32_t)(((D / 32 + c * (D / 16) / 32) << shift) + 8 * quarter));
+    }
+};
 
-        f32x4 acc[2];
+// x[i + N] of the sixteen lanes of a row, 0 behind them.
+template <int N>
+__device__ __forceinline__ float row_from(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x100 + N, 0xf, 0xf,
+                                                                 true));
+}
+
+// The running softmax sums of a wave over its tokens.  NH: up to 4 heads of three
+// columns each, 8 of two, or 16.
+template <typename T, int D, int NH>
+struct Sums {
+    static constexpr int NP = std::is_same<T, float>::value ? 3 : 1;  // bf16 parts of a query
+    static constexpr int NK = D / 32;  // products per 16 tokens: dwords of a lane's quarter row
+    static constexpr int NC = D / 16;  // channels per lane of V^T
+    static constexpr int NW = NH == 4 ? 1 : NH == 8 ? 2 : 3;  // parts of the weights per lane
+    bf16x8 q[NK][NP];
+    float m;
+    f32x4 den, o[NC];  // o[i][r]: channel NC (4 (lane / 16) + r) + i of column lane % 16
+
+    __device__ __forceinline__ void start(const T* rows, int G) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int c = lane & 15, quarter = lane >> 4, h = c & (NH - 1);
+        const bool used = h < G && c < (NH == 4 ? 12 : 16);
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+            if constexpr (NP == 1) {
+                u32x4 y = zero16();
+                if (used) y = ld16(rows + (size_t)h * D + D / 4 * quarter + 8 * s);
+                q[s][0] = __builtin_bit_cast(bf16x8, y);
+            } else {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    y[i] = used ? (float)rows[(size_t)h * D + D / 4 * quarter + 8 * s + i] : 0.0f;
+                split3(y, q[s]);
+            }
+        }
+        m = -INFINITY;
+        den = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NC; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    // The logits of 32 tokens, before scaling.
+    __device__ __forceinline__ void logits(const Step<D>& st, f32x4 (&acc)[2]) const {
+        const int c = threadIdx.x & 15;
 #pragma unroll
         for (int tile = 0; tile < 2; ++tile) {
-            const float sc = scale_float((ks[tile] >> (8 * (c & 3))) & 0xffu);
+            const float sc = scale_float((st.ks[tile] >> (8 * (c & 3))) & 0xffu);
             acc[tile] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int s = 0; s < NK; ++s) {
-                const bf16x8 kf = unpack8(kw[tile][s], sc);
+                const bf16x8 kf = unpack8(st.k[tile][s], sc);
 #pragma unroll
-                for (int a = NP - 1; a >= 0; --a) acc[tile] = mma(kf, qf[s][a], acc[tile]);
+                for (int a = NP - 1; a >= 0; --a) acc[tile] = mma(kf, q[s][a], acc[tile]);
             }
         }
-        float x[8];
-        bool raise = false;
+    }
+
+    // The tokens' share of the sums; the first `left` (at least one) count.
+    __device__ __forceinline__ void add(Step<D>& st, f32x4 (&acc)[2], int left, float sl2) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int c = lane & 15, quarter = lane >> 4;
+        if (left < kBlk) {
+            // rows behind the sequence hold anything: no weight, and zeros under it
+            __builtin_amdgcn_sched_barrier(0);  // a branch, not selects in every step
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = 8 * quarter + i < left ? acc[i >> 2][i & 3] * sl2 : -INFINITY;
-            raise |= x[i] > m + 64.0f;
+            for (int i = 0; i < 8; ++i)
+                if (8 * quarter + i >= left) {
+                    acc[i >> 2][i & 3] = -INFINITY;
+                    st.v[i] = 0;
+                    st.vs[i >> 2] &= ~(0xffu << (8 * (i & 3)));
+                }
         }
-        if (__builtin_amdgcn_ballot_w64(raise) != 0) {
-            float mn = m;
+        float top = acc[0][0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) mn = fmaxf(mn, x[i]);
-            mn = fmaxf(mn, __shfl_xor(mn, 16));
-            mn = fmaxf(mn, __shfl_xor(mn, 32));
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, acc[i >> 2][i & 3]);
+        if (__builtin_amdgcn_ballot_w64(top * sl2 > m + 64.0f) != 0) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float mn = fmaxf(m, top * sl2);
             const float alpha = mn == -INFINITY ? 1.0f : fast_exp2(m - mn);
-            den *= alpha;
             m = mn;
+            den *= alpha;
 #pragma unroll
             for (int i = 0; i < NC; ++i) o[i] *= alpha;
         }
         float w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            w[i] = 8 * quarter + i < left ? fast_exp2(x[i] - m) : 0.0f;
-            den += w[i];
-        }
-        bf16x8 pf[3];
-        split3(w, pf);
-
-        // rows behind the sequence hold anything: zeros under their zero weights
-        if (left < kBlk) {
+        for (int i = 0; i < 8; ++i) w[i] = fast_exp2(fmaf(acc[i >> 2][i & 3], sl2, -m));
+        bf16x8 part[NW];
+        if constexpr (NH == 4) {
+            // columns 0..3 keep the top 8 bits, 4..7 the 8 after them, 8..11 the rest
+            const uint32_t first = c >= 4 ? 0xffff0000u : 0u, second = c >= 8 ? 0xffff0000u : 0u;
+            uint32_t bits[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (8 * quarter + i >= left) {
-                    vw[i] = 0;
-                    vs[i >> 2] &= ~(0xffu << (8 * (i & 3)));
-                }
+            for (int i = 0; i < 8; ++i) {
+                float y = w[i] - __uint_as_float(__float_as_uint(w[i]) & first);
+                y = y - __uint_as_float(__float_as_uint(y) & second);
+                bits[i] = __float_as_uint(y);
+            }
+            part[0] = high_halves(bits);
+        } else if constexpr (NH == 8) {
+            // columns 0..7 keep the top 8 bits and the last, 8..15 the middle ones
+            uint32_t bits[8], rest[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = w[i] - __uint_as_float(__float_as_uint(w[i]) & 0xffff0000u);
+                const float z = y - __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+                bits[i] = __float_as_uint(c < 8 ? w[i] : y);
+                rest[i] = __float_as_uint(z);
+            }
+            part[0] = high_halves(bits);
+            u32x4 last = __builtin_bit_cast(u32x4, high_halves(rest));
+            last &= c < 8 ? 0xffffffffu : 0u;
+            part[1] = __builtin_bit_cast(bf16x8, last);
+        } else {
+            split3(w, part);
         }
         float sc[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sc[i] = scale_float((vs[i >> 2] >> (8 * (i & 3))) & 0xffu);
-        bf16x8 vf[NC];
-        unpack_tokens<0>(vw, sc, vf[0], vf[1]);
-        unpack_tokens<1>(vw, sc, vf[2], vf[3]);
+        for (int i = 0; i < 8; ++i) sc[i] = scale_float((st.vs[i >> 2] >> (8 * (i & 3))) & 0xffu);
+        const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+        for (int a = NW - 1; a >= 0; --a) den = mma(__builtin_bit_cast(bf16x8, ones), part[a], den);
+        values<0>(st, sc, part);
+        values<1>(st, sc, part);
         if constexpr (D == 128) {
-            unpack_tokens<2>(vw, sc, vf[4], vf[5]);
-            unpack_tokens<3>(vw, sc, vf[6], vf[7]);
+            values<2>(st, sc, part);
+            values<3>(st, sc, part);
         }
-#pragma unroll
-        for (int i = 0; i < NC; ++i)
-#pragma unroll
-            for (int a = 2; a >= 0; --a) o[i] = mma(vf[i], pf[a], o[i]);
     }
 
-    den += __shfl_xor(den, 16);
-    den += __shfl_xor(den, 32);
-    if (den != den && m == -INFINITY) m = 0.0f;  // every logit was NaN: the split is not empty
+    template <int SEL>
+    __device__ __forceinline__ void values(const Step<D>& st, const float (&sc)[8], const bf16x8 (&part)[NW]) {
+        bf16x8 even, odd;
+        unpack_tokens<SEL>(st.v, sc, even, odd);
+#pragma unroll
+        for (int a = NW - 1; a >= 0; --a) {
+            o[2 * SEL] = mma(even, part[a], o[2 * SEL]);
+            o[2 * SEL + 1] = mma(odd, part[a], o[2 * SEL + 1]);
+        }
+    }
+
+    // the parts of a head's sums added up in its first column
+    __device__ __forceinline__ void finish() {
+        if constexpr (NH == 4) {
+            den[0] = den[0] + (row_from<4>(den[0]) + row_from<8>(den[0]));
+#pragma unroll
+            for (int i = 0; i < NC; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] = o[i][r] + (row_from<4>(o[i][r]) + row_from<8>(o[i][r]));
+        }
+        if constexpr (NH == 8) {
+            den[0] += row_from<8>(den[0]);
+#pragma unroll
+            for (int i = 0; i < NC; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] += row_from<8>(o[i][r]);
+        }
+        if (den[0] != den[0] && m == -INFINITY) m = 0.0f;  // every logit was NaN: the split is not empty
+    }
+};
+
+// One workgroup per split of a sequence and (layer, KV head); its waves take 32
+// tokens in turn.  The next step's keys load into the registers of this step's as
+// soon as the logits are there, its values when this step's are added.
+template <typename T, int D, int NH>
+__global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(const T* __restrict__ q, PagePool p,
+                                                                  const int32_t* __restrict__ seq, int B, int G,
+                                                                  int max_tokens, int share, int groups, int whole,
+                                                                  float sl2, float* __restrict__ ws_o,
+                                                                  float2* __restrict__ ws_ml,
+                                                                  SplitRange* __restrict__ ranges,
+                                                                  float* __restrict__ out) {
+    constexpr int NC = D / 16;
+    __shared__ float s_ml[kWaves][2][NH];
+    __shared__ float s_o[kWaves][NH][D];
+
+    const int pairs = p.L * p.Hkv;
+    const int x = blockIdx.x / pairs, pair = blockIdx.x - x * pairs;
+    const int l = pair / p.Hkv, j = pair - l * p.Hkv;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int c = lane & 15, quarter = lane >> 4;
+
+    int b = x, per = 1 << 23;
+    SplitRange range{x, 1};
+    if (!whole) {
+        per = split_quanta(p, seq, B, max_tokens, share);
+        // the first workgroup's first wave leaves the ranges for the merge
+        b = find_split(p, seq, B, max_tokens, per, x, range, blockIdx.x == 0 && wv == 0 ? ranges : nullptr);
+        if (b < 0) return;
+    }
+    const int slot = slot_of(seq, b, p.S);
+    const int n = tokens_of(p, seq, b, max_tokens);
+    const int k0 = whole ? 0 : (x - range.first) * per * kDecodeQuantum;
+    const int k1 = whole ? n : (int)min((long long)n, k0 + (long long)per * kDecodeQuantum);
+    const int page = 1 << p.shift;
+    const size_t row0 = ((size_t)l * B + b) * p.Hkv + j;  // the segment's first query row, over G
+
+    Sums<T, D, NH> sums;
+    sums.start(q + row0 * G * D, G);
+
+    // page numbers of 64 pages at a time, one per lane; a step's tokens lie in one
+    // page.  Returns the tokens that count: none where the page number is invalid.
+    const int32_t* row = p.table + (size_t)max(slot, 0) * p.M;
+    int ids = 0, ids0 = -kWave;
+    const char* block = nullptr;
+    auto find = [&](int t0) -> int {
+        const int at = t0 >> p.shift;
+        if (at >= ids0 + kWave || ids0 < 0) {
+            ids0 = at;
+            ids = row[min(at + lane, p.M - 1)];
+        }
+        const int pg = __builtin_amdgcn_readlane(ids, at - ids0);
+        const bool there = pg >= 0 && pg < p.n_pages;
+        block = page_block<D>(p, l, there ? pg : 0, j);
+        return there ? k1 - t0 : 0;
+    };
+    constexpr int kStride = kWaves * kBlk;
+    Step<D> st;
+    int t0 = k0 + wv * kBlk, left = 0;
+    if (t0 < k1) {
+        left = find(t0);
+        st.load_keys(block, t0 & (page - 1), p.shift);
+        st.load_values(block, t0 & (page - 1), p.shift);
+    }
+    while (t0 < k1) {
+        const int t1 = t0 + kStride, now = left;
+        f32x4 acc[2];
+        sums.logits(st, acc);
+        if (t1 < k1) {
+            left = find(t1);
+            st.load_keys(block, t1 & (page - 1), p.shift);
+        }
+        if (now > 0) sums.add(st, acc, now, sl2);
+        if (t1 < k1) st.load_values(block, t1 & (page - 1), p.shift);
+        t0 = t1;
+    }
+    sums.finish();
+
     if (c < G) {
         if (quarter == 0) {
-            s_ml[wv][0][c] = m;
-            s_ml[wv][1][c] = den;
+            s_ml[wv][0][c] = sums.m;
+            s_ml[wv][1][c] = sums.den[0];
         }
-        // o[i][r]: channel NC (4 quarter + r) + i of head c
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int i = 0; i < NC; ++i) s_o[wv][c][NC * (4 * quarter + r) + i] = o[i][r];
+            for (int i = 0; i < NC; ++i) s_o[wv][c][NC * (4 * quarter + r) + i] = sums.o[i][r];
     }
     __syncthreads();
     // merge the waves' partial results of this split
@@ -268,28 +488,64 @@ __global__ __launch_bounds__(kThreads) void pages_split(const T* __restrict__ q,
                 ot = fmaf(a, s_o[w][h][ch], ot);
             }
         }
-        const size_t row = (size_t)blockIdx.x * G + h;
-        if (nsplit == 1) {  // the whole segment: the result itself
-            out[row * D + ch] = lt != 0.0f ? ot / lt : 0.0f;
+        if (range.count == 1) {  // the whole sequence: the result itself
+            out[(row0 * G + h) * D + ch] = lt != 0.0f ? ot / lt : 0.0f;
         } else {
-            ws_o[row * D + ch] = ot;
-            if (ch == 0) ws_ml[row] = make_float2(mx, lt);
+            const size_t part = ((size_t)pair * groups + x) * G + h;
+            ws_o[part * D + ch] = ot;
+            if (ch == 0) ws_ml[part] = make_float2(mx, lt);
         }
     }
+}
+
+// Merge the splits of sequences that have several, and write zeros for empty
+// ones.  Rows (layer, sample, KV head, head), kMergeWaves / WPR per workgroup.
+template <int D, int WPR>
+__global__ __launch_bounds__(kThreads) void pages_merge(int Hkv, int B, int G, int groups,
+                                                        const float* __restrict__ ws_o,
+                                                        const float2* __restrict__ ws_ml,
+                                                        const SplitRange* __restrict__ ranges, int n_rows,
+                                                        float* __restrict__ out) {
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int row = blockIdx.x * (kWaves / WPR) + wv / WPR;
+    if (row >= n_rows) return;  // WPR > 1: the whole workgroup
+    const int seg = row / G, h = row - seg * G;
+    const int lb = seg / Hkv, j = seg - lb * Hkv;
+    const int l = lb / B, b = lb - l * B;
+    const SplitRange range = ranges[b];
+    if (range.count == 1) return;  // written by its only split
+    const size_t base = (((size_t)l * Hkv + j) * groups + range.first) * G + h;
+    merge_row<D, WPR, true>(ws_o + base * D, ws_ml + base, G, range.count, true, out + (size_t)row * D);
+}
+
+template <typename T, int D, int NH>
+hipError_t run_heads(const void* q, const PagePool& p, int B, int Hq, int max_tokens, const int32_t* seq, float scale,
+               float* out, void* ws, hipStream_t st) {
+    const PagesPlan plan = decode_pages_plan(p.L, B, Hq, p.Hkv, max_tokens, D);
+    const int share = max(1, kDecodeUnits * kPerSimd<T, D, NH> / plan.pairs);  // one round of workgroups
+    float* wo = static_cast<float*>(ws);
+    float2* wml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.off_ml);
+    SplitRange* ranges = reinterpret_cast<SplitRange*>(static_cast<char*>(ws) + plan.off_ranges);
+    hipLaunchKernelGGL((pages_split<T, D, NH>), dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads), 0, st,
+                       static_cast<const T*>(q), p, seq, B, plan.G, max_tokens, share, plan.groups,
+                       (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
+    // up to 16 splits: one wave per row; more: four, which cut the chain of loads in four
+    const int rows = plan.pairs * B * plan.G;
+    if (!plan.whole && share > 16)
+        hipLaunchKernelGGL((pages_merge<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, p.Hkv, B, plan.G,
+                           plan.groups, wo, wml, ranges, rows, out);
+    else if (!plan.whole)
+        hipLaunchKernelGGL((pages_merge<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st,
+                           p.Hkv, B, plan.G, plan.groups, wo, wml, ranges, rows, out);
+    return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t run(const void* q, const PagePool& p, int B, int Hq, int max_tokens, const int32_t* seq, float scale,
                float* out, void* ws, hipStream_t st) {
-    const DecodePlan plan = decode_pages_plan(p.L, B, Hq, p.Hkv, max_tokens, D);
-    char* w = static_cast<char*>(ws);
-    float* wo = reinterpret_cast<float*>(w + plan.off_o);
-    float2* wml = reinterpret_cast<float2*>(w + plan.off_ml);
-    hipLaunchKernelGGL((pages_split<T, D>), dim3((unsigned)((size_t)plan.segs * plan.nsplit)), dim3(kThreads), 0, st,
-                       static_cast<const T*>(q), p, seq, B, plan.G, max_tokens, plan.nsplit, plan.split_keys,
-                       scale * kLog2e, wo, wml, out);
-    launch_merge<D, true>(wo, wml, plan.G, plan.nsplit, plan.segs * plan.G, out, st);
-    return hipGetLastError();
+    if (Hq / p.Hkv <= 4) return run_heads<T, D, 4>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);
+    if (Hq / p.Hkv <= 8) return run_heads<T, D, 8>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);
+    return run_heads<T, D, kPagesMaxGroup>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);
 }
 
 }  // namespace

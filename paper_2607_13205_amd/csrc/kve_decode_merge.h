@@ -28,25 +28,22 @@ __device__ __forceinline__ float read_lane(float v, int lane) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
 
-// Merge the splits of a (segment, head) row and normalise: WPR waves per row,
-// each a contiguous share of the splits, 64 at a time: lane s takes the
-// reference and denominator of split s, then the partial outputs are added
-// kAhead loads at a time.  What the merge costs is round trips to memory, not
-// bytes: a loop that loads split by split took 6.9 us for 13 splits of 128 rows.
+// The merge of one row's splits and its normalisation: WPR waves per row, each a
+// contiguous share of the splits, 64 at a time: lane s takes the reference and
+// denominator of split s, then the partial outputs are added kAhead loads at a
+// time.  What the merge costs is round trips to memory, not bytes: a loop that
+// loads split by split took 6.9 us for 13 splits of 128 rows.
+// ws_o, ws_ml: the row's first split; the next one is `step` rows on.  All waves
+// of a row must call it together; `store`: whether there is a row at all.
 // KeepNaN: a denominator that is not a number makes the row NaN, not zero.
 template <int D, int WPR, bool KeepNaN>
-__global__ __launch_bounds__(kMergeThreads) void decode_combine(const float* __restrict__ ws_o,
-                                                           const float2* __restrict__ ws_ml, int G, int nsplit,
-                                                           int n_rows, float* __restrict__ out) {
+__device__ __forceinline__ void merge_row(const float* __restrict__ ws_o, const float2* __restrict__ ws_ml, int step,
+                                          int nsplit, bool store, float* __restrict__ out) {
     constexpr int CPT = D / kWave;  // columns per lane
     constexpr int kAhead = 8;
     __shared__ float s_m[kMergeWaves], s_l[kMergeWaves], s_o[kMergeWaves][D];
     const int lane = threadIdx.x & (kWave - 1);
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int r = blockIdx.x * (kMergeWaves / WPR) + wv / WPR;
-    const int row = min(r, n_rows - 1);  // no early return: the workgroup has a barrier
-    const int seg = row / G, h = row - (row / G) * G;
-    const size_t base = (size_t)seg * nsplit;
     const int part = wv % WPR;
     const int s0 = nsplit * part / WPR, s1 = nsplit * (part + 1) / WPR;
     float mx = -INFINITY, lt = 0.0f, ot[CPT];
@@ -54,7 +51,7 @@ __global__ __launch_bounds__(kMergeThreads) void decode_combine(const float* __r
     for (int c = 0; c < CPT; ++c) ot[c] = 0.0f;
     for (int sb = s0; sb < s1; sb += kWave) {
         const int n = min(kWave, s1 - sb);
-        const float2 ml = ws_ml[(base + sb + min(lane, n - 1)) * G + h];
+        const float2 ml = ws_ml[(size_t)(sb + min(lane, n - 1)) * step];
         const float m = lane < n ? ml.x : -INFINITY;
         float mn = fmaxf(xor_max32(m), mx);
         mn = fmaxf(mn, __shfl_xor(mn, 32));
@@ -69,7 +66,7 @@ __global__ __launch_bounds__(kMergeThreads) void decode_combine(const float* __r
             float o[kAhead][CPT];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
-                const float* os = ws_o + ((base + sb + min(i + j, n - 1)) * G + h) * D + lane * CPT;
+                const float* os = ws_o + (size_t)(sb + min(i + j, n - 1)) * step * D + lane * CPT;
 #pragma unroll
                 for (int c = 0; c < CPT; ++c) o[j][c] = os[c];
             }
@@ -104,23 +101,11 @@ __global__ __launch_bounds__(kMergeThreads) void decode_combine(const float* __r
             }
         }
     }
-    if (r < n_rows) {
+    if (store) {
 #pragma unroll
-        for (int c = 0; c < CPT; ++c) out[(size_t)r * D + lane * CPT + c] = (KeepNaN ? lt != 0.0f : lt > 0.0f) ? ot[c] / lt : 0.0f;
+        for (int c = 0; c < CPT; ++c)
+            out[lane * CPT + c] = (KeepNaN ? lt != 0.0f : lt > 0.0f) ? ot[c] / lt : 0.0f;
     }
-}
-
-// ws_o [segments * nsplit, G, D], ws_ml [segments * nsplit, G], out [n_rows, D].
-// One split: nothing to merge.  Up to 16: one wave per row; more: four, which
-// cut the chain of loads (kAhead splits per round trip) in four.
-template <int D, bool KeepNaN>
-void launch_merge(const float* ws_o, const float2* ws_ml, int G, int nsplit, int n_rows, float* out, hipStream_t st) {
-    if (nsplit > 16)
-        hipLaunchKernelGGL((decode_combine<D, kMergeWaves, KeepNaN>), dim3((unsigned)n_rows), dim3(kMergeThreads), 0, st, ws_o,
-                           ws_ml, G, nsplit, n_rows, out);
-    else if (nsplit > 1)
-        hipLaunchKernelGGL((decode_combine<D, 1, KeepNaN>), dim3((unsigned)((n_rows + kMergeWaves - 1) / kMergeWaves)),
-                           dim3(kMergeThreads), 0, st, ws_o, ws_ml, G, nsplit, n_rows, out);
 }
 
 }  // namespace

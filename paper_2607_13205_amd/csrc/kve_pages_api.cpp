@@ -235,8 +235,8 @@ kve_status_t kve_decode_pages(const void* q, kve_dtype_t dtype, const kve_pages_
     if (!(std::isfinite(scale) && scale >= 0.0f))
         return fail(KVE_ERR_INVALID_ARG, "%s: scale must be finite and >= 0", fn);
     if ((double)pages->L * B * Hq > (double)kMaxGroups) return fail(KVE_ERR_UNSUPPORTED, "%s: shape too large", fn);
-    const kve::DecodePlan plan = kve::decode_pages_plan(pages->L, B, Hq, pages->Hkv, max_tokens, pages->d);
-    if ((long long)plan.segs * plan.nsplit > kMaxGroups)
+    const kve::PagesPlan plan = kve::decode_pages_plan(pages->L, B, Hq, pages->Hkv, max_tokens, pages->d);
+    if ((long long)plan.pairs * plan.groups > kMaxGroups)
         return fail(KVE_ERR_UNSUPPORTED, "%s: shape too large", fn);
     if (workspace_bytes < plan.total || workspace == nullptr)
         return fail(KVE_ERR_WORKSPACE, "%s: workspace of %zu bytes < %zu needed", fn, workspace_bytes, plan.total);

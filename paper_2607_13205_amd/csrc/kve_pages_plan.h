@@ -36,10 +36,36 @@ inline size_t pages_workspace(int n_pages, int n) {
     return align_up((size_t)n * 16) + align_up((size_t)n_pages * sizeof(int32_t));
 }
 
-// Plan of a decode over pages: max_tokens rows per segment in splits of whole
-// 128-row quanta, as over a dense cache.
-inline DecodePlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens, int d) {
-    return decode_plan(L, B, Hq, Hkv, max_tokens, d);
+// Plan of a decode over pages.  The lengths are on the device, so the splits are
+// cut there: in whole quanta of kDecodeQuantum tokens, equal for all sequences, the
+// fewest that make at most `share` splits (one round of resident workgroups over
+// all (layer, KV head) pairs) or, where one per sequence is more than that, at
+// most share + B.  The sequences' splits are numbered one after the other, and
+// workgroup x of each pair takes split x.
+struct PagesPlan {
+    int pairs, G, groups;  // groups: workgroups per (layer, KV head)
+    bool whole;            // one split per sequence: nothing to merge
+    size_t off_ml, off_ranges, total;
+};
+
+constexpr int kPagesMostResident = 4 * kDecodeUnits;  // workgroups, at four per compute unit
+
+inline PagesPlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens, int d) {
+    PagesPlan p{};
+    p.pairs = L * Hkv;
+    p.G = Hq / Hkv;
+    const long long quanta = ((long long)max_tokens + kDecodeQuantum - 1) / kDecodeQuantum;
+    p.whole = quanta == 1 || ((long long)p.pairs * B >= kPagesMostResident && quanta <= kDecodeLongest);
+    const int share = p.pairs < kPagesMostResident ? kPagesMostResident / p.pairs : 1;
+    long long groups = (long long)share + B;
+    if (groups > B * quanta) groups = B * quanta;
+    if (p.whole) groups = B;
+    p.groups = (int)groups;
+    const size_t parts = p.whole ? 0 : (size_t)p.pairs * p.groups * p.G;
+    p.off_ml = align_up(parts * d * sizeof(float));
+    p.off_ranges = p.off_ml + align_up(parts * 2 * sizeof(float));
+    p.total = p.off_ranges + align_up((size_t)B * 2 * sizeof(int32_t));  // every sequence's first split and count
+    return p;
 }
 
 }  // namespace kve

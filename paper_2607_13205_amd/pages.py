@@ -9,8 +9,8 @@ does not pass, and forward raw device pointers and the current HIP stream (or
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 from dataclasses import dataclass, field
 
 from . import binding as kb
@@ -23,6 +23,7 @@ class _CPages(ctypes.Structure):
         (n, ctypes.c_int) for n in ("L", "n_pages", "Hkv", "d", "page", "S", "M")]
 
 
+@functools.lru_cache(maxsize=None)
 def page_bytes(page: int, d: int) -> int:
     """Bytes of a page of one layer and KV head (0 if page or d is invalid)."""
     return int(LIB.kve_page_bytes(page, d))
@@ -47,30 +48,30 @@ class Pages:
     length: object
     page: int
     d: int
-    c: object = field(init=False, repr=False, compare=False)
+    c: object = field(init=False, repr=False, compare=False)      # kve_pages_t
+    index: int = field(init=False, repr=False, compare=False)     # the device's
 
     def __post_init__(self):
         torch = kb._torch()
         pool = self.pool
         if pool.dim() != 4 or pool.dtype != torch.uint8:
             raise ValueError("pool must be uint8 [L, n_pages, Hkv, page_bytes]")
+        L, n_pages, Hkv, have = pool.shape
         nb = page_bytes(self.page, self.d)
         if nb == 0:
             raise ValueError(f"page={self.page} must be a power of two in [32, 1024] and d={self.d} 64 or 128")
-        if pool.shape[3] != nb:
-            raise ValueError(f"pool has pages of {pool.shape[3]} bytes, page={self.page} and d={self.d} make {nb}")
+        if have != nb:
+            raise ValueError(f"pool has pages of {have} bytes, page={self.page} and d={self.d} make {nb}")
         if self.table.dim() != 2:
             raise ValueError("table must be int32 [S, M]")
         S, M = self.table.shape
-        for name, shape in (("refs", (pool.shape[1],)), ("table", (S, M)), ("held", (S,)), ("length", (S,))):
-            t = getattr(self, name)
-            if t.dtype != torch.int32 or tuple(t.shape) != shape:
-                raise ValueError(f"{name} must be int32 {list(shape)}")
-            if t.device != pool.device:
-                raise ValueError(f"{name} and pool are on different devices")
-        ptr = [kb._dev(getattr(self, n), n) for n in ("pool", "refs", "table", "held", "length")]
-        object.__setattr__(self, "c", _CPages(*ptr, pool.shape[0], pool.shape[1], pool.shape[2], self.d, self.page,
-                                              S, M))
+        object.__setattr__(self, "index", pool.get_device())
+        if self.index < 0 or not pool.is_contiguous():
+            raise ValueError("pool must be a contiguous device tensor")
+        object.__setattr__(self, "c", _CPages(
+            pool.data_ptr(), _ints(self.refs, (n_pages,), "refs", self), _ints(self.table, (S, M), "table", self),
+            _ints(self.held, (S,), "held", self), _ints(self.length, (S,), "length", self), L, n_pages, Hkv, self.d,
+            self.page, S, M))
 
     @property
     def L(self) -> int:
@@ -88,85 +89,97 @@ class Pages:
 def _on(pages: Pages, stream):
     """The stream to launch on; the cache's device must be the current one."""
     torch = kb._torch()
-    if pages.pool.device.index != torch.cuda.current_device():
+    if pages.index != torch.cuda.current_device():
         raise ValueError(f"the cache is on {pages.pool.device}, the current device is {torch.cuda.current_device()}")
-    return kb._stream(stream)
+    return torch._C._cuda_getCurrentRawStream(pages.index) if stream is None else stream.cuda_stream
 
 
-def _making(stream):
-    """Allocations inside belong to ``stream`` (None: the current one)."""
-    return contextlib.nullcontext() if stream is None else kb._torch().cuda.stream(stream)
+def _new(make, stream):
+    """make(), an allocation that belongs to ``stream`` (None: the current one)."""
+    if stream is None:
+        return make()
+    with kb._torch().cuda.stream(stream):
+        return make()
+
+
+def _workspace(pages, size, workspace, stream):
+    """(tensor, its pointer and bytes): the caller's workspace, or one made here of
+    size() bytes.  The tensor has to live until the call is enqueued."""
+    torch = kb._torch()
+    if workspace is None:
+        nbytes = size()
+        workspace = _new(lambda: torch.empty(nbytes, dtype=torch.uint8, device=pages.pool.device), stream)
+    elif workspace.get_device() != pages.index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous on the cache's device")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _ints(t, shape, name, pages, optional=False):
-    """Pointer of an int32 device tensor of the given shape, or None."""
+    """Pointer of a contiguous int32 device tensor of the given shape, or None."""
     if t is None and optional:
         return None
-    if t.dtype != kb._torch().int32 or tuple(t.shape) != tuple(shape):
+    if t.dtype is not kb._torch().int32 or t.shape != shape:
         raise ValueError(f"{name} must be int32 {list(shape)}")
-    if t.device != pages.pool.device:
-        raise ValueError(f"{name} is not on the cache's device")
-    return kb._dev(t, name)
+    if t.get_device() != pages.index or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous on the cache's device")
+    return t.data_ptr()
 
 
 def _rows(k, v, pages):
-    """(pointers and strides of both, dtype code) of row tensors [L, B, Hkv, T, d]."""
-    if v.shape != k.shape or v.dtype != k.dtype:
+    """(B, T, then pointer and strides of both, dtype code) of row tensors [L, B, Hkv, T, d]."""
+    shape = k.shape
+    if v.shape != shape or v.dtype is not k.dtype:
         raise ValueError("v must match k")
-    if k.dim() != 5 or k.shape[0] != pages.L or k.shape[2] != pages.Hkv or k.shape[4] != pages.d:
+    if len(shape) != 5 or shape[0] != pages.c.L or shape[2] != pages.c.Hkv or shape[4] != pages.d:
         raise ValueError(f"k and v must be [L={pages.L}, B, Hkv={pages.Hkv}, T, d={pages.d}]")
-    if k.device != pages.pool.device or v.device != pages.pool.device:
+    if k.get_device() != pages.index or v.get_device() != pages.index:
         raise ValueError("k or v is not on the cache's device")
-    dt = kb._dtype_code(k)
-    if k.numel() == 0:
-        return k.data_ptr(), None, v.data_ptr(), None, dt
-    kp, ks = (k.data_ptr(), None) if k.is_contiguous() else kb._view(k, "k")
-    vp, vs = (v.data_ptr(), None) if v.is_contiguous() else kb._view(v, "v")
-    return kp, None if ks is None else ctypes.byref(ks), vp, None if vs is None else ctypes.byref(vs), dt
+    at = []
+    for t, name in ((k, "k"), (v, "v")):
+        if t.is_contiguous():
+            at += [t.data_ptr(), None]
+        else:
+            p, st = kb._view(t, name)
+            at += [p, ctypes.byref(st)]
+    return (shape[1], shape[3], *at, kb._dtype_code(k))
 
 
 def pages_workspace_size(n_pages: int, S: int, n: int) -> int:
     return int(LIB.kve_pages_workspace_size(n_pages, S, n))
 
 
-def _book(pages, n, workspace):
-    return kb._workspace(lambda: pages_workspace_size(pages.c.n_pages, pages.c.S, n), pages.pool.device, workspace)
+def _book(pages, n, out, missing, name, workspace, stream):
+    """Outputs and workspace of a bookkeeping call on n entries: (out, missing, workspace, their
+    pointers and the workspace's bytes)."""
+    torch = kb._torch()
+    if out is None:
+        out = _new(lambda: torch.empty(n, dtype=torch.int32, device=pages.pool.device), stream)
+    if missing is None:
+        missing = _new(lambda: torch.empty(1, dtype=torch.int32, device=pages.pool.device), stream)
+    ws, wp, wsb = _workspace(pages, lambda: pages_workspace_size(pages.c.n_pages, pages.c.S, n), workspace, stream)
+    return out, missing, ws, (_ints(out, (n,), name, pages), _ints(missing, (1,), "missing", pages), wp, wsb)
 
 
 def pages_extend(pages: Pages, add, seq=None, start=None, missing=None, workspace=None, stream=None):
     """Room for add[i] more tokens in the sequence of slot seq[i] (slot i without
     seq): pages reserved, lengths advanced.  Returns (start, missing): the lengths
     before, -1 where an entry was refused, and the pages that were lacking."""
-    torch = kb._torch()
     n = add.numel()
     st = _on(pages, stream)
-    with _making(stream):
-        if start is None:
-            start = torch.empty(n, dtype=torch.int32, device=pages.pool.device)
-        if missing is None:
-            missing = torch.empty(1, dtype=torch.int32, device=pages.pool.device)
-        ws, wsb = _book(pages, n, workspace)
-        kb._check(LIB.kve_pages_extend(ctypes.byref(pages.c), _ints(seq, (n,), "seq", pages, True),
-                                       _ints(add, (n,), "add", pages), n, _ints(start, (n,), "start", pages),
-                                       _ints(missing, (1,), "missing", pages), kb._ptr(ws), wsb, st))
+    start, missing, _ws, at = _book(pages, n, start, missing, "start", workspace, stream)
+    kb._check(LIB.kve_pages_extend(ctypes.byref(pages.c), _ints(seq, (n,), "seq", pages, True),
+                                   _ints(add, (n,), "add", pages), n, *at, st))
     return start, missing
 
 
 def pages_fork(pages: Pages, src, dst, done=None, missing=None, workspace=None, stream=None):
     """Slot dst[i] becomes a continuation of the sequence in slot src[i].  Returns
     (done, missing): 1 per entry, 0 where it was refused, and the pages lacking."""
-    torch = kb._torch()
     n = src.numel()
     st = _on(pages, stream)
-    with _making(stream):
-        if done is None:
-            done = torch.empty(n, dtype=torch.int32, device=pages.pool.device)
-        if missing is None:
-            missing = torch.empty(1, dtype=torch.int32, device=pages.pool.device)
-        ws, wsb = _book(pages, n, workspace)
-        kb._check(LIB.kve_pages_fork(ctypes.byref(pages.c), _ints(src, (n,), "src", pages),
-                                     _ints(dst, (n,), "dst", pages), n, _ints(done, (n,), "done", pages),
-                                     _ints(missing, (1,), "missing", pages), kb._ptr(ws), wsb, st))
+    done, missing, _ws, at = _book(pages, n, done, missing, "done", workspace, stream)
+    kb._check(LIB.kve_pages_fork(ctypes.byref(pages.c), _ints(src, (n,), "src", pages),
+                                 _ints(dst, (n,), "dst", pages), n, *at, st))
     return done, missing
 
 
@@ -180,8 +193,7 @@ def pages_append(k, v, pages: Pages, start, n_new=None, seq=None, stream=None):
     """Packs the first n_new[b] (all without it) of the rows k, v [L, B, Hkv, T, d]
     into positions start[b] on of the sequence in slot seq[b]; views as for
     kv_compact_strided."""
-    kp, ks, vp, vs, dt = _rows(k, v, pages)
-    B, T = k.shape[1], k.shape[3]
+    B, T, kp, ks, vp, vs, dt = _rows(k, v, pages)
     kb._check(LIB.kve_pages_append(kp, ks, vp, vs, dt, B, T, _ints(n_new, (B,), "n_new", pages, True),
                                    _ints(start, (B,), "start", pages), _ints(seq, (B,), "seq", pages, True),
                                    ctypes.byref(pages.c), _on(pages, stream)))
@@ -191,11 +203,11 @@ def pages_compact(k, v, idx, count, pages: Pages, start, seq=None, stream=None):
     """kv_compact into pages: rows idx[l, b, j, :count[l, b, j]] of k, v
     [L, B, Hkv, N, d] packed into positions start[b] on of the sequence in slot
     seq[b]."""
-    kp, ks, vp, vs, dt = _rows(k, v, pages)
-    L, B, Hkv, N, _ = k.shape
+    B, N, kp, ks, vp, vs, dt = _rows(k, v, pages)
+    shape = (pages.c.L, B, pages.c.Hkv)
     k_cap = idx.shape[-1]
-    kb._check(LIB.kve_pages_compact(kp, ks, vp, vs, dt, B, N, _ints(idx, (L, B, Hkv, k_cap), "idx", pages),
-                                    _ints(count, (L, B, Hkv), "count", pages), k_cap,
+    kb._check(LIB.kve_pages_compact(kp, ks, vp, vs, dt, B, N, _ints(idx, shape + (k_cap,), "idx", pages),
+                                    _ints(count, shape, "count", pages), k_cap,
                                     _ints(start, (B,), "start", pages), _ints(seq, (B,), "seq", pages, True),
                                     ctypes.byref(pages.c), _on(pages, stream)))
 
@@ -219,23 +231,21 @@ def pages_read(pages: Pages, T: int, seq=None, start=None, count=None, dtype=Non
     have stay as they were, zero in outputs made here."""
     torch = kb._torch()
     B = pages.c.S if seq is None else seq.numel()
-    shape = (pages.L, B, pages.Hkv, T, pages.d)
+    shape = (pages.c.L, B, pages.c.Hkv, T, pages.d)
+    st = _on(pages, stream)
     for name, t in (("k_out", k_out), ("v_out", v_out)):
         if t is not None:
             dtype = t.dtype if dtype is None else dtype
-            if tuple(t.shape) != shape or t.dtype != dtype or t.device != pages.pool.device:
-                raise ValueError(f"{name} must be {dtype} {list(shape)} on the cache's device")
+            if t.shape != shape or t.dtype is not dtype or t.get_device() != pages.index or not t.is_contiguous():
+                raise ValueError(f"{name} must be {dtype} {list(shape)}, contiguous on the cache's device")
     dtype = torch.bfloat16 if dtype is None else dtype
-    st = _on(pages, stream)
-    with _making(stream):
-        if k_out is None:
-            k_out = torch.zeros(shape, dtype=dtype, device=pages.pool.device)
-        if v_out is None:
-            v_out = torch.zeros(shape, dtype=dtype, device=pages.pool.device)
-        kb._check(LIB.kve_pages_read(ctypes.byref(pages.c), kb._dtype_code(k_out), B, T,
-                                     _ints(seq, (B,), "seq", pages, True), _ints(start, (B,), "start", pages, True),
-                                     _ints(count, (B,), "count", pages, True), kb._dev(k_out, "k_out"),
-                                     kb._dev(v_out, "v_out"), st))
+    if k_out is None:
+        k_out = _new(lambda: torch.zeros(shape, dtype=dtype, device=pages.pool.device), stream)
+    if v_out is None:
+        v_out = _new(lambda: torch.zeros(shape, dtype=dtype, device=pages.pool.device), stream)
+    kb._check(LIB.kve_pages_read(ctypes.byref(pages.c), kb._dtype_code(k_out), B, T,
+                                 _ints(seq, (B,), "seq", pages, True), _ints(start, (B,), "start", pages, True),
+                                 _ints(count, (B,), "count", pages, True), k_out.data_ptr(), v_out.data_ptr(), st))
     return k_out, v_out
 
 
@@ -250,21 +260,21 @@ def decode_pages(q, pages: Pages, max_tokens: int | None = None, seq=None, scale
     max_tokens bounds the lengths (default: what the table can hold); the work is
     split by it."""
     torch = kb._torch()
-    if q.dim() != 4 or q.shape[0] != pages.L or q.shape[3] != pages.d or q.device != pages.pool.device:
-        raise ValueError(f"q must be [L={pages.L}, B, Hq, d={pages.d}] on the cache's device")
-    L, B, Hq, d = q.shape
+    shape = q.shape
+    if len(shape) != 4 or shape[0] != pages.c.L or shape[3] != pages.d or q.get_device() != pages.index or \
+            not q.is_contiguous():
+        raise ValueError(f"q must be [L={pages.L}, B, Hq, d={pages.d}], contiguous on the cache's device")
+    L, B, Hq, d = shape
     if max_tokens is None:
         max_tokens = pages.c.M * pages.page
-    if out is not None and (tuple(out.shape) != (L, B, Hq, d) or out.dtype != torch.float32 or
-                            out.device != q.device):
-        raise ValueError("out must be float32 [L, B, Hq, d] on the cache's device")
     st = _on(pages, stream)
-    with _making(stream):
-        if out is None:
-            out = torch.empty((L, B, Hq, d), dtype=torch.float32, device=q.device)
-        ws, wsb = kb._workspace(lambda: decode_pages_workspace_size(L, B, Hq, pages.Hkv, max_tokens, d), q.device,
-                                workspace)
-        kb._check(LIB.kve_decode_pages(kb._dev(q, "q"), kb._dtype_code(q), ctypes.byref(pages.c), B, Hq,
-                                       int(max_tokens), _ints(seq, (B,), "seq", pages, True), float(scale),
-                                       kb._dev(out, "out"), kb._ptr(ws), wsb, st))
+    if out is None:
+        out = _new(lambda: torch.empty(shape, dtype=torch.float32, device=q.device), stream)
+    elif out.shape != shape or out.dtype is not torch.float32 or out.get_device() != pages.index or \
+            not out.is_contiguous():
+        raise ValueError("out must be float32 [L, B, Hq, d], contiguous on the cache's device")
+    _ws, wp, wsb = _workspace(pages, lambda: decode_pages_workspace_size(L, B, Hq, pages.Hkv, max_tokens, d),
+                              workspace, stream)
+    kb._check(LIB.kve_decode_pages(q.data_ptr(), kb._dtype_code(q), ctypes.byref(pages.c), B, Hq, int(max_tokens),
+                                   _ints(seq, (B,), "seq", pages, True), float(scale), out.data_ptr(), wp, wsb, st))
     return out

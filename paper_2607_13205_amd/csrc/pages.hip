@@ -114,136 +114,197 @@ __device__ __forceinline__ uint32_t pack_eight(const Eight<T>& x, uint32_t& s) {
 }
 
 // ---------------------------------------------------------------------------
-// rows into pages: kve_pages_append (idx null) and kve_pages_compact
+// rows: into pages (kve_pages_append, kve_pages_compact), between sequences
+// (kve_pages_select) and out of them (kve_pages_read)
 // ---------------------------------------------------------------------------
 
 constexpr int kRows = 64;  // rows per workgroup
 
-// One workgroup per (segment, kRows rows), D / 8 lanes to a row.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void pack_rows(RowView kv, RowView vv, int B, int N,
+// The rows of a call: `cap` of each of L B Hkv segments (layer, sample, KV head).
+// A workgroup takes kRows rows of one segment, or, Flat, kRows rows of all
+// segments one after the other, where a segment has few: a decode step's single
+// rows of 4096 segments would else be a workgroup each.
+struct RowGrid {
+    int B, Hkv, cap, nblk;  // nblk: workgroups per segment
+    uint32_t rows;          // of all segments (Flat)
+};
+
+constexpr int kFlatRows = 32;  // rows per segment up to which workgroups take several segments
+
+struct RowAt {
+    int m, l, b, j;  // row m of segment (l, b, j)
+    size_t seg;
+};
+
+template <bool Flat>
+__device__ __forceinline__ RowAt row_at(const RowGrid& g, int in) {
+    RowAt r;
+    uint32_t seg;
+    if constexpr (Flat) {
+        const uint32_t at = min(blockIdx.x * (uint32_t)kRows + in, g.rows - 1);
+        seg = at / (uint32_t)g.cap;
+        r.m = (int)(at - seg * g.cap);
+    } else {
+        seg = blockIdx.x / (uint32_t)g.nblk;
+        r.m = (int)(blockIdx.x - seg * g.nblk) * kRows + in;
+    }
+    const uint32_t lb = seg / (uint32_t)g.Hkv;
+    r.seg = seg;
+    r.j = (int)(seg - lb * g.Hkv);
+    r.l = (int)(lb / (uint32_t)g.B);
+    r.b = (int)(lb - (uint32_t)r.l * g.B);
+    return r;
+}
+
+// Whether a workgroup's row `in` exists (it may lie behind its segment's count).
+template <bool Flat>
+__device__ __forceinline__ bool row_there(const RowGrid& g, int in) {
+    return !Flat || blockIdx.x * (uint32_t)kRows + in < g.rows;
+}
+
+// The page block and token of position first + m of a slot for a (layer, KV
+// head); null where the position has no page or is not below `limit`.
+template <int D>
+__device__ __forceinline__ char* find_row(const PagePool& p, int slot, int first, int m, int limit, const RowAt& r,
+                                          int& tok) {
+    if (slot < 0 || first < 0 || m >= limit - first) return nullptr;
+    const int pos = first + m;
+    const int pg = p.table[(size_t)slot * p.M + (pos >> p.shift)];
+    tok = pos & ((1 << p.shift) - 1);
+    return pg >= 0 && pg < p.n_pages ? page_block<D>(p, r.l, pg, r.j) : nullptr;
+}
+
+// Byte offsets in a page block: codes of token tok from channel 8 part on, and
+// the scale byte of the channels' block; the values' are behind the keys'.
+template <int D>
+struct PageAt {
+    size_t codes, scales;
+    __device__ __forceinline__ PageAt(int tok, int part, int shift)
+        : codes((size_t)tok * (D / 2) + part * 4),
+          scales(((size_t)D << shift) + ((size_t)(part / 4) << shift) + tok) {}
+    __device__ __forceinline__ static size_t values(int shift) { return (size_t)(D / 2) << shift; }
+    __device__ __forceinline__ static size_t value_scales(int shift) { return (size_t)(D / 32) << shift; }
+};
+
+// D / 8 lanes to a row.  All of a thread's rows are looked up, then loaded, then
+// packed, so that a workgroup waits for memory once per stage.
+template <typename T, int D, bool Flat>
+__global__ __launch_bounds__(kThreads) void pack_rows(RowView kv, RowView vv, RowGrid g, int N,
                                                       const int32_t* __restrict__ idx,
-                                                      const int32_t* __restrict__ count, int cap,
+                                                      const int32_t* __restrict__ count,
                                                       const int32_t* __restrict__ start,
-                                                      const int32_t* __restrict__ seq, PagePool p, int nblk) {
+                                                      const int32_t* __restrict__ seq, PagePool p) {
     constexpr int kLanes = D / 8;
     constexpr int kStep = kThreads / kLanes;
-    const int blk = blockIdx.x % nblk, seg = blockIdx.x / nblk;
-    const int j = seg % p.Hkv, lb = seg / p.Hkv;
-    const int l = lb / B, b = lb - l * B;
-    const int n = idx != nullptr ? min(count[seg], cap) : count != nullptr ? min(count[b], cap) : cap;
-    const int slot = slot_of(seq, b, p.S), first = start[b];
-    if (blk * kRows >= n || slot < 0 || first < 0) return;
-    const int rows_held = held_of(p, slot) << p.shift;
-    const char* k = kv.base + (size_t)l * kv.s_layer + (size_t)b * kv.s_batch + (size_t)j * kv.s_head;
-    const char* v = vv.base + (size_t)l * vv.s_layer + (size_t)b * vv.s_batch + (size_t)j * vv.s_head;
+    constexpr int kItems = kRows / kStep;
     const int part = threadIdx.x % kLanes;
-    const int page = 1 << p.shift;
-    for (int m = blk * kRows + (int)threadIdx.x / kLanes; m < min(n, (blk + 1) * kRows); m += kStep) {
-        const int t = idx != nullptr ? idx[(size_t)seg * cap + m] : m;
-        if (t < 0 || t >= N || m >= rows_held - first) continue;
-        const int pos = first + m;
-        const int pg = p.table[(size_t)slot * p.M + (pos >> p.shift)];
-        if (pg < 0 || pg >= p.n_pages) continue;
-        Eight<T> x, y;
-        x.load(k + (size_t)t * kv.s_token, part);
-        y.load(v + (size_t)t * vv.s_token, part);
-        char* block = page_block<D>(p, l, pg, j);
-        const int tok = pos & (page - 1);
+    char* block[kItems];
+    int tok[kItems];
+    Eight<T> x[kItems], y[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const int in = i * kStep + threadIdx.x / kLanes;
+        const RowAt r = row_at<Flat>(g, in);
+        const int n = idx != nullptr ? min(count[r.seg], g.cap) : count != nullptr ? min(count[r.b], g.cap) : g.cap;
+        block[i] = nullptr;
+        if (row_there<Flat>(g, in) && r.m < n) {
+            const int t = idx != nullptr ? idx[r.seg * g.cap + r.m] : r.m;
+            const int slot = slot_of(seq, r.b, p.S);
+            if (t >= 0 && t < N && slot >= 0)
+                block[i] = find_row<D>(p, slot, start[r.b], r.m, held_of(p, slot) << p.shift, r, tok[i]);
+            if (block[i] != nullptr) {
+                x[i].load(kv.base + (size_t)r.l * kv.s_layer + (size_t)r.b * kv.s_batch + (size_t)r.j * kv.s_head +
+                              (size_t)t * kv.s_token, part);
+                y[i].load(vv.base + (size_t)r.l * vv.s_layer + (size_t)r.b * vv.s_batch + (size_t)r.j * vv.s_head +
+                              (size_t)t * vv.s_token, part);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        if (block[i] == nullptr) continue;  // the same for all lanes of a row
         uint32_t sk, sv;
-        const uint32_t wk = pack_eight(x, sk), wv = pack_eight(y, sv);
-        char* row = block + (size_t)tok * (D / 2) + part * 4;
-        *reinterpret_cast<uint32_t*>(row) = wk;
-        *reinterpret_cast<uint32_t*>(row + (size_t)page * (D / 2)) = wv;
+        const uint32_t wk = pack_eight(x[i], sk), wv = pack_eight(y[i], sv);
+        const PageAt<D> at(tok[i], part, p.shift);
+        *reinterpret_cast<uint32_t*>(block[i] + at.codes) = wk;
+        *reinterpret_cast<uint32_t*>(block[i] + at.codes + at.values(p.shift)) = wv;
         if (part % 4 == 0) {
-            char* scales = block + (size_t)page * D + (size_t)(part / 4) * page + tok;
-            scales[0] = (char)sk;
-            scales[(size_t)page * (D / 32)] = (char)sv;
+            block[i][at.scales] = (char)sk;
+            block[i][at.scales + at.value_scales(p.shift)] = (char)sv;
         }
     }
 }
 
-// ---------------------------------------------------------------------------
-// rows of one sequence to another, unchanged: kve_pages_select
-// ---------------------------------------------------------------------------
-
-// One workgroup per (segment, kRows rows); a lane moves a block of 32 channels
-// (16 bytes of codes, one scale byte) of a key and a value row.
-template <int D>
-__global__ __launch_bounds__(kThreads) void select_rows(PagePool p, int B, const int32_t* __restrict__ src,
+// D / 32 lanes to a row, each a block of 32 channels (16 bytes of codes, one
+// scale byte) of a key and a value row.
+template <int D, bool Flat>
+__global__ __launch_bounds__(kThreads) void select_rows(PagePool p, RowGrid g, const int32_t* __restrict__ src,
                                                         const int32_t* __restrict__ idx,
-                                                        const int32_t* __restrict__ count, int cap,
+                                                        const int32_t* __restrict__ count,
                                                         const int32_t* __restrict__ dst,
-                                                        const int32_t* __restrict__ start, int nblk) {
+                                                        const int32_t* __restrict__ start) {
     constexpr int kLanes = D / 32;
-    constexpr int kStep = kThreads / kLanes;
-    const int blk = blockIdx.x % nblk, seg = blockIdx.x / nblk;
-    const int j = seg % p.Hkv, lb = seg / p.Hkv;
-    const int l = lb / B, b = lb - l * B;
-    const int n = min(count[seg], cap);
-    const int from = slot_of(src, b, p.S), to = slot_of(dst, b, p.S), first = start[b];
-    if (blk * kRows >= n || from < 0 || to < 0 || first < 0) return;
-    const int have = length_of(p, from), rows_held = held_of(p, to) << p.shift;
-    const int part = threadIdx.x % kLanes;
-    const int page = 1 << p.shift;
-    for (int m = blk * kRows + (int)threadIdx.x / kLanes; m < min(n, (blk + 1) * kRows); m += kStep) {
-        const int t = idx[(size_t)seg * cap + m];
-        if (t < 0 || t >= have || m >= rows_held - first) continue;
-        const int pos = first + m;
-        const int pa = p.table[(size_t)from * p.M + (t >> p.shift)];
-        const int pb = p.table[(size_t)to * p.M + (pos >> p.shift)];
-        if (pa < 0 || pa >= p.n_pages || pb < 0 || pb >= p.n_pages) continue;
-        const char* a = page_block<D>(p, l, pa, j);
-        char* o = page_block<D>(p, l, pb, j);
-        const int ta = t & (page - 1), to_ = pos & (page - 1);
-        const size_t ca = (size_t)ta * (D / 2) + part * 16, co = (size_t)to_ * (D / 2) + part * 16;
-        const size_t sa = (size_t)page * D + (size_t)part * page + ta, so = (size_t)page * D + (size_t)part * page + to_;
-        const u32x4 wk = ld16(a + ca), wv = ld16(a + (size_t)page * (D / 2) + ca);
-        const char sk = a[sa], sv = a[sa + (size_t)page * (D / 32)];
-        st16(o + co, wk);
-        st16(o + (size_t)page * (D / 2) + co, wv);
-        o[so] = sk;
-        o[so + (size_t)page * (D / 32)] = sv;
-    }
+    const int in = threadIdx.x / kLanes, part = threadIdx.x % kLanes * 4;
+    if (in >= kRows) return;  // rows of 64 channels: two lanes each
+    const RowAt r = row_at<Flat>(g, in);
+    if (!row_there<Flat>(g, in) || r.m >= min(count[r.seg], g.cap)) return;
+    const int from = slot_of(src, r.b, p.S), to = slot_of(dst, r.b, p.S);
+    if (from < 0 || to < 0) return;
+    const int t = idx[r.seg * g.cap + r.m];
+    int ta = 0, tb = 0;
+    const char* a = t < 0 ? nullptr : find_row<D>(p, from, 0, t, length_of(p, from), r, ta);
+    char* o = find_row<D>(p, to, start[r.b], r.m, held_of(p, to) << p.shift, r, tb);
+    if (a == nullptr || o == nullptr) return;
+    const PageAt<D> at_a(ta, part, p.shift), at_o(tb, part, p.shift);
+    const size_t values = at_a.values(p.shift), value_scales = at_a.value_scales(p.shift);
+    const u32x4 wk = ld16(a + at_a.codes), wv = ld16(a + at_a.codes + values);
+    const char sk = a[at_a.scales], sv = a[at_a.scales + value_scales];
+    st16(o + at_o.codes, wk);
+    st16(o + at_o.codes + values, wv);
+    o[at_o.scales] = sk;
+    o[at_o.scales + value_scales] = sv;
 }
 
-// ---------------------------------------------------------------------------
-// rows of the cache as the values they stand for: kve_pages_read
-// ---------------------------------------------------------------------------
-
-// One workgroup per (segment, kRows rows), D / 8 lanes to a row.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void read_rows(PagePool p, int B, int cap, const int32_t* __restrict__ seq,
+// D / 8 lanes to a row, as in pack_rows.
+template <typename T, int D, bool Flat>
+__global__ __launch_bounds__(kThreads) void read_rows(PagePool p, RowGrid g, const int32_t* __restrict__ seq,
                                                       const int32_t* __restrict__ start,
                                                       const int32_t* __restrict__ count, char* __restrict__ k_out,
-                                                      char* __restrict__ v_out, int nblk) {
+                                                      char* __restrict__ v_out) {
     constexpr int kLanes = D / 8;
     constexpr int kStep = kThreads / kLanes;
-    const int blk = blockIdx.x % nblk, seg = blockIdx.x / nblk;
-    const int j = seg % p.Hkv, lb = seg / p.Hkv;
-    const int l = lb / B, b = lb - l * B;
-    const int n = count != nullptr ? min(count[b], cap) : cap;
-    const int slot = slot_of(seq, b, p.S), first = start != nullptr ? start[b] : 0;
-    if (blk * kRows >= n || slot < 0 || first < 0) return;
-    const int have = length_of(p, slot);
+    constexpr int kItems = kRows / kStep;
     const int part = threadIdx.x % kLanes;
-    const int page = 1 << p.shift;
-    for (int m = blk * kRows + (int)threadIdx.x / kLanes; m < min(n, (blk + 1) * kRows); m += kStep) {
-        if (m >= have - first) break;
-        const int pos = first + m;
-        const int pg = p.table[(size_t)slot * p.M + (pos >> p.shift)];
-        if (pg < 0 || pg >= p.n_pages) continue;
-        const char* block = page_block<D>(p, l, pg, j);
-        const int tok = pos & (page - 1);
-        const char* row = block + (size_t)tok * (D / 2) + part * 4;
-        const char* scales = block + (size_t)page * D + (size_t)(part / 4) * page + tok;
-        const size_t o = ((size_t)seg * cap + m) * (D * sizeof(T));
-        if (k_out != nullptr)
-            Eight<T>::store(k_out + o, part, *reinterpret_cast<const uint32_t*>(row),
-                            scale_float((uint8_t)scales[0]));
-        if (v_out != nullptr)
-            Eight<T>::store(v_out + o, part, *reinterpret_cast<const uint32_t*>(row + (size_t)page * (D / 2)),
-                            scale_float((uint8_t)scales[(size_t)page * (D / 32)]));
+    size_t out[kItems];
+    bool there[kItems];
+    uint32_t wk[kItems], wv[kItems], sk[kItems], sv[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const int in = i * kStep + threadIdx.x / kLanes;
+        const RowAt r = row_at<Flat>(g, in);
+        const int n = count != nullptr ? min(count[r.b], g.cap) : g.cap;
+        const int slot = slot_of(seq, r.b, p.S);
+        out[i] = (r.seg * g.cap + r.m) * (D * sizeof(T));
+        there[i] = row_there<Flat>(g, in) && r.m < n && slot >= 0;
+        if (there[i]) {
+            int tok = 0;
+            const char* block = find_row<D>(p, slot, start != nullptr ? start[r.b] : 0, r.m, length_of(p, slot), r,
+                                            tok);
+            there[i] = block != nullptr;
+            if (there[i]) {
+                const PageAt<D> at(tok, part, p.shift);
+                wk[i] = *reinterpret_cast<const uint32_t*>(block + at.codes);
+                wv[i] = *reinterpret_cast<const uint32_t*>(block + at.codes + at.values(p.shift));
+                sk[i] = (uint8_t)block[at.scales];
+                sv[i] = (uint8_t)block[at.scales + at.value_scales(p.shift)];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        if (!there[i]) continue;
+        if (k_out != nullptr) Eight<T>::store(k_out + out[i], part, wk[i], scale_float(sk[i]));
+        if (v_out != nullptr) Eight<T>::store(v_out + out[i], part, wv[i], scale_float(sv[i]));
     }
 }
 
@@ -251,63 +312,87 @@ __global__ __launch_bounds__(kThreads) void read_rows(PagePool p, int B, int cap
 // bookkeeping
 // ---------------------------------------------------------------------------
 
+// These kernels are chains of a few memory latencies, and their code comes from
+// memory too when other kernels have run since: it is kept short (loops are not
+// unrolled; scans are lane moves).
 constexpr int kPlanThreads = kPagesMaxEntries;
 constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kLoads = 16;                                // pages per thread and round of find_free
+constexpr int kTallies = kLoads * kPlanWaves;             // counts of one round, in page order
+constexpr int kTalliesPerLane = kTallies / kWave;
+constexpr uint32_t kMostPages = 0x7fffffffu;              // where sums of needs stay
 
-// Exclusive prefix sum over the workgroup; total in `total`.  s: kPlanWaves words of LDS.
-__device__ __forceinline__ unsigned long long scan_exclusive(unsigned long long x, unsigned long long* s,
-                                                             unsigned long long& total) {
+// Sum of needs that stays at kMostPages.
+__device__ __forceinline__ uint32_t add_needs(uint32_t a, uint32_t b) { return min(a + b, kMostPages); }
+
+// Inclusive sum of needs over the lanes of a wave.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+#define KVE_SCAN_STEP(ctrl, rows) \
+    x = add_needs(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false))
+    KVE_SCAN_STEP(0x111, 0xf);  // the lane before
+    KVE_SCAN_STEP(0x112, 0xf);  // two before
+    KVE_SCAN_STEP(0x114, 0xf);
+    KVE_SCAN_STEP(0x118, 0xf);
+    KVE_SCAN_STEP(0x142, 0xa);  // lane 15 of a row to the next row
+    KVE_SCAN_STEP(0x143, 0xc);  // lane 31 to the upper half
+#undef KVE_SCAN_STEP
+    return x;
+}
+
+// Sum of needs over the threads before, and over all in `total`.  s: kPlanWaves words of LDS.
+__device__ __forceinline__ uint32_t scan_exclusive(uint32_t x, uint32_t* s, uint32_t& total) {
     const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
-    unsigned long long inc = x;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const unsigned long long y = __shfl_up(inc, o);
-        if (lane >= o) inc += y;
-    }
-    __syncthreads();  // the last scan's sums are read
+    const uint32_t inc = wave_scan(x);
     if (lane == kWave - 1) s[w] = inc;
     __syncthreads();
-    unsigned long long before = 0;
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < kPlanWaves; ++i) {
-        const unsigned long long y = s[i];
-        if (i < w) before += y;
-        total += y;
-    }
-    return before + inc - x;
+    const uint32_t sums = wave_scan(lane < kPlanWaves ? s[lane] : 0u);
+    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, kPlanWaves - 1);
+    const uint32_t before = w > 0 ? (uint32_t)__shfl((int)sums, w - 1) : 0u;
+    return add_needs(before, (uint32_t)__shfl_up((int)inc, 1) * (lane > 0));
 }
 
 // The first `want` free pages in ascending order into list; returns how many
-// there are (all free pages counted, where fewer than `want`).  Sixteen pages per
-// thread and round, as four loads of four: the counts of the four loads, at most
-// 4096 each, are scanned together as 16-bit fields.
-__device__ int find_free(const int32_t* __restrict__ refs, int n_pages, int want, int32_t* __restrict__ list,
-                         unsigned long long* s) {
-    constexpr int kPer = 4, kLoads = 4;
+// there are (all free pages, where fewer than `want`).  Every wave takes 64
+// neighbouring pages per load: a ballot ranks them, and the tallies of a round
+// are summed by every wave for itself.
+__device__ __noinline__ int find_free(const int32_t* refs, int n_pages, int want, int32_t* list) {
+    __shared__ uint32_t s_tally[kTallies];
+    const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
     int found = 0;
-    for (int base = 0; base < n_pages && found < want; base += kPlanThreads * kPer * kLoads) {
-        uint32_t free[kLoads];
-        unsigned long long counts = 0;
+    for (int base = 0; base < n_pages && found < want; base += kPlanThreads * kLoads) {
+        uint32_t free = 0;
+        const int at = base + (int)threadIdx.x;
+        const int loads = min(kLoads, (n_pages - base + kPlanThreads - 1) / kPlanThreads);
+        int32_t ref[kLoads];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            free[i] = 0;
-            const int at = base + (i * kPlanThreads + (int)threadIdx.x) * kPer;
+        for (int i = 0; i < kLoads; ++i) ref[i] = refs[min(at + i * kPlanThreads, n_pages - 1)];
 #pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (at + e < n_pages && refs[at + e] == 0) free[i] |= 1u << e;
-            counts |= (unsigned long long)__popc(free[i]) << (16 * i);
+        for (int i = 0; i < kLoads; ++i) free |= (uint32_t)(ref[i] == 0 && at + i * kPlanThreads < n_pages) << i;
+        __syncthreads();  // the last round's tallies are read
+#pragma unroll 1
+        for (int i = 0; i < loads; ++i) {
+            const uint64_t mask = __builtin_amdgcn_ballot_w64((free >> i) & 1u);
+            if (lane == 0) s_tally[i * kPlanWaves + w] = (uint32_t)__popcll(mask);
         }
-        unsigned long long total;
-        const unsigned long long before = scan_exclusive(counts, s, total);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            int r = found + (int)((before >> (16 * i)) & 0xffff);
-            const int at = base + (i * kPlanThreads + (int)threadIdx.x) * kPer;
-            for (uint32_t f = free[i]; f != 0; f &= f - 1, ++r)
-                if (r < want) list[r] = at + __ffs(f) - 1;
-            found += (int)((total >> (16 * i)) & 0xffff);
+        __syncthreads();
+        // lane: the tallies kTalliesPerLane lane .. of this round, those before them in `before`
+        uint32_t own = 0;
+#pragma unroll 1
+        for (int e = 0; e < kTalliesPerLane; ++e) {
+            const int t = lane * kTalliesPerLane + e;
+            own += t < loads * kPlanWaves ? s_tally[t] : 0u;
         }
+        const uint32_t inc = wave_scan(own), before = inc - own;
+#pragma unroll 1
+        for (int i = 0; i < loads; ++i) {
+            const int t = i * kPlanWaves + w, first = t / kTalliesPerLane * kTalliesPerLane;
+            uint32_t r = (uint32_t)__builtin_amdgcn_readlane((int)before, __builtin_amdgcn_readfirstlane(t / kTalliesPerLane));
+            for (int e = first; e < t; ++e) r += s_tally[e];
+            const uint64_t mask = __builtin_amdgcn_ballot_w64((free >> i) & 1u);
+            r += (uint32_t)found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+            if (((free >> i) & 1u) != 0 && r < (uint32_t)want) list[r] = at + i * kPlanThreads;
+        }
+        found += __builtin_amdgcn_readlane((int)inc, kWave - 1);
     }
     __syncthreads();  // list is whole
     return found;
@@ -316,7 +401,12 @@ __device__ int find_free(const int32_t* __restrict__ refs, int n_pages, int want
 // Whether an earlier entry names the same slot.  s_seq holds the entries' slots.
 __device__ __forceinline__ bool named_before(const int* s_seq, int i, int slot) {
     bool hit = false;
-    for (int e = 0; e < i; ++e) hit |= s_seq[e] == slot;
+#pragma unroll 1
+    for (int e = 0; e < i; e += 4) {
+        const int4 four = *reinterpret_cast<const int4*>(s_seq + e);
+        hit |= four.x == slot | ((four.y == slot) & (e + 1 < i)) | ((four.z == slot) & (e + 2 < i)) |
+               ((four.w == slot) & (e + 3 < i));
+    }
     return hit;
 }
 
@@ -342,29 +432,29 @@ __global__ __launch_bounds__(kPlanThreads) void extend_kernel(PagePool p, const 
                                                               int32_t* __restrict__ start,
                                                               int32_t* __restrict__ missing,
                                                               int32_t* __restrict__ list) {
-    __shared__ int s_seq[kPlanThreads], s_off[kPlanThreads], s_held[kPlanThreads], s_ok[kPlanThreads];
-    __shared__ unsigned long long s_scan[kPlanWaves];
+    __shared__ __attribute__((aligned(16))) int s_seq[kPlanThreads];
+    __shared__ int s_off[kPlanThreads], s_held[kPlanThreads], s_ok[kPlanThreads];
+    __shared__ uint32_t s_scan[kPlanWaves];
     const int i = threadIdx.x;
     const int slot = i < n ? slot_of(seq, i, p.S) : -1;
     s_seq[i] = slot;
     __syncthreads();
-    bool valid = slot >= 0 && !named_before(s_seq, i, slot);
-    int held = 0, len = 0, more = 0;
-    long long need = 0;
-    if (valid) {
+    int held = 0, len = 0, more = -1;
+    if (slot >= 0) {
         held = held_of(p, slot);
         len = length_of(p, slot);
         more = add[i];
-        const long long now = (long long)len + more;
-        valid = more >= 0 && now <= (long long)p.M << p.shift;
-        if (valid) need = max(0LL, ((now + (1 << p.shift) - 1) >> p.shift) - held);
     }
-    unsigned long long total;
-    const unsigned long long off = scan_exclusive((unsigned long long)need, s_scan, total);
-    const int want = (int)min(total, (unsigned long long)p.n_pages);
-    const int found = find_free(p.refs, p.n_pages, want, list, s_scan);
-    const bool given = valid && (need == 0 || off + need <= (unsigned long long)found);
-    s_off[i] = (int)min(off, (unsigned long long)p.n_pages);
+    bool valid = slot >= 0 && !named_before(s_seq, i, slot);
+    const long long now = (long long)len + more;
+    valid = valid && more >= 0 && now <= (long long)p.M << p.shift;
+    const uint32_t need = valid ? (uint32_t)max(0, (int)((now + (1 << p.shift) - 1) >> p.shift) - held) : 0u;
+    uint32_t total;
+    const uint32_t off = scan_exclusive(need, s_scan, total);
+    const int want = min((int)total, p.n_pages);
+    const int found = find_free(p.refs, p.n_pages, want, list);
+    const bool given = valid && (need == 0 || off + need <= (uint32_t)found);
+    s_off[i] = min((int)off, p.n_pages);
     s_held[i] = held;
     s_ok[i] = given;
     __syncthreads();
@@ -382,7 +472,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_kernel(PagePool p, const 
             p.length[slot] = len + more;
         }
     }
-    if (i == 0) *missing = (int)min(total - (unsigned long long)min(want, found), 2147483647ULL);
+    if (i == 0) *missing = (int)total - min(want, found);
 }
 
 // What fork_copy does for an entry: full pages shared (-1: refused), the partial
@@ -397,21 +487,23 @@ __global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagePool p, const in
                                                             int32_t* __restrict__ missing,
                                                             ForkPlan* __restrict__ plan,
                                                             int32_t* __restrict__ list) {
-    __shared__ int s_dst[kPlanThreads];
-    __shared__ unsigned long long s_scan[kPlanWaves];
+    __shared__ __attribute__((aligned(16))) int s_dst[kPlanThreads];
+    __shared__ uint32_t s_scan[kPlanWaves];
     const int i = threadIdx.x;
     const int from = i < n ? slot_of(src, i, p.S) : -1, to = i < n ? slot_of(dst, i, p.S) : -1;
     s_dst[i] = to;
     __syncthreads();
-    const bool valid = from >= 0 && to >= 0 && !named_before(s_dst, i, to) && p.held[to] == 0 && p.length[to] == 0;
-    const int len = valid ? length_of(p, from) : 0;
+    const bool free = from >= 0 && to >= 0 && p.held[to] == 0 && p.length[to] == 0;
+    int len = free ? length_of(p, from) : 0;
+    const bool valid = free && !named_before(s_dst, i, to);
+    if (!valid) len = 0;
     const int full = len >> p.shift, rows = len & ((1 << p.shift) - 1);
-    const int need = rows != 0 ? 1 : 0;
-    unsigned long long total;
-    const unsigned long long off = scan_exclusive((unsigned long long)need, s_scan, total);
-    // all sources are read (the scan's barriers); destinations may be written
-    const int found = find_free(p.refs, p.n_pages, (int)total, list, s_scan);
-    const bool given = valid && (need == 0 || off < (unsigned long long)found);
+    const uint32_t need = rows != 0 ? 1u : 0u;
+    uint32_t total;
+    const uint32_t off = scan_exclusive(need, s_scan, total);
+    // all sources are read (the scan's barrier); destinations may be written
+    const int found = find_free(p.refs, p.n_pages, (int)total, list);
+    const bool given = valid && (need == 0 || off < (uint32_t)found);
     if (i < n) {
         ForkPlan f{given ? full : -1, -1, -1, rows};
         if (given) {
@@ -481,20 +573,50 @@ __global__ __launch_bounds__(kThreads) void free_kernel(PagePool p, const int32_
     }
 }
 
-template <typename T, int D>
-void run_pack(const RowView& k, const RowView& v, int B, int N, const int32_t* idx, const int32_t* count, int cap,
-              const int32_t* start, const int32_t* seq, const PagePool& p, hipStream_t st) {
-    const int nblk = (cap + kRows - 1) / kRows;
-    hipLaunchKernelGGL((pack_rows<T, D>), dim3((unsigned)p.L * B * p.Hkv * nblk), dim3(kThreads), 0, st, k, v, B, N,
-                       idx, count, cap, start, seq, p, nblk);
+RowGrid row_grid(const PagePool& p, int B, int cap) {
+    return RowGrid{B, p.Hkv, cap, (cap + kRows - 1) / kRows, (uint32_t)p.L * B * p.Hkv * (uint32_t)cap};
+}
+
+bool is_flat(const RowGrid& g) { return g.cap <= kFlatRows; }
+
+dim3 row_blocks(const PagePool& p, const RowGrid& g) {
+    return dim3(is_flat(g) ? (g.rows + kRows - 1) / kRows : (unsigned)p.L * g.B * g.Hkv * g.nblk);
 }
 
 template <typename T, int D>
-void run_read(const PagePool& p, int B, int T_, const int32_t* seq, const int32_t* start, const int32_t* count,
+void run_pack(const RowView& k, const RowView& v, int B, int N, const int32_t* idx, const int32_t* count, int cap,
+              const int32_t* start, const int32_t* seq, const PagePool& p, hipStream_t st) {
+    const RowGrid g = row_grid(p, B, cap);
+    if (is_flat(g))
+        hipLaunchKernelGGL((pack_rows<T, D, true>), row_blocks(p, g), dim3(kThreads), 0, st, k, v, g, N, idx, count,
+                           start, seq, p);
+    else
+        hipLaunchKernelGGL((pack_rows<T, D, false>), row_blocks(p, g), dim3(kThreads), 0, st, k, v, g, N, idx, count,
+                           start, seq, p);
+}
+
+template <int D>
+void run_select(const PagePool& p, int B, const int32_t* src, const int32_t* idx, const int32_t* count, int cap,
+                const int32_t* dst, const int32_t* start, hipStream_t st) {
+    const RowGrid g = row_grid(p, B, cap);
+    if (is_flat(g))
+        hipLaunchKernelGGL((select_rows<D, true>), row_blocks(p, g), dim3(kThreads), 0, st, p, g, src, idx, count, dst,
+                           start);
+    else
+        hipLaunchKernelGGL((select_rows<D, false>), row_blocks(p, g), dim3(kThreads), 0, st, p, g, src, idx, count,
+                           dst, start);
+}
+
+template <typename T, int D>
+void run_read(const PagePool& p, int B, int cap, const int32_t* seq, const int32_t* start, const int32_t* count,
               void* k_out, void* v_out, hipStream_t st) {
-    const int nblk = (T_ + kRows - 1) / kRows;
-    hipLaunchKernelGGL((read_rows<T, D>), dim3((unsigned)p.L * B * p.Hkv * nblk), dim3(kThreads), 0, st, p, B, T_,
-                       seq, start, count, static_cast<char*>(k_out), static_cast<char*>(v_out), nblk);
+    const RowGrid g = row_grid(p, B, cap);
+    if (is_flat(g))
+        hipLaunchKernelGGL((read_rows<T, D, true>), row_blocks(p, g), dim3(kThreads), 0, st, p, g, seq, start, count,
+                           static_cast<char*>(k_out), static_cast<char*>(v_out));
+    else
+        hipLaunchKernelGGL((read_rows<T, D, false>), row_blocks(p, g), dim3(kThreads), 0, st, p, g, seq, start, count,
+                           static_cast<char*>(k_out), static_cast<char*>(v_out));
 }
 
 }  // namespace
@@ -541,14 +663,10 @@ hipError_t launch_pages_select(const PagePool& p, int d, int B, const int32_t* s
                                const int32_t* count, int cap, const int32_t* dst, const int32_t* start,
                                hipStream_t st) {
     if (cap == 0) return hipSuccess;
-    const int nblk = (cap + kRows - 1) / kRows;
-    const dim3 grid((unsigned)p.L * B * p.Hkv * nblk);
     if (d == 128)
-        hipLaunchKernelGGL(select_rows<128>, grid, dim3(kThreads), 0, st, p, B, src, idx, count, cap, dst, start,
-                           nblk);
+        run_select<128>(p, B, src, idx, count, cap, dst, start, st);
     else
-        hipLaunchKernelGGL(select_rows<64>, grid, dim3(kThreads), 0, st, p, B, src, idx, count, cap, dst, start,
-                           nblk);
+        run_select<64>(p, B, src, idx, count, cap, dst, start, st);
     return hipGetLastError();
 }
 

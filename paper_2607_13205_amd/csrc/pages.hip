@@ -139,20 +139,22 @@ struct RowAt {
 template <bool Flat>
 __device__ __forceinline__ RowAt row_at(const RowGrid& g, int in) {
     RowAt r;
-    uint32_t seg;
+    uint32_t lb;
     if constexpr (Flat) {
         const uint32_t at = min(blockIdx.x * (uint32_t)kRows + in, g.rows - 1);
-        seg = at / (uint32_t)g.cap;
+        const uint32_t seg = at / (uint32_t)g.cap;
         r.m = (int)(at - seg * g.cap);
+        lb = seg / (uint32_t)g.Hkv;
+        r.j = (int)(seg - lb * g.Hkv);
     } else {
-        seg = blockIdx.x / (uint32_t)g.nblk;
-        r.m = (int)(blockIdx.x - seg * g.nblk) * kRows + in;
+        const uint32_t x = blockIdx.x / (uint32_t)g.Hkv;
+        r.j = (int)(blockIdx.x - x * g.Hkv);
+        lb = x / (uint32_t)g.nblk;
+        r.m = (int)(x - lb * g.nblk) * kRows + in;
     }
-    const uint32_t lb = seg / (uint32_t)g.Hkv;
-    r.seg = seg;
-    r.j = (int)(seg - lb * g.Hkv);
     r.l = (int)(lb / (uint32_t)g.B);
     r.b = (int)(lb - (uint32_t)r.l * g.B);
+    r.seg = (size_t)lb * g.Hkv + r.j;
     return r;
 }
 

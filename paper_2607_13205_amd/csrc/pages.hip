@@ -24,14 +24,22 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 // eight channels of a row as a dword of codes, and back
 // ---------------------------------------------------------------------------
 
+// Once: non-temporal, for rows of a large tensor that are read once.
+template <bool Once>
+__device__ __forceinline__ u32x4 load16(const char* at) {
+    if constexpr (Once) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
+    return ld16(at);
+}
+
 template <typename T>
 struct Eight;
 
 template <>
 struct Eight<__bf16> {
     u32x4 v;
+    template <bool Once>
     __device__ __forceinline__ void load(const char* row, int part) {
-        v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row) + part);
+        v = load16<Once>(row + part * 16);
     }
     // bits of the largest magnitude, as a float32
     __device__ __forceinline__ uint32_t top() const {
@@ -63,9 +71,10 @@ struct Eight<__bf16> {
 template <>
 struct Eight<float> {
     u32x4 v[2];
+    template <bool Once>
     __device__ __forceinline__ void load(const char* row, int part) {
-        v[0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row) + 2 * part);
-        v[1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row) + 2 * part + 1);
+        v[0] = load16<Once>(row + part * 32);
+        v[1] = load16<Once>(row + part * 32 + 16);
     }
     __device__ __forceinline__ uint32_t top() const {
         uint32_t m = 0;
@@ -189,8 +198,12 @@ struct PageAt {
 };
 
 // D / 8 lanes to a row.  All of a thread's rows are looked up, then loaded, then
-// packed, so that a workgroup waits for memory once per stage.
-template <typename T, int D, bool Flat>
+// packed, so that a workgroup waits for memory once per stage.  Gather: rows idx of
+// a prompt's keys and values, which are read once (32 layers, 1639 of 32768 rows:
+// 207 us with non-temporal loads, 218 without, 5.3 TB/s); else all rows of what a
+// projection has just left in the caches (1003 rows of four sequences, 8 layers:
+// 31 and 24 us).
+template <typename T, int D, bool Flat, bool Gather>
 __global__ __launch_bounds__(kThreads) void pack_rows(RowView kv, RowView vv, RowGrid g, int N,
                                                       const int32_t* __restrict__ idx,
                                                       const int32_t* __restrict__ count,
@@ -207,17 +220,17 @@ __global__ __launch_bounds__(kThreads) void pack_rows(RowView kv, RowView vv, Ro
     for (int i = 0; i < kItems; ++i) {
         const int in = i * kStep + threadIdx.x / kLanes;
         const RowAt r = row_at<Flat>(g, in);
-        const int n = idx != nullptr ? min(count[r.seg], g.cap) : count != nullptr ? min(count[r.b], g.cap) : g.cap;
+        const int n = Gather ? min(count[r.seg], g.cap) : count != nullptr ? min(count[r.b], g.cap) : g.cap;
         block[i] = nullptr;
         if (row_there<Flat>(g, in) && r.m < n) {
-            const int t = idx != nullptr ? idx[r.seg * g.cap + r.m] : r.m;
+            const int t = Gather ? idx[r.seg * g.cap + r.m] : r.m;
             const int slot = slot_of(seq, r.b, p.S);
             if (t >= 0 && t < N && slot >= 0)
                 block[i] = find_row<D>(p, slot, start[r.b], r.m, held_of(p, slot) << p.shift, r, tok[i]);
             if (block[i] != nullptr) {
-                x[i].load(kv.base + (size_t)r.l * kv.s_layer + (size_t)r.b * kv.s_batch + (size_t)r.j * kv.s_head +
+                x[i].template load<Gather>(kv.base + (size_t)r.l * kv.s_layer + (size_t)r.b * kv.s_batch + (size_t)r.j * kv.s_head +
                               (size_t)t * kv.s_token, part);
-                y[i].load(vv.base + (size_t)r.l * vv.s_layer + (size_t)r.b * vv.s_batch + (size_t)r.j * vv.s_head +
+                y[i].template load<Gather>(vv.base + (size_t)r.l * vv.s_layer + (size_t)r.b * vv.s_batch + (size_t)r.j * vv.s_head +
                               (size_t)t * vv.s_token, part);
             }
         }
@@ -585,16 +598,25 @@ dim3 row_blocks(const PagePool& p, const RowGrid& g) {
     return dim3(is_flat(g) ? (g.rows + kRows - 1) / kRows : (unsigned)p.L * g.B * g.Hkv * g.nblk);
 }
 
+template <typename T, int D, bool Flat, bool Gather>
+void launch_pack(const RowView& k, const RowView& v, const RowGrid& g, int N, const int32_t* idx,
+                 const int32_t* count, const int32_t* start, const int32_t* seq, const PagePool& p, hipStream_t st) {
+    hipLaunchKernelGGL((pack_rows<T, D, Flat, Gather>), row_blocks(p, g), dim3(kThreads), 0, st, k, v, g, N, idx,
+                       count, start, seq, p);
+}
+
 template <typename T, int D>
 void run_pack(const RowView& k, const RowView& v, int B, int N, const int32_t* idx, const int32_t* count, int cap,
               const int32_t* start, const int32_t* seq, const PagePool& p, hipStream_t st) {
     const RowGrid g = row_grid(p, B, cap);
-    if (is_flat(g))
-        hipLaunchKernelGGL((pack_rows<T, D, true>), row_blocks(p, g), dim3(kThreads), 0, st, k, v, g, N, idx, count,
-                           start, seq, p);
+    if (is_flat(g) && idx != nullptr)
+        launch_pack<T, D, true, true>(k, v, g, N, idx, count, start, seq, p, st);
+    else if (is_flat(g))
+        launch_pack<T, D, true, false>(k, v, g, N, idx, count, start, seq, p, st);
+    else if (idx != nullptr)
+        launch_pack<T, D, false, true>(k, v, g, N, idx, count, start, seq, p, st);
     else
-        hipLaunchKernelGGL((pack_rows<T, D, false>), row_blocks(p, g), dim3(kThreads), 0, st, k, v, g, N, idx, count,
-                           start, seq, p);
+        launch_pack<T, D, false, false>(k, v, g, N, idx, count, start, seq, p, st);
 }
 
 template <int D>

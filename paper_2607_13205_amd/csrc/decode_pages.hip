@@ -8,13 +8,16 @@
 //
 // Both products are taken transposed, so that the weights never leave their
 // registers.  A wave takes 32 tokens per step.  S^T = K Q^T, 16 tokens by 16 query
-// heads per 16x16x32 product: row m of tile T is token 8 (m / 4) + 4 T + m % 4,
-// and lane l (head l % 16, quarter l / 16) receives rows 4 (l / 16) .. + 4, that
-// is the eight tokens 8 (l / 16) .. + 8 from its two tiles, in order.  Those are
-// what the second product O^T = V^T P^T wants from that lane.  The value rows'
-// dwords hold eight channels of one token and the product eight tokens of one
-// channel: the scaled conversion gives two channels of a token, and a byte
-// permutation pairs the tokens.
+// heads per 16x16x32 product: row m of tile T is token 16 T + 4 (m % 4) + m / 4,
+// and lane l (head l % 16, quarter q = l / 16) receives rows 4 q .. + 4, that is
+// tokens 4 i + q, i < 8, from its two tiles.  Those are what the second product
+// O^T = V^T P^T wants from that lane.  The value rows' dwords hold eight channels
+// of one token and the product eight tokens of one channel: the scaled conversion
+// gives two channels of a token, and a byte permutation pairs the tokens.
+//
+// The bytes of a step go straight to LDS, into the wave's own ring of slots, two
+// steps ahead and without a register held for them; four workgroups share a
+// compute unit.
 //
 // With up to four heads per KV head the sixteen columns hold every head three
 // times, and each copy's lanes make another of the three parts of the weights: a
@@ -32,6 +35,7 @@
 #include "kve_device.h"
 #include "kve_internal.h"
 #include "kve_pages_device.h"
+#include "kve_stream.h"
 
 namespace kve {
 namespace {
@@ -40,6 +44,13 @@ constexpr int kThreads = kMergeThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBlk = 32;    // tokens per wave step
 constexpr int kSplitTries = 4;
+constexpr int kMostQuanta = (1 << 30) / kDecodeQuantum;  // of a sequence
+
+// One direct-to-LDS load of four bytes per lane, as lds_dma16.
+__device__ __forceinline__ void lds_dma4(const char* base, unsigned voff, const char* lds_dst) {
+    const unsigned m0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds_dst);
+    asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(base), "{m0}"(m0) : "memory");
+}
 
 // Waves per SIMD that the registers are kept to, and so workgroups per compute unit.
 template <typename T, int D, int NH>
@@ -107,41 +118,32 @@ __device__ __forceinline__ void unpack_tokens(const uint32_t (&w)[8], const floa
     odd = __builtin_bit_cast(bf16x8, o);
 }
 
-// Tokens that sample b has for a decode.
-__device__ __forceinline__ int tokens_of(const PagePool& p, const int32_t* seq, int b, int max_tokens) {
-    const int slot = slot_of(seq, b, p.S);
-    return slot < 0 ? 0 : min(length_of(p, slot), max_tokens);
-}
-
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor(x, o);
+// Inclusive sum over the lanes of a wave, with lane moves (an LDS exchange per
+// step is several times their latency).
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // the lane before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // two before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
     return x;
 }
 
-__device__ __forceinline__ int quanta_of(const PagePool& p, const int32_t* seq, int b, int B, int max_tokens) {
-    return b < B ? (tokens_of(p, seq, b, max_tokens) + kDecodeQuantum - 1) / kDecodeQuantum : 0;
-}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), kWave - 1); }
 
-// How the sequences are cut (PagesPlan): quanta per split, such that the splits
-// are at most `share`, or at most share + B where a few tries find no such size.
-// Every wave works it out for itself, 64 sequences at a time.
-__device__ __forceinline__ int split_quanta(const PagePool& p, const int32_t* seq, int B, int max_tokens, int share) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int q0 = quanta_of(p, seq, lane, B, max_tokens);  // the first 64: loaded once
-    long long total = __builtin_amdgcn_readfirstlane(wave_sum(q0));
-    for (int b0 = kWave; b0 < B; b0 += kWave)
-        total += __builtin_amdgcn_readfirstlane(wave_sum(quanta_of(p, seq, b0 + lane, B, max_tokens)));
-    int per = (int)max(1LL, (total + share - 1) / share);
-    for (int tries = 0; tries < kSplitTries; ++tries) {
-        int splits = __builtin_amdgcn_readfirstlane(wave_sum((q0 + per - 1) / per));
-        for (int b0 = kWave; b0 < B; b0 += kWave)
-            splits += __builtin_amdgcn_readfirstlane(
-                wave_sum((quanta_of(p, seq, b0 + lane, B, max_tokens) + per - 1) / per));
-        if (splits <= share) break;
-        per = max(per + 1, (int)((long long)per * splits / share));
+// A sequence as a lane holds it: its slot (-1: none) and its tokens.
+struct Sequence {
+    int slot, tokens;
+    __device__ __forceinline__ Sequence(const PagePool& p, const int32_t* seq, int b, int B, int max_tokens) {
+        slot = b < B ? slot_of(seq, b, p.S) : -1;
+        tokens = slot < 0 ? 0 : min(length_of(p, slot), max_tokens);
     }
-    return per;
+    __device__ __forceinline__ int quanta() const { return (tokens + kDecodeQuantum - 1) / kDecodeQuantum; }
+};
+
+__device__ __forceinline__ int splits_of(int quanta, int per) {
+    return (int)((unsigned)(quanta + per - 1) / (unsigned)per);
 }
 
 // Splits before and of a sequence.
@@ -149,74 +151,94 @@ struct SplitRange {
     int first, count;
 };
 
-// The sequence that split x belongs to, or -1, and its range.  ranges: where not
-// null, every sequence's range is written there (by one wave).
-__device__ __forceinline__ int find_split(const PagePool& p, const int32_t* seq, int B, int max_tokens, int per,
-                                          int x, SplitRange& r, SplitRange* ranges) {
+// What a workgroup works on: tokens [k0, k1) of sample b, in slot `slot`.
+struct Work {
+    int b, slot, k0, k1;
+    SplitRange range;
+};
+
+// How the sequences are cut (PagesPlan): quanta per split, such that the splits
+// are at most `share`, or at most share + B where a few tries find no such size;
+// and split x of them (b = -1: there is none).  Every wave works it out for
+// itself, 64 sequences at a time, the first 64 loaded once.  ranges: where not
+// null, every sequence's range is written there.
+__device__ __forceinline__ Work find_work(const PagePool& p, const int32_t* seq, int B, int max_tokens, int share,
+                                          int x, SplitRange* ranges) {
     const int lane = threadIdx.x & (kWave - 1);
-    int before = 0, found = -1;
+    const Sequence mine(p, seq, lane, B, max_tokens);
+    const int q0 = mine.quanta();
+    long long total = wave_sum(q0);
+    for (int b0 = kWave; b0 < B; b0 += kWave)
+        total += wave_sum(Sequence(p, seq, b0 + lane, B, max_tokens).quanta());
+    // no sequence has more than kMostQuanta
+    int per = total < kMostQuanta ? max(1, splits_of((int)total, share))
+                                  : (int)min((total + share - 1) / share, (long long)kMostQuanta);
+    for (int tries = 0; tries < kSplitTries; ++tries) {
+        int splits = wave_sum(splits_of(q0, per));
+        for (int b0 = kWave; b0 < B; b0 += kWave)
+            splits += wave_sum(splits_of(Sequence(p, seq, b0 + lane, B, max_tokens).quanta(), per));
+        if (splits <= share) break;
+        per = (int)min(per + max(1LL, (long long)splits_of(per, share) * (splits - share)), (long long)kMostQuanta);
+    }
+    Work w{-1, -1, 0, 0, {0, 0}};
+    int before = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
-        const int n = (quanta_of(p, seq, b0 + lane, B, max_tokens) + per - 1) / per;
-        int inc = n;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int y = __shfl_up(inc, o);
-            if (lane >= o) inc += y;
-        }
+        Sequence s = mine;
+        if (b0 > 0) s = Sequence(p, seq, b0 + lane, B, max_tokens);
+        const int n = splits_of(s.quanta(), per), inc = wave_scan(n);
         const int first = before + inc - n;
         if (ranges != nullptr && b0 + lane < B) ranges[b0 + lane] = SplitRange{first, n};
         const uint64_t mask = __builtin_amdgcn_ballot_w64(x >= first && x < first + n);
         if (mask != 0) {
             const int at = __builtin_ctzll(mask);
-            r.first = __builtin_amdgcn_readlane(first, at);
-            r.count = __builtin_amdgcn_readlane(n, at);
-            found = b0 + at;
-            if (ranges == nullptr) return found;
+            w.b = b0 + at;
+            w.slot = __builtin_amdgcn_readlane(s.slot, at);
+            w.range.first = __builtin_amdgcn_readlane(first, at);
+            w.range.count = __builtin_amdgcn_readlane(n, at);
+            const int tokens = __builtin_amdgcn_readlane(s.tokens, at);
+            w.k0 = (x - w.range.first) * per * kDecodeQuantum;
+            w.k1 = (int)min((long long)tokens, w.k0 + (long long)per * kDecodeQuantum);
+            if (ranges == nullptr) return w;
         }
         before += __builtin_amdgcn_readlane(inc, kWave - 1);
     }
-    return found;
+    return w;
 }
 
-// What a wave loads for 32 tokens: a quarter row per lane and tile of the keys
-// and their scales, NC channels of eight tokens of the values and theirs.
-// block: the page of this (layer, KV head); tok: the first token in it, both the
-// same for all lanes, whose own offsets do not change.
+// Has the compiler wait for x here.  A wait for a tracked load inside the loop
+// over the steps would wait for the direct-to-LDS loads behind it too.
+template <typename X>
+__device__ __forceinline__ void settle(X& x) {
+    asm volatile("" : "+v"(x));
+}
+
+// What a wave loads for 32 tokens of a page block: key codes, value codes, and the
+// scale bytes of both, [2 D / 32][32 tokens], in a slot of LDS.  The 16-byte
+// pieces of a 64-byte key row are permuted by the row's place in groups of
+// sixteen (piece ^ row / 4 % 4), so that the sixteen rows a quarter wave reads at
+// once lie in distinct banks.
 template <int D>
-struct Step {
-    static constexpr int NK = D / 32;
-    uint32_t k[2][NK], v[8];
-    u32x2 ks, vs;
+struct Slot {
+    static constexpr int kCodes = kBlk * D / 2;  // bytes of the key, and of the value codes
+    static constexpr int kLoads = 2 * kCodes / 1024 + 1;
+    static constexpr int kBytes = 2 * kCodes + 256;
+    static constexpr int kSlots = 4096 / kCodes;  // two steps of 128 channels ahead, four of 64
+    static constexpr int kRow = D / 2;
 
-    __device__ __forceinline__ void load_keys(const char* block, int tok, int shift) {
+    // The wave's loads of tokens tok .. + 32 of a block into `slot`: kLoads of them.
+    __device__ __forceinline__ static void load(const char* block, int tok, int shift, const char* slot) {
         const int lane = threadIdx.x & (kWave - 1);
-        const int c = lane & 15, quarter = lane >> 4;
-        const char* keys = block + tok * (D / 2);
-        const char* scales = block + ((size_t)D << shift) + tok;
-        const uint32_t at = (8 * (c >> 2) + (c & 3)) * (D / 2) + quarter * (D / 8);
+        const char* keys = block + tok * kRow;
+        const char* values = keys + ((size_t)kRow << shift);
+        const uint32_t piece = D == 128 ? (lane ^ ((lane >> 4) & 3)) * 16 : lane * 16;
 #pragma unroll
-        for (int tile = 0; tile < 2; ++tile)
+        for (int i = 0; i < kCodes / 1024; ++i) lds_dma16<true>(keys + i * 1024, piece, slot + i * 1024);
 #pragma unroll
-            for (int s = 0; s < NK; ++s)
-                k[tile][s] = reinterpret_cast<const uint32_t*>(keys + at + tile * 4 * (D / 2))[s];
-        ks = *reinterpret_cast<const u32x2*>(scales + (uint32_t)(((quarter * D / 128) << shift) + 8 * (c >> 2)));
-    }
-
-    __device__ __forceinline__ void load_values(const char* block, int tok, int shift) {
-        const int lane = threadIdx.x & (kWave - 1);
-        const int c = lane & 15, quarter = lane >> 4;
-        const char* values = block + ((size_t)(D / 2) << shift) + tok * (D / 2);
-        const char* scales = block + ((size_t)D << shift) + tok;
-        const uint32_t at = 8 * quarter * (D / 2) + c * (D / 32);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (D == 128)
-                v[i] = *reinterpret_cast<const uint32_t*>(values + at + i * (D / 2));
-            else
-                v[i] = *reinterpret_cast<const uint16_t*>(values + at + i * (D / 2));
-        }
-        vs = *reinterpret_cast<const u32x2*>(scales +
-                                             (uint32_t)(((D / 32 + c * (D / 16) / 32) << shift) + 8 * quarter));
+        for (int i = 0; i < kCodes / 1024; ++i)
+            lds_dma16<true>(values + i * 1024, lane * 16, slot + kCodes + i * 1024);
+        // 2 D / 32 rows of 32 bytes, eight lanes each; lanes beyond them load the last one again
+        const uint32_t row = min(lane >> 3, 2 * D / 32 - 1);
+        lds_dma4(block + ((size_t)D << shift) + tok, (row << shift) + (lane & 7) * 4, slot + 2 * kCodes);
     }
 };
 
@@ -231,6 +253,7 @@ __device__ __forceinline__ float row_from(float x) {
 // columns each, 8 of two, or 16.
 template <typename T, int D, int NH>
 struct Sums {
+    using S = Slot<D>;
     static constexpr int NP = std::is_same<T, float>::value ? 3 : 1;  // bf16 parts of a query
     static constexpr int NK = D / 32;  // products per 16 tokens: dwords of a lane's quarter row
     static constexpr int NC = D / 16;  // channels per lane of V^T
@@ -263,35 +286,61 @@ struct Sums {
         for (int i = 0; i < NC; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    __device__ __forceinline__ void settle_queries() {
+#pragma unroll
+        for (int s = 0; s < NK; ++s)
+#pragma unroll
+            for (int a = 0; a < NP; ++a) settle(q[s][a]);
+    }
+
     // The logits of 32 tokens, before scaling.
-    __device__ __forceinline__ void logits(const Step<D>& st, f32x4 (&acc)[2]) const {
-        const int c = threadIdx.x & 15;
+    __device__ __forceinline__ void logits(const char* slot, f32x4 (&acc)[2]) const {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int c = lane & 15, quarter = lane >> 4;
+        const int tok = 4 * (c & 3) + (c >> 2);
+        const char* row = slot + tok * S::kRow + (D == 128 ? (quarter ^ (c & 3)) * 16 : quarter * 8);
+        const uint8_t* scale = reinterpret_cast<const uint8_t*>(slot + 2 * S::kCodes + quarter * D / 128 * kBlk + tok);
 #pragma unroll
         for (int tile = 0; tile < 2; ++tile) {
-            const float sc = scale_float((st.ks[tile] >> (8 * (c & 3))) & 0xffu);
+            uint32_t k[NK];
+#pragma unroll
+            for (int e = 0; e < NK; ++e) k[e] = reinterpret_cast<const uint32_t*>(row + tile * 16 * S::kRow)[e];
+            const float sc = scale_float(scale[16 * tile]);
             acc[tile] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int s = 0; s < NK; ++s) {
-                const bf16x8 kf = unpack8(st.k[tile][s], sc);
+            for (int e = 0; e < NK; ++e) {
+                const bf16x8 kf = unpack8(k[e], sc);
 #pragma unroll
-                for (int a = NP - 1; a >= 0; --a) acc[tile] = mma(kf, q[s][a], acc[tile]);
+                for (int a = NP - 1; a >= 0; --a) acc[tile] = mma(kf, q[e][a], acc[tile]);
             }
         }
     }
 
     // The tokens' share of the sums; the first `left` (at least one) count.
-    __device__ __forceinline__ void add(Step<D>& st, f32x4 (&acc)[2], int left, float sl2) {
+    __device__ __forceinline__ void add(const char* slot, f32x4 (&acc)[2], int left, float sl2) {
         const int lane = threadIdx.x & (kWave - 1);
         const int c = lane & 15, quarter = lane >> 4;
+        const char* rows = slot + S::kCodes + quarter * S::kRow + c * (D / 32);
+        const uint8_t* scales =
+            reinterpret_cast<const uint8_t*>(slot + 2 * S::kCodes + (D / 32 + c * (D / 16) / 32) * kBlk + quarter);
+        uint32_t v[8], vs[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (D == 128)
+                v[i] = *reinterpret_cast<const uint32_t*>(rows + 4 * i * S::kRow);
+            else
+                v[i] = *reinterpret_cast<const uint16_t*>(rows + 4 * i * S::kRow);
+            vs[i] = scales[4 * i];
+        }
         if (left < kBlk) {
             // rows behind the sequence hold anything: no weight, and zeros under it
             __builtin_amdgcn_sched_barrier(0);  // a branch, not selects in every step
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (8 * quarter + i >= left) {
+                if (4 * i + quarter >= left) {
                     acc[i >> 2][i & 3] = -INFINITY;
-                    st.v[i] = 0;
-                    st.vs[i >> 2] &= ~(0xffu << (8 * (i & 3)));
+                    v[i] = 0;
+                    vs[i] = 0;
                 }
         }
         float top = acc[0][0];
@@ -341,22 +390,22 @@ struct Sums {
         }
         float sc[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sc[i] = scale_float((st.vs[i >> 2] >> (8 * (i & 3))) & 0xffu);
+        for (int i = 0; i < 8; ++i) sc[i] = scale_float(vs[i]);
         const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int a = NW - 1; a >= 0; --a) den = mma(__builtin_bit_cast(bf16x8, ones), part[a], den);
-        values<0>(st, sc, part);
-        values<1>(st, sc, part);
+        values<0>(v, sc, part);
+        values<1>(v, sc, part);
         if constexpr (D == 128) {
-            values<2>(st, sc, part);
-            values<3>(st, sc, part);
+            values<2>(v, sc, part);
+            values<3>(v, sc, part);
         }
     }
 
     template <int SEL>
-    __device__ __forceinline__ void values(const Step<D>& st, const float (&sc)[8], const bf16x8 (&part)[NW]) {
+    __device__ __forceinline__ void values(const uint32_t (&v)[8], const float (&sc)[8], const bf16x8 (&part)[NW]) {
         bf16x8 even, odd;
-        unpack_tokens<SEL>(st.v, sc, even, odd);
+        unpack_tokens<SEL>(v, sc, even, odd);
 #pragma unroll
         for (int a = NW - 1; a >= 0; --a) {
             o[2 * SEL] = mma(even, part[a], o[2 * SEL]);
@@ -385,8 +434,7 @@ struct Sums {
 };
 
 // One workgroup per split of a sequence and (layer, KV head); its waves take 32
-// tokens in turn.  The next step's keys load into the registers of this step's as
-// soon as the logits are there, its values when this step's are added.
+// tokens in turn.
 template <typename T, int D, int NH>
 __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(const T* __restrict__ q, PagePool p,
                                                                   const int32_t* __restrict__ seq, int B, int G,
@@ -396,8 +444,12 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
                                                                   SplitRange* __restrict__ ranges,
                                                                   float* __restrict__ out) {
     constexpr int NC = D / 16;
+    using S = Slot<D>;
+    // the waves' rings, and behind their last use the waves' sums
+    constexpr int kRing = S::kSlots * S::kBytes, kSums = NH * D * (int)sizeof(float);
+    __shared__ __attribute__((aligned(16))) char s_ring[kWaves * (kRing > kSums ? kRing : kSums)];
     __shared__ float s_ml[kWaves][2][NH];
-    __shared__ float s_o[kWaves][NH][D];
+    float(*s_o)[NH][D] = reinterpret_cast<float(*)[NH][D]>(s_ring);
 
     const int pairs = p.L * p.Hkv;
     const int x = blockIdx.x / pairs, pair = blockIdx.x - x * pairs;
@@ -406,18 +458,17 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int c = lane & 15, quarter = lane >> 4;
 
-    int b = x, per = 1 << 23;
-    SplitRange range{x, 1};
-    if (!whole) {
-        per = split_quanta(p, seq, B, max_tokens, share);
+    Work work{x, -1, 0, 0, {x, 1}};
+    if (whole) {
+        const Sequence s(p, seq, x, B, max_tokens);
+        work.slot = s.slot;
+        work.k1 = s.tokens;
+    } else {
         // the first workgroup's first wave leaves the ranges for the merge
-        b = find_split(p, seq, B, max_tokens, per, x, range, blockIdx.x == 0 && wv == 0 ? ranges : nullptr);
-        if (b < 0) return;
+        work = find_work(p, seq, B, max_tokens, share, x, blockIdx.x == 0 && wv == 0 ? ranges : nullptr);
+        if (work.b < 0) return;
     }
-    const int slot = slot_of(seq, b, p.S);
-    const int n = tokens_of(p, seq, b, max_tokens);
-    const int k0 = whole ? 0 : (x - range.first) * per * kDecodeQuantum;
-    const int k1 = whole ? n : (int)min((long long)n, k0 + (long long)per * kDecodeQuantum);
+    const int b = work.b, slot = work.slot, k0 = work.k0, k1 = work.k1;
     const int page = 1 << p.shift;
     const size_t row0 = ((size_t)l * B + b) * p.Hkv + j;  // the segment's first query row, over G
 
@@ -425,43 +476,51 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
     sums.start(q + row0 * G * D, G);
 
     // page numbers of 64 pages at a time, one per lane; a step's tokens lie in one
-    // page.  Returns the tokens that count: none where the page number is invalid.
+    // page.  A step whose page number is invalid loads page 0 and is passed over.
     const int32_t* row = p.table + (size_t)max(slot, 0) * p.M;
+    const char* ring = s_ring + wv * kRing;
     int ids = 0, ids0 = -kWave;
-    const char* block = nullptr;
-    auto find = [&](int t0) -> int {
-        const int at = t0 >> p.shift;
+    uint32_t there = 0;  // by slot
+    auto issue = [&](int t, int at_slot) {
+        const int at = t >> p.shift;
         if (at >= ids0 + kWave || ids0 < 0) {
             ids0 = at;
             ids = row[min(at + lane, p.M - 1)];
+            settle(ids);
         }
         const int pg = __builtin_amdgcn_readlane(ids, at - ids0);
-        const bool there = pg >= 0 && pg < p.n_pages;
-        block = page_block<D>(p, l, there ? pg : 0, j);
-        return there ? k1 - t0 : 0;
+        const bool ok = pg >= 0 && pg < p.n_pages;
+        there = (there & ~(1u << at_slot)) | (uint32_t)ok << at_slot;
+        S::load(page_block<D>(p, l, ok ? pg : 0, j), t & (page - 1), p.shift, ring + at_slot * S::kBytes);
     };
     constexpr int kStride = kWaves * kBlk;
-    Step<D> st;
-    int t0 = k0 + wv * kBlk, left = 0;
-    if (t0 < k1) {
-        left = find(t0);
-        st.load_keys(block, t0 & (page - 1), p.shift);
-        st.load_values(block, t0 & (page - 1), p.shift);
-    }
-    while (t0 < k1) {
-        const int t1 = t0 + kStride, now = left;
-        f32x4 acc[2];
-        sums.logits(st, acc);
-        if (t1 < k1) {
-            left = find(t1);
-            st.load_keys(block, t1 & (page - 1), p.shift);
+    int t0 = k0 + wv * kBlk;
+    sums.settle_queries();
+#pragma unroll
+    for (int i = 0; i < S::kSlots; ++i)
+        if (t0 + i * kStride < k1) issue(t0 + i * kStride, i);
+    for (int at = 0; t0 < k1; t0 += kStride) {
+        // the slot's loads are the oldest: those of the slots behind it may be in flight
+        if (t0 + (S::kSlots - 1) * kStride < k1)
+            wait_vmcnt<(S::kSlots - 1) * S::kLoads>();
+        else
+            wait_vmcnt<0>();
+        asm volatile("" ::: "memory");
+        if ((there >> at) & 1u) {
+            const char* slot_at = ring + at * S::kBytes;
+            f32x4 acc[2];
+            sums.logits(slot_at, acc);
+            sums.add(slot_at, acc, k1 - t0, sl2);
         }
-        if (now > 0) sums.add(st, acc, now, sl2);
-        if (t1 < k1) st.load_values(block, t1 & (page - 1), p.shift);
-        t0 = t1;
+        if (t0 + S::kSlots * kStride < k1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
+            issue(t0 + S::kSlots * kStride, at);
+        }
+        at = at + 1 == S::kSlots ? 0 : at + 1;
     }
     sums.finish();
 
+    __syncthreads();  // every wave is done with its ring
     if (c < G) {
         if (quarter == 0) {
             s_ml[wv][0][c] = sums.m;
@@ -488,7 +547,7 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
                 ot = fmaf(a, s_o[w][h][ch], ot);
             }
         }
-        if (range.count == 1) {  // the whole sequence: the result itself
+        if (work.range.count == 1) {  // the whole sequence: the result itself
             out[(row0 * G + h) * D + ch] = lt != 0.0f ? ot / lt : 0.0f;
         } else {
             const size_t part = ((size_t)pair * groups + x) * G + h;

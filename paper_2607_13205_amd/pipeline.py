@@ -2,8 +2,9 @@
 
 score (SnapKV windowed + pooled, H2O, or the one-shot Quest page bound)  ->
 role allocation (host)  ->
-per-role top-k  ->  K/V compaction.  Buffers are allocated once by
-``EvictBuffers`` so that repeated steps allocate nothing.
+per-role top-k  ->  K/V compaction, into a dense cache or into the pages of a
+4-bit one (``alloc_pages``).  Buffers are allocated once by ``EvictBuffers`` so
+that repeated steps allocate nothing.
 
 ``Policy`` names how the budget is split over buckets: the role-conditional
 weights of §4.1, fair eviction (§4.1, the same rate for every bucket) or the
@@ -17,6 +18,7 @@ from dataclasses import dataclass
 import numpy as np
 
 from . import binding as kb
+from . import pages as kp
 
 
 @dataclass(frozen=True)
@@ -97,18 +99,30 @@ class EvictBuffers:
     k_cap: int
     copy_done: object = None   # event after the last quota upload from quota_host
     hist: object = None        # per-tile role histograms of the fused SnapKV epilogue, [L, words per layer]
+    pages: object = None       # the Pages that take the kept rows in place of k_out and v_out
+    add: object = None         # with pages: kept rows of each sample, int32 [B]
+    start: object = None       # with pages: each sample's first position (-1: no room), int32 [B]
+    missing: object = None     # with pages: pages that were lacking, int32 [1]
+    ws_pages: object = None
 
 
 def alloc_buffers(k, n_q_heads: int, W: int, R: int, k_cap: int, scorer: str = "snapkv",
-                  with_v: bool = True, fused: bool = False) -> EvictBuffers:
+                  with_v: bool = True, fused: bool = False, pages=None) -> EvictBuffers:
     """Buffers of repeated eviction steps.  fused (SnapKV only): the score's
     pool epilogue counts the top-k's first digit per role bucket
     (snapkv_score_hist / topk_select_hist) and the histograms live here.  Off
     by default: on the 32-layer N = 32768 step the counting adds more to the
-    pool (about 100 us) than it takes off the top-k (about 25 us)."""
+    pool (about 100 us) than it takes off the top-k (about 25 us).  pages: a
+    Pages of as many layers that the steps pack the kept rows into (evict's
+    ``slots``); there is no dense output then."""
     import torch
     L, B, Hkv, N, d = k.shape
     dev = k.device
+    if pages is not None and not with_v:
+        raise ValueError("pages hold keys and values")
+    if pages is not None and (pages.L, pages.Hkv, pages.d) != (L, Hkv, d):
+        raise ValueError(f"pages are of L={pages.L}, Hkv={pages.Hkv}, d={pages.d}, the keys of {L}, {Hkv}, {d}")
+    dense = pages is None
     if scorer == "snapkv":
         wsb = kb.snapkv_workspace_size(L, B, n_q_heads, Hkv, N, W, d)
     elif scorer == "quest":
@@ -123,12 +137,33 @@ def alloc_buffers(k, n_q_heads: int, W: int, R: int, k_cap: int, scorer: str = "
         quota_dev=torch.zeros((B, R), dtype=torch.int32, device=dev),
         idx=torch.full((L, B, Hkv, k_cap), -1, dtype=torch.int32, device=dev),
         count=torch.zeros((L, B, Hkv), dtype=torch.int32, device=dev),
-        k_out=torch.zeros((L, B, Hkv, k_cap, d), dtype=k.dtype, device=dev),
-        v_out=torch.zeros((L, B, Hkv, k_cap, d), dtype=k.dtype, device=dev) if with_v else None,
+        k_out=torch.zeros((L, B, Hkv, k_cap, d), dtype=k.dtype, device=dev) if dense else None,
+        v_out=torch.zeros((L, B, Hkv, k_cap, d), dtype=k.dtype, device=dev) if with_v and dense else None,
         k_cap=k_cap,
         hist=(torch.empty((L, kb.role_hist_size(1, B, Hkv, N, R) // 4), dtype=torch.int32, device=dev)
               if fused and scorer == "snapkv" else None),
+        pages=pages,
+        add=None if dense else torch.zeros(B, dtype=torch.int32, device=dev),
+        start=None if dense else torch.zeros(B, dtype=torch.int32, device=dev),
+        missing=None if dense else torch.zeros(1, dtype=torch.int32, device=dev),
+        ws_pages=None if dense else torch.empty(kp.pages_workspace_size(pages.c.n_pages, pages.c.S, B),
+                                                dtype=torch.uint8, device=dev),
     )
+
+
+def alloc_pages(L: int, Hkv: int, d: int, n_pages: int, slots: int, max_tokens: int, page: int = 64,
+                device="cuda") -> kp.Pages:
+    """An empty paged 4-bit cache: n_pages pages of ``page`` tokens for ``slots``
+    sequences of up to max_tokens tokens."""
+    import torch
+    nb = kp.page_bytes(page, d)
+    if nb == 0:
+        raise ValueError(f"page={page} must be a power of two in [32, 1024] and d={d} 64 or 128")
+
+    def zeros(*shape):
+        return torch.zeros(shape, dtype=torch.int32, device=device)
+    return kp.Pages(torch.zeros((L, n_pages, Hkv, nb), dtype=torch.uint8, device=device), zeros(n_pages),
+                    zeros(slots, -(-max_tokens // page)), zeros(slots), zeros(slots), page, d)
 
 
 def _fused(bufs, scorer, lse_win):
@@ -159,7 +194,24 @@ def _score(q, k, bufs, scorer, pool_k, scale, page, l0, l1, stream=None, lse_win
         kb.h2o_score(q, k, scale, score=score, workspace=bufs.ws_score, stream=stream)
 
 
-def _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=None, events=None, fused=False):
+def _compact(k, v, bufs, idx, count, l0, l1, slots, stream):
+    """Compaction of layers [l0, l1): into the dense cache, or into pages, for which
+    the first layers' counts (all layers' and heads' are equal) make room."""
+    if bufs.pages is None:
+        kb.kv_compact(k, v, idx, count, k_out=_part(bufs.k_out, l0, l1), v_out=_part(bufs.v_out, l0, l1),
+                      stream=stream)
+        return
+    if l0 == 0:
+        import torch
+        with torch.cuda.stream(torch.cuda.current_stream() if stream is None else stream):
+            bufs.add.copy_(count[0, :, 0])
+        kp.pages_extend(bufs.pages, bufs.add, seq=slots, start=bufs.start, missing=bufs.missing,
+                        workspace=bufs.ws_pages, stream=stream)
+    pages = bufs.pages if l0 == 0 and l1 == bufs.pages.L else bufs.pages.layers(l0, l1)
+    kp.pages_compact(k, v, idx, count, pages, bufs.start, seq=slots, stream=stream)
+
+
+def _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=None, events=None, fused=False, slots=None):
     """Top-k and compaction of layers [l0, l1) on ``stream`` (None: current);
     ``events``, three torch.cuda.Event, are recorded before the top-k, between
     the two calls and after the compaction.  fused: the score call counted the
@@ -175,8 +227,7 @@ def _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=None, events=None, fused
                        workspace=bufs.ws_topk, stream=stream)
     if events is not None:
         events[1].record(stream)
-    kb.kv_compact(_part(k, l0, l1), _part(v, l0, l1), idx, count, k_out=_part(bufs.k_out, l0, l1),
-                  v_out=_part(bufs.v_out, l0, l1), stream=stream)
+    _compact(_part(k, l0, l1), _part(v, l0, l1), bufs, idx, count, l0, l1, slots, stream)
     if events is not None:
         events[2].record(stream)
 
@@ -200,7 +251,7 @@ def _upload_quotas(policy, roles_host, budget, W, bufs, stream):
 def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: int,
           pool_k: int, bufs: EvictBuffers, scorer: str = "snapkv", scale: float = 0.0,
           score_events=None, page: int = 16, chunks: int = 1, side_stream=None, lse_win=None,
-          select_events=None):
+          select_events=None, slots=None):
     """One eviction step; returns (quota [B, R] host, kept [B] host).
 
     q is the window queries [L, B, Hq, W, d] (SnapKV; Quest, which scores
@@ -213,6 +264,12 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
     ``lse_win`` (SnapKV only),
     the window rows' log-sum-exp [L, B, Hq, W] as the prefill attention
     returned it, lets the score read K once.
+
+    With buffers made for a paged cache (alloc_buffers(pages=...)) the kept rows
+    are packed behind the sequences in slots ``slots`` (int32 [B] on the device;
+    None: sample b in slot b), from position bufs.start[b] on.  A sample that the
+    cache has no room for keeps nothing: its start is -1, and bufs.missing, on
+    the device like start, tells how many pages were lacking.
 
     The score does not depend on the quotas: it is queued first, and the host
     works the quotas out from the labels and queues their upload while the
@@ -238,7 +295,7 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
         if score_events is not None:
             score_events[1].record(main)
         quota, kept = _upload_quotas(policy, roles_host, budget, W, bufs, main)
-        _select(k, v, roles_dev, bufs, W, R, 0, L, stream=main, events=select_events, fused=fused)
+        _select(k, v, roles_dev, bufs, W, R, 0, L, stream=main, events=select_events, fused=fused, slots=slots)
         return quota, kept
     quota, kept = _upload_quotas(policy, roles_host, budget, W, bufs, main)
     side_stream.wait_stream(main)         # the quota upload and earlier work
@@ -252,7 +309,7 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
         done = torch.cuda.Event()
         done.record(main)
         side_stream.wait_event(done)
-        _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=side_stream, fused=fused)
+        _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=side_stream, fused=fused, slots=slots)
     if score_events is not None:
         score_events[1].record(main)
     main.wait_stream(side_stream)
@@ -277,6 +334,8 @@ class StepGraph:
     def __init__(self, q, k, v, roles_dev, policy, W: int, pool_k: int, bufs: EvictBuffers,
                  scorer: str = "snapkv", scale: float = 0.0, page: int = 16, lse_win=None):
         import torch
+        if bufs.pages is not None:
+            raise ValueError("a replayed step would extend the sequences of its slots each time: use evict")
         self.policy = as_policy(policy)
         self.W = W
         self.bufs = bufs

@@ -572,3 +572,127 @@ def test_forked_sequences_go_their_own_ways(K):
     assert np.array_equal(rows_of(pages, 3)[1], O.mx4_round(y[:, 0].double().cpu().numpy()))
     K.pages_free(pages)
     assert not pages.refs.any()
+
+
+# ---------------------------------------------------------------------------
+# the eviction step into pages
+# ---------------------------------------------------------------------------
+
+def _workload(name, **kw):
+    import workload as WL
+    base = WL.get_workload("layer8k")
+    f = dict(L=3, B=2, Hq=8, Hkv=2, N=700, W=16, d=64, pool_k=5, dtype="bf16", mix=base.mix, budgets=(0.2,))
+    f.update(kw)
+    wl = WL.Workload(name, **f)
+    return WL, wl, WL.make_inputs(wl, device="cuda:0")
+
+
+@pytest.mark.parametrize("chunks", [1, 2])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 128)])
+def test_evict_into_pages_keeps_the_rows_of_the_dense_step(K, chunks, dtype, d):
+    from paper_2607_13205_amd import pipeline
+    WL, wl, inp = _workload("paged", dtype=dtype, d=d)
+    alpha = WL.default_alpha(0.0)
+    k_cap = K.role_allocate(inp["roles"], 4, alpha, 0.2, wl.W)[2]
+    args = (inp["q"], inp["k"], inp["v"], inp["roles"], inp["roles_t"], alpha, 0.2, wl.W, wl.pool_k)
+    dense = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, k_cap)
+    _, kept = pipeline.evict(*args, dense)
+    cache = pipeline.alloc_pages(wl.L, wl.Hkv, d, 40, 5, 2 * k_cap, page=32)
+    bufs = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, k_cap, pages=cache)
+    assert bufs.k_out is None and bufs.v_out is None
+    slots = dev([3, 1])
+    side = torch.cuda.Stream() if chunks > 1 else None
+    for times in (1, 2):  # a second step packs behind the first
+        _, kept2 = pipeline.evict(*args, bufs, chunks=chunks, side_stream=side, slots=slots)
+        assert np.array_equal(kept, kept2) and bufs.missing.item() == 0
+        assert bufs.start.tolist() == [(times - 1) * int(n) for n in kept]
+        assert cache.length[slots.long()].tolist() == [times * int(n) for n in kept]
+    for b, slot in enumerate((3, 1)):
+        n = int(kept[b])
+        for got, x in zip(rows_of(cache, slot), (dense.k_out, dense.v_out)):
+            want = O.mx4_round(x[:, b, :, :n].double().cpu().numpy())
+            assert np.array_equal(got[:, :, :n], want) and np.array_equal(got[:, :, n:], want)
+    # no room: the first sample's pages are there, the second's are not
+    small = pipeline.alloc_pages(wl.L, wl.Hkv, d, -(-int(kept[0]) // 32), 2, k_cap, page=32)
+    bufs = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, k_cap, pages=small)
+    pipeline.evict(*args, bufs)
+    assert bufs.start.tolist() == [0, -1] and bufs.missing.item() == -(-int(kept[1]) // 32)
+    assert small.length.tolist() == [int(kept[0]), 0]
+
+
+def test_evict_into_pages_refusals(K):
+    from paper_2607_13205_amd import pipeline
+    WL, wl, inp = _workload("paged_no")
+    cache = pipeline.alloc_pages(wl.L, wl.Hkv, wl.d, 4, 2, 64)
+    with pytest.raises(ValueError):
+        pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, 60, with_v=False, pages=cache)
+    with pytest.raises(ValueError):
+        pipeline.alloc_buffers(inp["k"][:2], wl.Hq, wl.W, 4, 60, pages=cache)
+    bufs = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, 60, pages=cache)
+    with pytest.raises(ValueError):
+        pipeline.StepGraph(inp["q"], inp["k"], inp["v"], inp["roles_t"], WL.default_alpha(0.0), wl.W, wl.pool_k, bufs)
+    for kw in (dict(page=48), dict(d=96)):
+        with pytest.raises(ValueError):
+            pipeline.alloc_pages(**dict(dict(L=1, Hkv=1, d=64, n_pages=4, slots=1, max_tokens=10), **kw))
+
+
+def test_a_sequence_from_prompt_to_end(K):
+    """Eviction into pages, decode steps, two continuations, a second eviction of what has grown, and the end."""
+    from paper_2607_13205_amd import pipeline
+    WL, wl, inp = _workload("paged_life", B=1, N=900)
+    L, Hkv, G, d, page = wl.L, wl.Hkv, wl.Hq // wl.Hkv, wl.d, 32
+    alpha = WL.default_alpha(0.0)
+    k_cap = K.role_allocate(inp["roles"], 4, alpha, 0.2, wl.W)[2]
+    cache = pipeline.alloc_pages(L, Hkv, d, 60, 4, 400, page=page)
+    bufs = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, k_cap, pages=cache)
+    slot0 = dev([2])
+    _, kept = pipeline.evict(inp["q"], inp["k"], inp["v"], inp["roles"], inp["roles_t"], alpha, 0.2, wl.W, wl.pool_k,
+                             bufs, slots=slot0)
+    n = int(kept[0])
+    rows = [x[:, :, :] for x in rows_of(cache, 2)]                   # [L, Hkv, n, d], as held
+
+    def step(slots, seed, rows):
+        B = len(slots)
+        seq = dev(slots)
+        k, v = normal((L, B, Hkv, 1, d), "bf16", seed).cuda(), normal((L, B, Hkv, 1, d), "bf16", seed + 1).cuda()
+        q = normal((L, B, wl.Hq, d), "bf16", seed + 2).cuda()
+        start, missing = K.pages_extend(cache, dev([1] * B), seq=seq)
+        K.pages_append(k, v, cache, start, seq=seq)
+        out = K.decode_pages(q, cache, seq=seq)
+        assert missing.item() == 0
+        for b in range(B):
+            for i, x in enumerate((k, v)):
+                rows[b][i] = np.concatenate([rows[b][i], O.mx4_round(x[:, b].double().cpu().numpy())], axis=2)
+            for l in range(L):
+                want, mag, top = _decode_ref(q[l, b].double().cpu().numpy(), rows[b][0][l], rows[b][1][l], G)
+                check_decode(out[l, b].cpu().numpy(), want, mag, top)
+
+    first = [list(rows)]
+    for t in range(5):
+        step([2], 10 * t, first)
+    done, _ = K.pages_fork(cache, dev([2, 2]), dev([0, 3]))
+    assert done.tolist() == [1, 1]
+    K.pages_free(cache, slot0)
+    two = [list(first[0]), list(first[0])]
+    for t in range(40):
+        step([0, 3], 1000 + 10 * t, two)
+    # a second eviction of slot 0: scored on its keys as read back, one bucket, window kept
+    N2 = n + 45
+    k2, _ = K.pages_read(cache, N2, seq=dev([0]))
+    q2 = normal((L, 1, wl.Hq, wl.W, d), "bf16", 5).cuda()
+    score = K.snapkv_score(q2, k2, wl.pool_k)
+    zero = torch.zeros((1, N2), dtype=torch.int8, device="cuda")
+    keep = 70
+    idx, count = K.topk_select(score, zero, dev([[keep - wl.W]]), wl.W, 1, keep)
+    start, missing = K.pages_extend(cache, dev([keep]), seq=slot0)
+    K.pages_select(cache, dev([0]), idx, count, slot0, start)
+    K.pages_free(cache, dev([0]))
+    assert missing.item() == 0 and (count == keep).all()
+    at = idx[:, 0].cpu().numpy()
+    third = [[np.take_along_axis(x, at[..., None].astype(np.int64), axis=2) for x in two[0]]]
+    for got, want in zip(rows_of(cache, 2), third[0]):
+        assert np.array_equal(got, want)
+    step([2], 7, third)
+    step([3], 8, [two[1]])
+    K.pages_free(cache)
+    assert not cache.refs.any() and not cache.length.any()

@@ -51,6 +51,11 @@
  * sequences, page numbers outside [0, n_pages) as missing rows, held as at most
  * M, length as at most held * page.  No call reads or writes outside the
  * buffers whatever they hold.
+ *
+ * Calls on one cache are ordered by the caller, on one stream or by events, where
+ * one changes bookkeeping or rows that the other uses.  Calls that only read
+ * (kve_pages_read, kve_decode_pages) may overlap, and so may calls that write
+ * rows of different sequences.
  */
 #ifndef KVE_PAGES_H
 #define KVE_PAGES_H

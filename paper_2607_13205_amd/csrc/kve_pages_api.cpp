@@ -70,7 +70,7 @@ kve_status_t check_rows(const char* fn, const kve_pages_t* c, int B, int cap, co
     if (need_seq && seq == nullptr) return fail(KVE_ERR_INVALID_ARG, "%s: null slots", fn);
     if (seq == nullptr && B > c->S)
         return fail(KVE_ERR_INVALID_ARG, "%s: %d samples without slots, the cache has %d", fn, B, c->S);
-    const double groups = (double)c->L * B * c->Hkv * (cap / kve::kPagesRowsMin + 1);
+    const double groups = (double)c->L * B * c->Hkv * (cap / kve::kPagesRows + 1);
     if (cap > (1 << 30) || groups > (double)kMaxGroups) return fail(KVE_ERR_UNSUPPORTED, "%s: shape too large", fn);
     return KVE_OK;
 }

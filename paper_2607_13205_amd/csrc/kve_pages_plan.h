@@ -11,7 +11,8 @@ namespace kve {
 constexpr int kPageMin = 32, kPageMax = 1024;  // tokens per page, powers of two
 constexpr int kPagesMaxEntries = 1024;         // entries of one bookkeeping call: one per thread of its workgroup
 constexpr int kPagesMaxGroup = 16;             // query heads per KV head: the columns of a 16x16 product
-constexpr int kPagesRowsMin = 16;              // fewest rows per workgroup of a call on rows
+constexpr int kPagesRows = 64;                 // rows per workgroup of a call on rows
+constexpr int kPagesPlanBytes = 32;            // what a fork notes for an entry
 
 // The cache as kernels see it.  shift: log2 of the page size.
 struct PagePool {
@@ -30,10 +31,10 @@ inline int pages_copy_blocks(int Hkv, int page, int d) {
     return (int)((Hkv * page_block_bytes(page, d) + kPagesCopyBytes - 1) / kPagesCopyBytes);
 }
 
-// Workspace of extend and fork: one fork_plan entry per entry, then the free
-// pages found, at most as many as there are.
+// Workspace of extend and fork: a note per entry, then the free pages found, at
+// most as many as there are.
 inline size_t pages_workspace(int n_pages, int n) {
-    return align_up((size_t)n * 16) + align_up((size_t)n_pages * sizeof(int32_t));
+    return align_up((size_t)n * kPagesPlanBytes) + align_up((size_t)n_pages * sizeof(int32_t));
 }
 
 // Plan of a decode over pages.  The lengths are on the device, so the splits are

@@ -127,7 +127,7 @@ __device__ __forceinline__ uint32_t pack_eight(const Eight<T>& x, uint32_t& s) {
 // (kve_pages_select) and out of them (kve_pages_read)
 // ---------------------------------------------------------------------------
 
-constexpr int kRows = 64;  // rows per workgroup
+constexpr int kRows = kPagesRows;  // per workgroup
 
 // The rows of a call: `cap` of each of L B Hkv segments (layer, sample, KV head).
 // A workgroup takes kRows rows of one segment, or, Flat, kRows rows of all
@@ -442,11 +442,8 @@ __device__ __forceinline__ int owner_of(const int* s_off, int n, int r) {
 // kve_pages_extend: one workgroup, one thread per entry.  Needs are summed over
 // the entries before, the free pages listed, and every listed page given to the
 // entry whose range of the list it falls in.
-__global__ __launch_bounds__(kPlanThreads) void extend_kernel(PagePool p, const int32_t* __restrict__ seq,
-                                                              const int32_t* __restrict__ add, int n,
-                                                              int32_t* __restrict__ start,
-                                                              int32_t* __restrict__ missing,
-                                                              int32_t* __restrict__ list) {
+__global__ __launch_bounds__(kPlanThreads) void extend_kernel(PagePool p, const int32_t* seq, const int32_t* add, int n,
+                                                              int32_t* start, int32_t* missing, int32_t* list) {
     __shared__ __attribute__((aligned(16))) int s_seq[kPlanThreads];
     __shared__ int s_off[kPlanThreads], s_held[kPlanThreads], s_ok[kPlanThreads];
     __shared__ uint32_t s_scan[kPlanWaves];
@@ -491,17 +488,15 @@ __global__ __launch_bounds__(kPlanThreads) void extend_kernel(PagePool p, const 
 }
 
 // What fork_copy does for an entry: full pages shared (-1: refused), the partial
-// page's source and copy (copy < 0: none) and its rows.
+// page's source and copy (copy < 0: none) and its rows, and the two slots.  The
+// caller's arrays are read once: `done` may be one of them.
 struct ForkPlan {
-    int full, from, to, rows;
+    int full, from, to, rows, src, dst, unused[2];
 };
 
-__global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagePool p, const int32_t* __restrict__ src,
-                                                            const int32_t* __restrict__ dst, int n,
-                                                            int32_t* __restrict__ done,
-                                                            int32_t* __restrict__ missing,
-                                                            ForkPlan* __restrict__ plan,
-                                                            int32_t* __restrict__ list) {
+__global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagePool p, const int32_t* src, const int32_t* dst, int n,
+                                                            int32_t* done, int32_t* missing, ForkPlan* plan,
+                                                            int32_t* list) {
     __shared__ __attribute__((aligned(16))) int s_dst[kPlanThreads];
     __shared__ uint32_t s_scan[kPlanWaves];
     const int i = threadIdx.x;
@@ -520,7 +515,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagePool p, const in
     const int found = find_free(p.refs, p.n_pages, (int)total, list);
     const bool given = valid && (need == 0 || off < (uint32_t)found);
     if (i < n) {
-        ForkPlan f{given ? full : -1, -1, -1, rows};
+        ForkPlan f{given ? full : -1, -1, -1, rows, from, to, {0, 0}};
         if (given) {
             if (need != 0) {
                 f.from = p.table[(size_t)from * p.M + full];
@@ -541,15 +536,13 @@ __global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagePool p, const in
 // written rows of the partial page, kPagesCopyBytes of one layer's heads each.  A
 // 16-byte piece is copied when it holds a byte of a written row.
 template <int D>
-__global__ __launch_bounds__(kThreads) void fork_copy(PagePool p, const int32_t* __restrict__ src,
-                                                      const int32_t* __restrict__ dst,
-                                                      const ForkPlan* __restrict__ plan, int nblk) {
+__global__ __launch_bounds__(kThreads) void fork_copy(PagePool p, const ForkPlan* __restrict__ plan, int nblk) {
     const int i = blockIdx.x / (1 + p.L * nblk), part = blockIdx.x - i * (1 + p.L * nblk);
     const ForkPlan f = plan[i];
     if (f.full < 0) return;
     if (part == 0) {
-        const int32_t* a = p.table + (size_t)src[i] * p.M;
-        int32_t* o = p.table + (size_t)dst[i] * p.M;
+        const int32_t* a = p.table + (size_t)f.src * p.M;
+        int32_t* o = p.table + (size_t)f.dst * p.M;
         for (int e = threadIdx.x; e < f.full; e += kThreads) {
             const int pg = a[e];
             o[e] = pg;
@@ -654,16 +647,16 @@ hipError_t launch_pages_extend(const PagePool& p, const int32_t* seq, const int3
 
 hipError_t launch_pages_fork(const PagePool& p, int d, const int32_t* src, const int32_t* dst, int n, int32_t* done,
                              int32_t* missing, void* ws, hipStream_t st) {
-    static_assert(sizeof(ForkPlan) == 16, "pages_workspace counts 16 bytes per entry");
+    static_assert(sizeof(ForkPlan) == kPagesPlanBytes, "the workspace holds a plan per entry");
     ForkPlan* plan = static_cast<ForkPlan*>(ws);
     int32_t* list = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + align_up((size_t)n * sizeof(ForkPlan)));
     hipLaunchKernelGGL(fork_kernel, dim3(1), dim3(kPlanThreads), 0, st, p, src, dst, n, done, missing, plan, list);
     const int nblk = pages_copy_blocks(p.Hkv, 1 << p.shift, d);
     const dim3 grid((unsigned)n * (1 + p.L * nblk));
     if (d == 128)
-        hipLaunchKernelGGL(fork_copy<128>, grid, dim3(kThreads), 0, st, p, src, dst, plan, nblk);
+        hipLaunchKernelGGL(fork_copy<128>, grid, dim3(kThreads), 0, st, p, plan, nblk);
     else
-        hipLaunchKernelGGL(fork_copy<64>, grid, dim3(kThreads), 0, st, p, src, dst, plan, nblk);
+        hipLaunchKernelGGL(fork_copy<64>, grid, dim3(kThreads), 0, st, p, plan, nblk);
     return hipGetLastError();
 }
 

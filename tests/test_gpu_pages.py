@@ -335,6 +335,20 @@ def test_bookkeeping_follows_the_oracle(K, seed, S, M, page, n_pages):
     assert not pages.refs.any() and not pages.held.any() and not pages.length.any()
 
 
+def test_outputs_may_take_the_place_of_inputs(K):
+    """done in the array of sources, start in that of the counts: read before they are written."""
+    pages, k, _ = _filled(K, 1, 1, 64, 32, [75, 40], extra_slots=4, spare=8)
+    src, dst = dev([1, 0, 0]), dev([5, 3, 4])
+    done, _ = K.pages_fork(pages, src, dst, done=src)
+    assert done.tolist() == [1, 1, 1] and pages.length.tolist() == [75, 40, 0, 75, 75, 40]
+    for slot, of in ((3, 0), (4, 0), (5, 1)):
+        n = int(pages.length[slot])
+        assert np.array_equal(rows_of(pages, slot)[0], O.mx4_round(k[:, of, :, :n].double().cpu().numpy()))
+    add = dev([7, 0, 9])
+    start, _ = K.pages_extend(pages, add, seq=dev([3, 4, 5]), start=add)
+    assert start.tolist() == [75, 75, 40] and pages.length.tolist() == [75, 40, 0, 82, 75, 49]
+
+
 def test_many_entries_and_a_large_pool(K):
     """1024 entries; free pages scattered over 300000, found in ascending order over many rounds."""
     r = np.random.default_rng(11)

@@ -442,6 +442,33 @@ def test_decode(K, Hkv, G, d, page, lengths, most, dtype, qs):
     report(f"paged decode worst err/bound g{G} d{d} {dtype} x{qs:g}", round(worst, 4))
 
 
+@pytest.mark.parametrize("L,B,Hkv,G,page,longest,most", [
+    (1, 150, 1, 2, 32, 700, None),     # more sequences than a wave has lanes, several splits each
+    (1, 64, 2, 4, 64, 200, 200),
+    (1, 65, 1, 1, 32, 1500, None),
+    (130, 2, 8, 1, 64, 2300, None),    # more (layer, KV head) pairs than resident workgroups: one split per sequence
+    (40, 30, 1, 4, 128, 1100, 1100),   # a workgroup per sequence
+])
+def test_decode_of_many_sequences_and_pairs(K, L, B, Hkv, G, page, longest, most):
+    """Ragged lengths with empty sequences among them, slots named twice and in any order."""
+    r = np.random.default_rng(B)
+    d, Hq = 64, Hkv * G
+    lengths = [longest] + [int(r.integers(0, longest + 1)) if r.random() < 0.8 else 0 for _ in range(B - 1)]
+    pages, _, _ = _filled(K, L, Hkv, d, page, lengths, seed=B)
+    order = np.concatenate([r.permutation(B)[:B - 1], [0]])
+    q = normal((L, B, Hq, d), "bf16", 78).cuda()
+    out = torch.full((L, B, Hq, d), float("nan"), device="cuda")
+    K.decode_pages(q, pages, max_tokens=most, seq=dev(order), out=out)
+    k, v = (x.float().cpu().numpy().astype(np.float64) for x in K.pages_read(pages, longest, seq=dev(order)))
+    qn, on = q.double().cpu().numpy(), out.double().cpu().numpy()
+    for l in sorted({0, L // 2, L - 1}):
+        for i, s in enumerate(order):
+            n = lengths[s]
+            want, mag, top = _decode_ref(qn[l, i], k[l, i, :, :n], v[l, i, :, :n], G)
+            check_decode(on[l, i], want, mag, top, f"sample {i} of {n} layer {l}")
+    assert torch.isfinite(out).all()
+
+
 def test_decode_equals_decode_over_the_rows_read_back(K):
     """The same rows dense in bf16: decode_attention gives the same to float32 rounding."""
     lengths = [700, 64, 0, 333]

@@ -517,6 +517,90 @@ def test_decode_leaves_out_missing_pages_and_passes_nan_on(K):
 
 
 # ---------------------------------------------------------------------------
+# offsets beyond 32 bits
+# ---------------------------------------------------------------------------
+
+def test_pages_beyond_four_gigabytes(K):
+    """The last pages of a pool of 4.9 GB: rows written, forked, moved, read and attended to where they belong."""
+    Hkv, d, page, n_pages = 8, 128, 64, 70_000
+    pool = torch.zeros((1, n_pages, Hkv, K.page_bytes(page, d)), dtype=torch.uint8, device="cuda")
+    assert pool.numel() > 1 << 32
+    refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    refs[-8:] = 0                                                    # only the last pages are free
+    z = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    pages = K.Pages(pool, refs, z(3, 4), z(3), z(3), page, d)
+    n = 100
+    start, _ = K.pages_extend(pages, dev([n]), seq=dev([0]))
+    x = normal((2, 1, 1, Hkv, n, d), "bf16", 1).cuda()
+    K.pages_append(x[0], x[1], pages, start, seq=dev([0]))
+    assert pages.table[0, :2].tolist() == [n_pages - 8, n_pages - 7]
+    K.pages_fork(pages, dev([0]), dev([1]))
+    start, missing = K.pages_extend(pages, dev([n]), seq=dev([2]))
+    idx = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda").expand(1, 1, Hkv, n).contiguous()
+    K.pages_select(pages, dev([0]), idx, torch.full((1, 1, Hkv), n, dtype=torch.int32, device="cuda"), dev([2]), start)
+    assert missing.item() == 0
+    k, v = K.pages_read(pages, n, dtype=torch.float32)
+    want = [O.mx4_round(t[0, 0].double().cpu().numpy()) for t in x]
+    for got, w in ((k, want[0]), (v, want[1])):
+        got = got[0].double().cpu().numpy()
+        assert np.array_equal(got[0], w) and np.array_equal(got[1], w) and np.array_equal(got[2], w[:, ::-1])
+    assert not pool[:, :n_pages - 8].any()                           # nothing landed 4 GB lower
+    q = normal((1, 3, Hkv, d), "bf16", 2).cuda()
+    out = K.decode_pages(q, pages)
+    for s in range(3):
+        ref, mag, top = _decode_ref(q[0, s].double().cpu().numpy(), want[0], want[1], 1)
+        check_decode(out[0, s].cpu().numpy(), ref, mag, top)
+
+
+def test_millions_of_tokens(K):
+    """A table that names one page over and over: 8.4 million tokens to read (4.3 GB of float32 rows) and to attend
+    to.  The softmax over copies of a page is that over the page."""
+    Hkv, d, page = 1, 128, 32
+    M = (1 << 18) + 4
+    z = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    one = K.Pages(torch.zeros((1, 1, Hkv, K.page_bytes(page, d)), dtype=torch.uint8, device="cuda"), z(1), z(1, M), z(1),
+                  z(1), page, d)
+    start, _ = K.pages_extend(one, dev([page]))
+    x = normal((2, 1, 1, Hkv, page, d), "bf16", 3).cuda()
+    K.pages_append(x[0], x[1], one, start)
+    one.held.fill_(M)
+    one.length.fill_(M * page)
+    T = M * page
+    k_out = torch.empty((1, 1, Hkv, T, d), dtype=torch.float32, device="cuda")
+    v_out = torch.empty((1, 1, Hkv, T, d), dtype=torch.float32, device="cuda")
+    assert k_out.numel() * 4 > 1 << 32
+    K.pages_read(one, T, k_out=k_out, v_out=v_out)
+    for got, t in ((k_out, x[0]), (v_out, x[1])):
+        want = torch.from_numpy(O.mx4_round(t[0, 0, 0].double().cpu().numpy())).float().cuda()
+        assert bool((got.view(M, page, d) == want).all())
+    del k_out, v_out
+    q = normal((1, 1, 4, d), "bf16", 4).cuda()
+    out = K.decode_pages(q, one)
+    k, v = (O.mx4_round(t[0, 0].double().cpu().numpy()) for t in x)
+    ref, mag, top = _decode_ref(q[0, 0].double().cpu().numpy(), k, v, 4)
+    # 2^18 steps of 32 tokens over 4096 waves are 64 additions each, 32 within a product and at most 1024 splits
+    # merged: 1120 roundings of 2^-24 are 6.7e-5, inside the bound's 1e-4
+    check_decode(out[0, 0].cpu().numpy(), ref, mag, top)
+
+
+def test_source_rows_far_apart(K):
+    """A strided view whose rows lie 32 MiB apart, the last one beyond 4 GiB."""
+    d, N, far = 64, 140, 1 << 25
+    buf = torch.zeros((N * far + 256) // 2, dtype=torch.bfloat16, device="cuda")
+    view = torch.as_strided(buf, (1, 1, 1, N, d), (0, 0, 0, far // 2, 1))
+    x = normal((1, 1, 1, N, d), "bf16", 5).cuda()
+    view.copy_(x)
+    pages = make(K, 1, 1, d, 32, 6, 1, 6)
+    start, _ = K.pages_extend(pages, dev([N]))
+    K.pages_append(view, view, pages, start)
+    assert np.array_equal(rows_of(pages, 0)[1], O.mx4_round(x[0].double().cpu().numpy()))
+    idx = torch.tensor([[[[N - 1, 3]]]], dtype=torch.int32, device="cuda")
+    K.pages_compact(view, view, idx, torch.full((1, 1, 1), 2, dtype=torch.int32, device="cuda"), pages, start)
+    got = rows_of(pages, 0)[0][0, 0, :2]
+    assert np.array_equal(got, O.mx4_round(x[0, 0, 0, [N - 1, 3]].double().cpu().numpy()))
+
+
+# ---------------------------------------------------------------------------
 # together
 # ---------------------------------------------------------------------------
 

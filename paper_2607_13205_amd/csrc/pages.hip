@@ -251,7 +251,9 @@ __global__ __launch_bounds__(kThreads) void pack_rows(RowView kv, RowView vv, Ro
 }
 
 // D / 32 lanes to a row, each a block of 32 channels (16 bytes of codes, one
-// scale byte) of a key and a value row.
+// scale byte) of a key and a value row.  The source rows are read once and their
+// sequence ends, as a rule: non-temporal loads (16 layers, 4 sequences, 4001 of
+// 16001 rows: 105 us, 5.3 TB/s read and written; 115 without).
 template <int D, bool Flat>
 __global__ __launch_bounds__(kThreads) void select_rows(PagePool p, RowGrid g, const int32_t* __restrict__ src,
                                                         const int32_t* __restrict__ idx,
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void select_rows(PagePool p, RowGrid g, c
     if (a == nullptr || o == nullptr) return;
     const PageAt<D> at_a(ta, part, p.shift), at_o(tb, part, p.shift);
     const size_t values = at_a.values(p.shift), value_scales = at_a.value_scales(p.shift);
-    const u32x4 wk = ld16(a + at_a.codes), wv = ld16(a + at_a.codes + values);
+    const u32x4 wk = load16<true>(a + at_a.codes), wv = load16<true>(a + at_a.codes + values);
     const char sk = a[at_a.scales], sv = a[at_a.scales + value_scales];
     st16(o + at_o.codes, wk);
     st16(o + at_o.codes + values, wv);
@@ -280,7 +282,10 @@ __global__ __launch_bounds__(kThreads) void select_rows(PagePool p, RowGrid g, c
     o[at_o.scales + value_scales] = sv;
 }
 
-// D / 8 lanes to a row, as in pack_rows.
+// D / 8 lanes to a row, as in pack_rows.  Bound by HBM: 2 M rows of a pool of
+// 1.1 GB in 267 us, 5.0 TB/s read and written; 1.7 M rows just packed in 155 us.
+// Non-temporal loads of the codes gain 8% on the former and lose 7% on the
+// latter; cached stores lose 30%.
 template <typename T, int D, bool Flat>
 __global__ __launch_bounds__(kThreads) void read_rows(PagePool p, RowGrid g, const int32_t* __restrict__ seq,
                                                       const int32_t* __restrict__ start,

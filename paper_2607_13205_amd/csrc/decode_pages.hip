@@ -52,7 +52,10 @@ __device__ __forceinline__ void lds_dma4(const char* base, unsigned voff, const 
     asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(base), "{m0}"(m0) : "memory");
 }
 
-// Waves per SIMD that the registers are kept to, and so workgroups per compute unit.
+// Waves per SIMD that the registers are kept to, and so workgroups per compute
+// unit: four where the registers suffice without spills (8 layers, 4 sequences of
+// 8192: float32 queries 60 us at three and 70 at four, 16 heads per KV head 64.5
+// and 67).
 template <typename T, int D, int NH>
 constexpr int kPerSimd = D == 128 && (std::is_same<T, float>::value || NH > 8) ? 3 : 4;
 
@@ -222,7 +225,7 @@ struct Slot {
     static constexpr int kCodes = kBlk * D / 2;  // bytes of the key, and of the value codes
     static constexpr int kLoads = 2 * kCodes / 1024 + 1;
     static constexpr int kBytes = 2 * kCodes + 256;
-    static constexpr int kSlots = 4096 / kCodes;  // two steps of 128 channels ahead, four of 64
+    static constexpr int kSlots = 2;  // steps ahead; four of 64 channels gain nothing (61.5 and 61.8 us for 286 MB)
     static constexpr int kRow = D / 2;
 
     // The wave's loads of tokens tok .. + 32 of a block into `slot`: kLoads of them.
@@ -434,7 +437,11 @@ struct Sums {
 };
 
 // One workgroup per split of a sequence and (layer, KV head); its waves take 32
-// tokens in turn.
+// tokens in turn.  Bound by the loads: 32 layers, 4 sequences of 1639 tokens, 8 KV
+// heads of 4 query heads (228 MB of pages): 42 us, 5.4 TB/s, and 38.8 without any
+// arithmetic.  The vector unit is busy for about half of that; it converts K and V
+// (64 instructions per 32 tokens), pairs V's tokens (36), splits the weights (32)
+// and takes 8 exponentials and multiply-adds.
 template <typename T, int D, int NH>
 __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(const T* __restrict__ q, PagePool p,
                                                                   const int32_t* __restrict__ seq, int B, int G,
@@ -602,6 +609,10 @@ hipError_t run_heads(const void* q, const PagePool& p, int B, int Hq, int max_to
 template <typename T, int D>
 hipError_t run(const void* q, const PagePool& p, int B, int Hq, int max_tokens, const int32_t* seq, float scale,
                float* out, void* ws, hipStream_t st) {
+    // fewer columns per part of the weights are more products: with the sixteen-head
+    // form 4 heads take 57.6 us in place of 54.1 (8 layers, 4 sequences of 8192, d =
+    // 128), 70.8 in place of 61 (d = 64, 16 layers), 8 heads 88 in place of 71 (32
+    // ragged sequences of up to 32768)
     if (Hq / p.Hkv <= 4) return run_heads<T, D, 4>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);
     if (Hq / p.Hkv <= 8) return run_heads<T, D, 8>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);
     return run_heads<T, D, kPagesMaxGroup>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);

@@ -49,6 +49,10 @@ struct PagesPlan {
     size_t off_ml, off_ranges, total;
 };
 
+// `whole`, one split per sequence with no search and no merge, where there are
+// enough sequences and none can be long (32 layers x 8 heads: 4 sequences of 1639
+// tokens 43.5 us so and 45.5 without the rule, 8 of 300 26 and 32, 8 of 1639 81 and
+// 86); longer ones may differ too much.
 constexpr int kPagesMostResident = 4 * kDecodeUnits;  // workgroups, at four per compute unit
 
 inline PagesPlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens, int d) {

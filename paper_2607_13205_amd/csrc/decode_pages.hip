@@ -27,7 +27,7 @@
 //
 // Split-K and the lazy softmax reference are those of the dense decode
 // (decode.hip): weights are exp2(x - m) with m raised only when a logit exceeds it
-// by more than 64.  The denominators are one more row of the second product, a
+// by more than kRaise.  The denominators are one more row of the second product, a
 // row of ones.
 #include <type_traits>
 
@@ -43,7 +43,10 @@ namespace {
 constexpr int kThreads = kMergeThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBlk = 32;    // tokens per wave step
-constexpr int kSplitTries = 4;
+constexpr int kStaged = 4096;  // most sequences whose lengths are kept in LDS for the search
+// A weight may grow to 2^kRaise before the reference is raised: rarely after the
+// first step, and far from where the value sums overflow.
+constexpr float kRaise = 16.0f;
 constexpr int kMostQuanta = (1 << 30) / kDecodeQuantum;  // of a sequence
 
 // One direct-to-LDS load of four bytes per lane, as lds_dma16.
@@ -138,12 +141,15 @@ __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlan
 // A sequence as a lane holds it: its slot (-1: none) and its tokens.
 struct Sequence {
     int slot, tokens;
-    __device__ __forceinline__ Sequence(const PagePool& p, const int32_t* seq, int b, int B, int max_tokens) {
-        slot = b < B ? slot_of(seq, b, p.S) : -1;
-        tokens = slot < 0 ? 0 : min(length_of(p, slot), max_tokens);
-    }
-    __device__ __forceinline__ int quanta() const { return (tokens + kDecodeQuantum - 1) / kDecodeQuantum; }
 };
+
+__device__ __forceinline__ Sequence sequence_of(const PagePool& p, const int32_t* seq, int b, int B,
+                                                int max_tokens) {
+    const int slot = b < B ? slot_of(seq, b, p.S) : -1;
+    return Sequence{slot, slot < 0 ? 0 : min(length_of(p, slot), max_tokens)};
+}
+
+__device__ __forceinline__ int quanta_of(int tokens) { return (tokens + kDecodeQuantum - 1) / kDecodeQuantum; }
 
 __device__ __forceinline__ int splits_of(int quanta, int per) {
     return (int)((unsigned)(quanta + per - 1) / (unsigned)per);
@@ -160,47 +166,48 @@ struct Work {
     SplitRange range;
 };
 
-// How the sequences are cut (PagesPlan): quanta per split, such that the splits
-// are at most `share`, or at most share + B where a few tries find no such size;
-// and split x of them (b = -1: there is none).  Every wave works it out for
-// itself, 64 sequences at a time, the first 64 loaded once.  ranges: where not
+// How the sequences are cut (PagesPlan): the quanta of a split are a `share`-th of
+// all, rounded up, which makes at most share + B splits; and split x of them (b =
+// -1: there is none).  Longer ones that make no more than `share` are worse: the
+// longest then outlasts the others by more than a second round of short ones
+// costs (64 ragged sequences of up to 16384 tokens, 8 KV heads: 87 us so, 64.5
+// with a share-th; half of it and twice it 63.6 and 73).  Every wave works it out for
+// itself, 64 sequences at a time.  staged: the lengths of all sequences (null:
+// they are loaded; up to 64 once, and more several times).  ranges: where not
 // null, every sequence's range is written there.
 __device__ __forceinline__ Work find_work(const PagePool& p, const int32_t* seq, int B, int max_tokens, int share,
-                                          int x, SplitRange* ranges) {
+                                          int x, const int* staged, SplitRange* ranges) {
     const int lane = threadIdx.x & (kWave - 1);
-    const Sequence mine(p, seq, lane, B, max_tokens);
-    const int q0 = mine.quanta();
-    long long total = wave_sum(q0);
-    for (int b0 = kWave; b0 < B; b0 += kWave)
-        total += wave_sum(Sequence(p, seq, b0 + lane, B, max_tokens).quanta());
+    Sequence mine{-1, 0};
+    if (staged == nullptr) mine = sequence_of(p, seq, lane, B, max_tokens);
+    auto tokens_at = [&](int b0) -> int {
+        if (staged != nullptr) return b0 + lane < B ? staged[b0 + lane] : 0;
+        return b0 == 0 ? mine.tokens : sequence_of(p, seq, b0 + lane, B, max_tokens).tokens;
+    };
+    // sums over the lanes' shares: up to 2^23 quanta each, any number of sequences
+    long long total = 0;
+    for (int b0 = 0; b0 < B; b0 += kWave) total += wave_sum(quanta_of(tokens_at(b0)));
     // no sequence has more than kMostQuanta
     int per = total < kMostQuanta ? max(1, splits_of((int)total, share))
                                   : (int)min((total + share - 1) / share, (long long)kMostQuanta);
-    for (int tries = 0; tries < kSplitTries; ++tries) {
-        int splits = wave_sum(splits_of(q0, per));
-        for (int b0 = kWave; b0 < B; b0 += kWave)
-            splits += wave_sum(splits_of(Sequence(p, seq, b0 + lane, B, max_tokens).quanta(), per));
-        if (splits <= share) break;
-        per = (int)min(per + max(1LL, (long long)splits_of(per, share) * (splits - share)), (long long)kMostQuanta);
-    }
     Work w{-1, -1, 0, 0, {0, 0}};
     int before = 0;
     for (int b0 = 0; b0 < B; b0 += kWave) {
-        Sequence s = mine;
-        if (b0 > 0) s = Sequence(p, seq, b0 + lane, B, max_tokens);
-        const int n = splits_of(s.quanta(), per), inc = wave_scan(n);
+        const int tokens = tokens_at(b0);
+        const int n = splits_of(quanta_of(tokens), per), inc = wave_scan(n);
         const int first = before + inc - n;
         if (ranges != nullptr && b0 + lane < B) ranges[b0 + lane] = SplitRange{first, n};
         const uint64_t mask = __builtin_amdgcn_ballot_w64(x >= first && x < first + n);
         if (mask != 0) {
             const int at = __builtin_ctzll(mask);
             w.b = b0 + at;
-            w.slot = __builtin_amdgcn_readlane(s.slot, at);
+            w.slot = b0 == 0 && staged == nullptr ? __builtin_amdgcn_readlane(mine.slot, at)
+                                                  : __builtin_amdgcn_readfirstlane(slot_of(seq, w.b, p.S));
             w.range.first = __builtin_amdgcn_readlane(first, at);
             w.range.count = __builtin_amdgcn_readlane(n, at);
-            const int tokens = __builtin_amdgcn_readlane(s.tokens, at);
             w.k0 = (x - w.range.first) * per * kDecodeQuantum;
-            w.k1 = (int)min((long long)tokens, w.k0 + (long long)per * kDecodeQuantum);
+            w.k1 = (int)min((long long)__builtin_amdgcn_readlane(tokens, at),
+                            w.k0 + (long long)per * kDecodeQuantum);
             if (ranges == nullptr) return w;
         }
         before += __builtin_amdgcn_readlane(inc, kWave - 1);
@@ -349,7 +356,7 @@ struct Sums {
         float top = acc[0][0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) top = fmaxf(top, acc[i >> 2][i & 3]);
-        if (__builtin_amdgcn_ballot_w64(top * sl2 > m + 64.0f) != 0) {
+        if (__builtin_amdgcn_ballot_w64(top * sl2 > m + kRaise) != 0) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float mn = fmaxf(m, top * sl2);
@@ -467,12 +474,22 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
 
     Work work{x, -1, 0, 0, {x, 1}};
     if (whole) {
-        const Sequence s(p, seq, x, B, max_tokens);
+        const Sequence s = sequence_of(p, seq, x, B, max_tokens);
         work.slot = s.slot;
         work.k1 = s.tokens;
     } else {
+        // many sequences: their lengths are loaded once, by all waves (200 ragged ones of
+        // up to 4000 tokens, 8 KV heads: 86 us with every wave loading them, 74 so)
+        int* staged = nullptr;
+        if (B > kWave && B <= kStaged) {
+            static_assert(kStaged * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
+            staged = reinterpret_cast<int*>(s_ring);
+            for (int e = threadIdx.x; e < B; e += kThreads) staged[e] = sequence_of(p, seq, e, B, max_tokens).tokens;
+            __syncthreads();
+        }
         // the first workgroup's first wave leaves the ranges for the merge
-        work = find_work(p, seq, B, max_tokens, share, x, blockIdx.x == 0 && wv == 0 ? ranges : nullptr);
+        work = find_work(p, seq, B, max_tokens, share, x, staged, blockIdx.x == 0 && wv == 0 ? ranges : nullptr);
+        if (staged != nullptr) __syncthreads();  // the rings take the lengths' place
         if (work.b < 0) return;
     }
     const int b = work.b, slot = work.slot, k0 = work.k0, k1 = work.k1;

@@ -38,11 +38,11 @@ inline size_t pages_workspace(int n_pages, int n) {
 }
 
 // Plan of a decode over pages.  The lengths are on the device, so the splits are
-// cut there: in whole quanta of kDecodeQuantum tokens, equal for all sequences, the
-// fewest that make at most `share` splits (one round of resident workgroups over
-// all (layer, KV head) pairs) or, where one per sequence is more than that, at
-// most share + B.  The sequences' splits are numbered one after the other, and
-// workgroup x of each pair takes split x.
+// cut there: in whole quanta of kDecodeQuantum tokens, all of the same size, which
+// is a `share`-th of all sequences' quanta, `share` being one round of resident
+// workgroups over all (layer, KV head) pairs.  That makes at most share + B splits
+// (a sequence's last one may be short).  They are numbered one sequence after the
+// other, and workgroup x of each pair takes split x.
 struct PagesPlan {
     int pairs, G, groups;  // groups: workgroups per (layer, KV head)
     bool whole;            // one split per sequence: nothing to merge

@@ -442,6 +442,25 @@ def test_decode(K, Hkv, G, d, page, lengths, most, dtype, qs):
     report(f"paged decode worst err/bound g{G} d{d} {dtype} x{qs:g}", round(worst, 4))
 
 
+@pytest.mark.parametrize("G,d", [(1, 64), (4, 128), (8, 64), (16, 128)])
+def test_decode_of_large_values_under_rising_logits(K, G, d):
+    """Each token's logit is above the one before, by 90 in all, over values around 2^100: the unnormalised sums of a
+    reference that is never raised would leave float32."""
+    n = 500
+    pages, _, _ = _filled(K, 1, 1, d, 32, [n], seed=G)
+    k = torch.zeros((1, 1, 1, n, d))
+    k[..., 0] = torch.linspace(0.5, 6.0, n)
+    v = normal((1, 1, 1, n, d), "f32", 5, 2.0 ** 100)
+    K.pages_append(k.cuda(), v.cuda(), pages, dev([0]))
+    q = torch.zeros((1, 1, G, d))
+    q[..., 0] = 15.0 * np.sqrt(d)
+    q[..., 1:] = normal((1, 1, G, d - 1), "f32", 6)
+    out = K.decode_pages(q.bfloat16().cuda(), pages).double().cpu().numpy()
+    kk, vv = rows_of(pages, 0)
+    want, mag, top = _decode_ref(q.bfloat16().double().numpy()[0, 0], kk[0], vv[0], G)
+    check_decode(out[0, 0], want, mag, top)
+
+
 @pytest.mark.parametrize("L,B,Hkv,G,page,longest,most", [
     (1, 150, 1, 2, 32, 700, None),     # more sequences than a wave has lanes, several splits each
     (1, 64, 2, 4, 64, 200, 200),

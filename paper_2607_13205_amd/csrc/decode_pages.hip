@@ -449,8 +449,9 @@ struct Sums {
 // arithmetic.  The vector unit is busy for about half of that; it converts K and V
 // (64 instructions per 32 tokens), pairs V's tokens (36), splits the weights (32)
 // and takes 8 exponentials and multiply-adds.
-template <typename T, int D, int NH>
-__global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(const T* __restrict__ q, PagePool p,
+// NWV: waves per workgroup, kWaves, or as many as a compute unit holds.
+template <typename T, int D, int NH, int NWV>
+__global__ __launch_bounds__(NWV * kWave, (kPerSimd<T, D, NH>)) void pages_split(const T* __restrict__ q, PagePool p,
                                                                   const int32_t* __restrict__ seq, int B, int G,
                                                                   int max_tokens, int share, int groups, int whole,
                                                                   float sl2, float* __restrict__ ws_o,
@@ -461,8 +462,8 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
     using S = Slot<D>;
     // the waves' rings, and behind their last use the waves' sums
     constexpr int kRing = S::kSlots * S::kBytes, kSums = NH * D * (int)sizeof(float);
-    __shared__ __attribute__((aligned(16))) char s_ring[kWaves * (kRing > kSums ? kRing : kSums)];
-    __shared__ float s_ml[kWaves][2][NH];
+    __shared__ __attribute__((aligned(16))) char s_ring[NWV * (kRing > kSums ? kRing : kSums)];
+    __shared__ float s_ml[NWV][2][NH];
     float(*s_o)[NH][D] = reinterpret_cast<float(*)[NH][D]>(s_ring);
 
     const int pairs = p.L * p.Hkv;
@@ -484,7 +485,7 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
         if (B > kWave && B <= kStaged) {
             static_assert(kStaged * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
             staged = reinterpret_cast<int*>(s_ring);
-            for (int e = threadIdx.x; e < B; e += kThreads) staged[e] = sequence_of(p, seq, e, B, max_tokens).tokens;
+            for (int e = threadIdx.x; e < B; e += NWV * kWave) staged[e] = sequence_of(p, seq, e, B, max_tokens).tokens;
             __syncthreads();
         }
         // the first workgroup's first wave leaves the ranges for the merge
@@ -517,7 +518,7 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
         there = (there & ~(1u << at_slot)) | (uint32_t)ok << at_slot;
         S::load(page_block<D>(p, l, ok ? pg : 0, j), t & (page - 1), p.shift, ring + at_slot * S::kBytes);
     };
-    constexpr int kStride = kWaves * kBlk;
+    constexpr int kStride = NWV * kBlk;
     int t0 = k0 + wv * kBlk;
     sums.settle_queries();
 #pragma unroll
@@ -557,15 +558,15 @@ __global__ __launch_bounds__(kThreads, (kPerSimd<T, D, NH>)) void pages_split(co
     }
     __syncthreads();
     // merge the waves' partial results of this split
-    for (int e = threadIdx.x; e < G * D; e += kThreads) {
+    for (int e = threadIdx.x; e < G * D; e += NWV * kWave) {
         const int h = e / D, ch = e - h * D;
         float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, s_ml[w][0][h]);
+        for (int w = 0; w < NWV; ++w) mx = fmaxf(mx, s_ml[w][0][h]);
         float lt = 0.0f, ot = 0.0f;
         if (mx != -INFINITY) {
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < NWV; ++w) {
                 const float a = fast_exp2(s_ml[w][0][h] - mx);
                 lt = fmaf(a, s_ml[w][1][h], lt);
                 ot = fmaf(a, s_o[w][h][ch], ot);
@@ -609,9 +610,16 @@ hipError_t run_heads(const void* q, const PagePool& p, int B, int Hq, int max_to
     float* wo = static_cast<float*>(ws);
     float2* wml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.off_ml);
     SplitRange* ranges = reinterpret_cast<SplitRange*>(static_cast<char*>(ws) + plan.off_ranges);
-    hipLaunchKernelGGL((pages_split<T, D, NH>), dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads), 0, st,
-                       static_cast<const T*>(q), p, seq, B, plan.G, max_tokens, share, plan.groups,
-                       (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
+    if (plan.wide) {
+        constexpr int kWide = 4 * kPerSimd<T, D, NH>;
+        hipLaunchKernelGGL((pages_split<T, D, NH, kWide>), dim3((unsigned)plan.pairs * plan.groups),
+                           dim3(kWide * kWave), 0, st, static_cast<const T*>(q), p, seq, B, plan.G, max_tokens, share,
+                           plan.groups, (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
+    } else {
+        hipLaunchKernelGGL((pages_split<T, D, NH, kWaves>), dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads),
+                           0, st, static_cast<const T*>(q), p, seq, B, plan.G, max_tokens, share, plan.groups,
+                           (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
+    }
     // up to 16 splits: one wave per row; more: four, which cut the chain of loads in four
     const int rows = plan.pairs * B * plan.G;
     if (!plan.whole && share > 16)

@@ -419,6 +419,12 @@ DECODES = [  # Hkv, G, d, page, lengths, max_tokens, dtype, scale of the queries
     (1, 7, 128, 64, [900, 90], None, "f32", 40.0),
     (1, 2, 128, 64, [600], 350, "bf16", 1.0),           # fewer tokens than the sequence has
     (1, 4, 128, 32, [70000, 3], None, "bf16", 1.0),     # many splits
+    # a compute unit to a sequence: 16 or 12 waves, some without a step
+    (1, 4, 128, 32, [500, 31, 480, 0, 513 - 1], 512, "bf16", 1.0),
+    (1, 8, 64, 64, [511, 64, 65], 512, "bf16", 20.0),
+    (2, 3, 128, 64, [512, 100, 384, 385], 512, "f32", 1.0),
+    (1, 13, 128, 32, [512, 1, 200], 512, "bf16", 1.0),
+    (64, 2, 64, 128, [2000, 70, 0], 2048, "bf16", 1.0),
 ]
 
 

@@ -449,7 +449,7 @@ struct Sums {
 // arithmetic.  The vector unit is busy for about half of that; it converts K and V
 // (64 instructions per 32 tokens), pairs V's tokens (36), splits the weights (32)
 // and takes 8 exponentials and multiply-adds.
-// NWV: waves per workgroup, kWaves, or as many as a compute unit holds.
+// NWV: waves per workgroup, kWaves, or all or half that a compute unit holds.
 template <typename T, int D, int NH, int NWV>
 __global__ __launch_bounds__(NWV * kWave, (kPerSimd<T, D, NH>)) void pages_split(const T* __restrict__ q, PagePool p,
                                                                   const int32_t* __restrict__ seq, int B, int G,
@@ -610,16 +610,19 @@ hipError_t run_heads(const void* q, const PagePool& p, int B, int Hq, int max_to
     float* wo = static_cast<float*>(ws);
     float2* wml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.off_ml);
     SplitRange* ranges = reinterpret_cast<SplitRange*>(static_cast<char*>(ws) + plan.off_ranges);
-    if (plan.wide) {
-        constexpr int kWide = 4 * kPerSimd<T, D, NH>;
-        hipLaunchKernelGGL((pages_split<T, D, NH, kWide>), dim3((unsigned)plan.pairs * plan.groups),
-                           dim3(kWide * kWave), 0, st, static_cast<const T*>(q), p, seq, B, plan.G, max_tokens, share,
-                           plan.groups, (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
-    } else {
-        hipLaunchKernelGGL((pages_split<T, D, NH, kWaves>), dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads),
+    auto launch = [&](auto waves) {
+        constexpr int NWV = decltype(waves)::value;
+        hipLaunchKernelGGL((pages_split<T, D, NH, NWV>), dim3((unsigned)plan.pairs * plan.groups), dim3(NWV * kWave),
                            0, st, static_cast<const T*>(q), p, seq, B, plan.G, max_tokens, share, plan.groups,
                            (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
-    }
+    };
+    constexpr int kAll = 4 * kPerSimd<T, D, NH>;  // waves of a compute unit
+    if (plan.per_unit == 1)
+        launch(std::integral_constant<int, kAll>{});
+    else if (plan.per_unit == 2)
+        launch(std::integral_constant<int, kAll / 2>{});
+    else
+        launch(std::integral_constant<int, kWaves>{});
     // up to 16 splits: one wave per row; more: four, which cut the chain of loads in four
     const int rows = plan.pairs * B * plan.G;
     if (!plan.whole && share > 16)

@@ -46,20 +46,18 @@ inline size_t pages_workspace(int n_pages, int n) {
 struct PagesPlan {
     int pairs, G, groups;  // groups: workgroups per (layer, KV head)
     bool whole;            // one split per sequence: nothing to merge
-    bool wide;             // of as many waves as a compute unit holds
+    int per_unit;          // workgroups that share a compute unit: 1, 2 or 4
     size_t off_ml, off_ranges, total;
 };
 
-// `whole`, one split per sequence with no search and no merge, where there are
-// enough sequences and none can be long (32 layers x 8 heads: 4 sequences of 1639
-// tokens 43.5 us so and 45.5 without the rule, 8 of 300 26 and 32, 8 of 1639 81 and
-// 86); longer ones may differ too much.
-// `wide`, the same with a compute unit to a sequence, where they are few: up to
-// one per unit, and no longer than the fewer they are (device time of a captured
-// call, 8 KV heads of 4 query heads, wide and split: 32 sequences of 1000 tokens
-// 11.8 and 17.2 us, of 2000 16.9 and 22.2, 16 of 2000 15.0 and 16.3, 4 of 500 8.5
-// and 9.1, but of 1639 12.5 and 10.4, one of 500 8.4 and 9.2, of 1000 10.3 and 9.0,
-// 100 of 500 32.2 and 20.1).
+// `whole`, one split per sequence with no search and no merge, where none can be
+// long (longer ones may differ too much) or long for their number; a workgroup
+// then has all waves of a compute unit, half of them or four, so that the
+// sequences fill the chip once.  Device time of a captured call, 8 KV heads of 4
+// query heads, so and split: 32 sequences of 1000 tokens 11.7 and 17.2 us, of 2000
+// 17 and 22.2, 64 of 1000 17 and 22.9, 100 of 500 16.2 and 20.2, 120 of 2000 49 and
+// 78, 16 of 2000 15.0 and 16.3, 4 of 500 8.5 and 9.1, but 4 of 1639 12.5 and 10.4,
+// one of 1000 10.3 and 9.0.
 constexpr int kPagesMostResident = 4 * kDecodeUnits;  // workgroups, at four per compute unit
 
 inline PagesPlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens, int d) {
@@ -67,11 +65,9 @@ inline PagesPlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens
     p.pairs = L * Hkv;
     p.G = Hq / Hkv;
     const long long quanta = ((long long)max_tokens + kDecodeQuantum - 1) / kDecodeQuantum;
-    p.whole = quanta == 1 || ((long long)p.pairs * B >= kPagesMostResident && quanta <= kDecodeLongest);
     const long long segs = (long long)p.pairs * B;
-    p.wide = !p.whole && segs <= kDecodeUnits && quanta <= kDecodeLongest &&
-             quanta <= (segs / 8 > 4 ? segs / 8 : 4);
-    p.whole = p.whole || p.wide;
+    p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > 4 ? segs / 8 : 4);
+    p.per_unit = !p.whole ? 4 : segs <= kDecodeUnits ? 1 : segs <= 2 * kDecodeUnits ? 2 : 4;
     const int share = p.pairs < kPagesMostResident ? kPagesMostResident / p.pairs : 1;
     long long groups = (long long)share + B;
     if (groups > B * quanta) groups = B * quanta;

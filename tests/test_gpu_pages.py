@@ -472,7 +472,10 @@ def test_decode_of_large_values_under_rising_logits(K, G, d):
     (1, 64, 2, 4, 64, 200, 200),
     (1, 65, 1, 1, 32, 1500, None),
     (130, 2, 8, 1, 64, 2300, None),    # more (layer, KV head) pairs than resident workgroups: one split per sequence
-    (40, 30, 1, 4, 128, 1100, 1100),   # a workgroup per sequence
+    (40, 30, 1, 4, 128, 1100, 1100),   # a workgroup per sequence, of four waves
+    (3, 50, 2, 4, 32, 500, 500),       # of eight
+    (2, 100, 1, 11, 64, 300, 320),     # of sixteen, G = 11
+    (5, 75, 1, 8, 32, 2000, 2048),
 ])
 def test_decode_of_many_sequences_and_pairs(K, L, B, Hkv, G, page, longest, most):
     """Ragged lengths with empty sequences among them, slots named twice and in any order."""

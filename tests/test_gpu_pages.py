@@ -267,6 +267,18 @@ def test_read_ranges(K, L, B, Hkv, N, d, page, cap, dtype):
     assert torch.equal(k3[:, 2, :, page:], k2[:, 0, :, page:])
 
 
+def test_read_of_keys_or_values_alone(K):
+    import ctypes
+    pages, _, _ = _filled(K, 2, 2, 64, 32, [70, 5])
+    k, v = K.pages_read(pages, 70)
+    for which, want in ((0, k), (1, v)):
+        out = torch.zeros_like(want)
+        at = [out.data_ptr() if i == which else None for i in (0, 1)]
+        assert K.binding.LIB.kve_pages_read(ctypes.byref(pages.c), 0, 2, 70, None, None, None, *at,
+                                            torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(out, want)
+
+
 @pytest.mark.parametrize("L,B,Hkv,N,d,page,cap,dtype", CASES)
 def test_select(K, L, B, Hkv, N, d, page, cap, dtype):
     r = np.random.default_rng(7 * N)

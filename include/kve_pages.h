@@ -230,7 +230,8 @@ size_t kve_decode_pages_workspace_size(int L, int B, int Hq, int Hkv, int max_to
  *   out[l, b, h] = sum_t softmax_t(scale * <q[l, b, h], k_t>) v_t,
  * k_t and v_t the rows of KV head h / (Hq/Hkv) as kve_pages_read gives them.  A
  * sequence with n = 0 gives zeros; rows whose page number is invalid are left out.
- * A NaN row makes the heads that read it NaN.
+ * A NaN row makes the heads that read it NaN.  Logits are float32: one that falls
+ * below its range has no weight.
  *
  *   q          [L, B, Hq, d] bf16 or fp32 (device), 16-byte aligned
  *   max_tokens a bound of the lengths that the caller knows (at most M * page):

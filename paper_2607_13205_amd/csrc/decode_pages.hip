@@ -47,6 +47,9 @@ constexpr int kStaged = 4096;  // most sequences whose lengths are kept in LDS f
 // A weight may grow to 2^kRaise before the reference is raised: rarely after the
 // first step, and far from where the value sums overflow.
 constexpr float kRaise = 16.0f;
+// The reference before any logit: finite, so that logits of minus infinity (products
+// that leave float32) have weights of zero under it, not NaN.
+constexpr float kLowest = -3.4028234663852886e38f;
 constexpr int kMostQuanta = (1 << 30) / kDecodeQuantum;  // of a sequence
 
 // One direct-to-LDS load of four bytes per lane, as lds_dma16.
@@ -290,7 +293,7 @@ struct Sums {
                 split3(y, q[s]);
             }
         }
-        m = -INFINITY;
+        m = kLowest;
         den = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < NC; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -360,7 +363,7 @@ struct Sums {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float mn = fmaxf(m, top * sl2);
-            const float alpha = mn == -INFINITY ? 1.0f : fast_exp2(m - mn);
+            const float alpha = fast_exp2(m - mn);
             m = mn;
             den *= alpha;
 #pragma unroll
@@ -439,7 +442,6 @@ struct Sums {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[i][r] += row_from<8>(o[i][r]);
         }
-        if (den[0] != den[0] && m == -INFINITY) m = 0.0f;  // every logit was NaN: the split is not empty
     }
 };
 
@@ -560,17 +562,15 @@ __global__ __launch_bounds__(NWV * kWave, (kPerSimd<T, D, NH>)) void pages_split
     // merge the waves' partial results of this split
     for (int e = threadIdx.x; e < G * D; e += NWV * kWave) {
         const int h = e / D, ch = e - h * D;
-        float mx = -INFINITY;
+        float mx = kLowest;
 #pragma unroll
         for (int w = 0; w < NWV; ++w) mx = fmaxf(mx, s_ml[w][0][h]);
         float lt = 0.0f, ot = 0.0f;
-        if (mx != -INFINITY) {
 #pragma unroll
-            for (int w = 0; w < NWV; ++w) {
-                const float a = fast_exp2(s_ml[w][0][h] - mx);
-                lt = fmaf(a, s_ml[w][1][h], lt);
-                ot = fmaf(a, s_o[w][h][ch], ot);
-            }
+        for (int w = 0; w < NWV; ++w) {
+            const float a = fast_exp2(s_ml[w][0][h] - mx);
+            lt = fmaf(a, s_ml[w][1][h], lt);
+            ot = fmaf(a, s_o[w][h][ch], ot);
         }
         if (work.range.count == 1) {  // the whole sequence: the result itself
             out[(row0 * G + h) * D + ch] = lt != 0.0f ? ot / lt : 0.0f;

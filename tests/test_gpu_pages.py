@@ -479,6 +479,25 @@ def test_decode_of_large_values_under_rising_logits(K, G, d):
     check_decode(out[0, 0], want, mag, top)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,d,n,drowned,most", [(1, 64, 150, 70, None), (4, 128, 150, 70, 150), (8, 64, 600, 520, None),
+                                                (16, 128, 3000, 2500, None), (3, 128, 40, 39, 40)])
+def test_decode_of_logits_below_float32(K, G, d, n, drowned, most, dtype):
+    """The first `drowned` logits are products that leave float32 downwards, all those of some waves and splits: they
+    have no weight, and the others, which are zero, share it."""
+    pages, _, _ = _filled(K, 1, 1, d, 32, [n], seed=G)
+    k = torch.zeros((1, 1, 1, n, d))
+    k[..., :drowned, 0] = -6.0
+    v = normal((1, 1, 1, n, d), "f32", 5)
+    K.pages_append(k.cuda(), v.cuda(), pages, dev([0]))
+    q = torch.zeros((1, 1, G, d))
+    q[..., 0] = 2.0 ** 127
+    out = K.decode_pages(q.to(TORCH[dtype]).cuda(), pages, max_tokens=most).double().cpu().numpy()
+    _, vv = rows_of(pages, 0)
+    rest = vv[0, 0, drowned:]
+    check_decode(out[0, 0], np.tile(rest.mean(0), (G, 1)), np.tile(np.abs(rest).mean(0), (G, 1)), 0.0)
+
+
 @pytest.mark.parametrize("L,B,Hkv,G,page,longest,most", [
     (1, 150, 1, 2, 32, 700, None),     # more sequences than a wave has lanes, several splits each
     (1, 64, 2, 4, 64, 200, 200),

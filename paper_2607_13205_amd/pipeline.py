@@ -282,6 +282,11 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
     overlapping the scoring of the next; the current stream waits for the side
     stream before returning."""
     import torch
+    if bufs.pages is None and slots is not None:
+        raise ValueError("slots are those of a paged cache: make the buffers with pages")
+    # the rows are looked at after the sequences have been extended
+    if bufs.pages is not None and (v is None or v.shape != k.shape or v.dtype is not k.dtype):
+        raise ValueError("pages hold keys and values: v must match k")
     policy = as_policy(policy)
     R = policy.R
     L = k.shape[0]

@@ -164,3 +164,21 @@ def test_python_checks(kve):
             kve.Pages(**dict(ok, **bad))
     with pytest.raises(ValueError, match="device"):
         kve.Pages(**ok)
+
+
+def test_evict_checks_what_goes_into_pages(kve):
+    """Refused before anything is queued: the sequences would be extended otherwise."""
+    import types
+
+    import torch
+    from paper_2607_13205_amd import pipeline
+    k = torch.zeros((1, 1, 1, 8, 64))
+
+    def evict(v, pages, **kw):
+        bufs = types.SimpleNamespace(pages=pages, hist=None)
+        pipeline.evict(None, k, v, None, None, None, 0.5, 4, 1, bufs, **kw)
+    for v in (None, k[:, :, :, :4], k.bfloat16()):
+        with pytest.raises(ValueError, match="v must match k"):
+            evict(v, object())
+    with pytest.raises(ValueError, match="slots"):
+        evict(k, None, slots=torch.zeros(1, dtype=torch.int32))

@@ -528,6 +528,29 @@ def test_decode_of_many_sequences_and_pairs(K, L, B, Hkv, G, page, longest, most
     assert torch.isfinite(out).all()
 
 
+def test_decode_of_thousands_of_samples(K):
+    """More samples than lengths are kept in LDS for, on few slots, some of them outside the cache, beside long ones."""
+    B, G, d = 4500, 2, 64
+    lengths = [2600, 1, 0, 33, 300, 64, 900]
+    pages, _, _ = _filled(K, 1, 1, d, 32, lengths)
+    r = np.random.default_rng(8)
+    order = r.integers(-1, len(lengths) + 1, B)
+    order[[0, 63, 64, B - 1]] = 0
+    q = normal((1, B, G, d), "bf16", 79).cuda()
+    out = torch.full((1, B, G, d), float("nan"), device="cuda")
+    K.decode_pages(q, pages, seq=dev(order), out=out)
+    rows = [rows_of(pages, s) for s in range(len(lengths))]
+    qn, on = q.double().cpu().numpy(), out.double().cpu().numpy()
+    assert np.isfinite(on).all()
+    for i in [0, 1, 62, 63, 64, 65, B - 2, B - 1, *r.integers(0, B, 150)]:
+        s = order[i]
+        if 0 <= s < len(lengths):
+            want, mag, top = _decode_ref(qn[0, i], rows[s][0][0], rows[s][1][0], G)
+            check_decode(on[0, i], want, mag, top, f"sample {i} slot {s}")
+        else:
+            assert not on[0, i].any()
+
+
 def test_decode_equals_decode_over_the_rows_read_back(K):
     """The same rows dense in bf16: decode_attention gives the same to float32 rounding."""
     lengths = [700, 64, 0, 333]

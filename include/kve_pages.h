@@ -180,7 +180,8 @@ kve_status_t kve_pages_append(const void* k, const kve_strides_t* k_strides, con
  *   k, v   [L, B, Hkv, N, d] (device, dtype), views as in kve.h
  *   idx    [L, B, Hkv, k_cap] int32 (device)
  *   count  [L, B, Hkv] int32 (device)
- *   others as for kve_pages_append; k_cap = 0 is a valid size
+ *   others as for kve_pages_append; k_cap = 0 is a valid size (nothing is launched;
+ *          k and v, where not NULL, are checked all the same)
  */
 kve_status_t kve_pages_compact(const void* k, const kve_strides_t* k_strides, const void* v,
                                const kve_strides_t* v_strides, kve_dtype_t dtype, int B, int N,

@@ -92,13 +92,14 @@ kve_status_t pack_common(const char* fn, const void* k, const kve_strides_t* k_s
     if ((st = check_rows(fn, pages, B, cap, seq, false)) != KVE_OK) return st;
     if (N < 0 || N > (1 << 30)) return fail(KVE_ERR_INVALID_ARG, "%s: invalid N=%d", fn, N);
     if (start == nullptr) return fail(KVE_ERR_INVALID_ARG, "%s: null start", fn);
-    if (cap == 0 || N == 0) return ok();
+    if (N == 0 || (cap == 0 && (k == nullptr || v == nullptr))) return ok();
     if (k == nullptr || v == nullptr) return fail(KVE_ERR_INVALID_ARG, "%s: null tensor pointer", fn);
     const int es = dtype == KVE_DTYPE_BF16 ? 2 : 4;
     kve::RowView kv, vv;
     if ((st = make_view(fn, "k", k, k_st, B, pages->Hkv, N, pages->d, es, &kv)) != KVE_OK) return st;
     if ((st = make_view(fn, "v", v, v_st, B, pages->Hkv, N, pages->d, es, &vv)) != KVE_OK) return st;
     if (misaligned16(k) || misaligned16(v)) return fail(KVE_ERR_INVALID_ARG, "%s: k or v not 16-byte aligned", fn);
+    if (cap == 0) return ok();  // nothing to do, but what would be refused with rows has been
     return from_hip(kve::launch_pages_pack(kv, vv, (int)dtype, pages->d, B, N, idx, count, cap, start, seq, p,
                                            static_cast<hipStream_t>(stream)),
                     fn);

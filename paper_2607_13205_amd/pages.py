@@ -212,6 +212,15 @@ def pages_compact(k, v, idx, count, pages: Pages, start, seq=None, stream=None):
                                     ctypes.byref(pages.c), _on(pages, stream)))
 
 
+def check_compact(k, v, idx, count, pages: Pages, start, seq=None):
+    """Raises what pages_compact would raise for these arguments; nothing is launched."""
+    pages_compact(k, v, idx[..., :0], count, pages, start, seq)
+    B, k_cap = k.shape[1], idx.shape[-1]
+    _ints(idx, (pages.c.L, B, pages.c.Hkv, k_cap), "idx", pages)
+    if pages.c.L * B * pages.c.Hkv * (k_cap // 64 + 1) >= 1 << 24:    # workgroups of 64 rows in one launch
+        raise ValueError("too many rows for one call")
+
+
 def pages_select(pages: Pages, src, idx, count, dst, start, stream=None):
     """A second eviction: rows idx[l, b, j, :count[l, b, j]] of the sequence in
     slot src[b] moved, unchanged, to positions start[b] on of slot dst[b]."""

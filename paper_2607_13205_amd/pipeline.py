@@ -122,6 +122,8 @@ def alloc_buffers(k, n_q_heads: int, W: int, R: int, k_cap: int, scorer: str = "
         raise ValueError("pages hold keys and values")
     if pages is not None and (pages.L, pages.Hkv, pages.d) != (L, Hkv, d):
         raise ValueError(f"pages are of L={pages.L}, Hkv={pages.Hkv}, d={pages.d}, the keys of {L}, {Hkv}, {d}")
+    if pages is not None and kp.pages_workspace_size(pages.c.n_pages, pages.c.S, B) == 0:
+        raise ValueError(f"{B} samples: more than a bookkeeping call takes")
     dense = pages is None
     if scorer == "snapkv":
         wsb = kb.snapkv_workspace_size(L, B, n_q_heads, Hkv, N, W, d)
@@ -192,6 +194,19 @@ def _score(q, k, bufs, scorer, pool_k, scale, page, l0, l1, stream=None, lse_win
         kb.quest_score(q, k, page, score=score, workspace=bufs.ws_score, stream=stream)
     else:
         kb.h2o_score(q, k, scale, score=score, workspace=bufs.ws_score, stream=stream)
+
+
+def _check_paged(q, k, v, lse_win, bufs, slots, per):
+    """Refuses a step into pages, in chunks of ``per`` layers, that a call behind
+    pages_extend would refuse: the sequences would be longer by rows never written."""
+    if v is None or v.shape != k.shape or v.dtype is not k.dtype:
+        raise ValueError("pages hold keys and values: v must match k")
+    L = k.shape[0]
+    if any(t is not None and t.shape[0] != L for t in (q, lse_win)) or bufs.pages.L != L or \
+            bufs.idx.shape[:3] != k.shape[:3]:
+        raise ValueError("q, k, lse_win, the pages and the buffers must be of the same layers and samples")
+    kp.check_compact(_part(k, 0, per), _part(v, 0, per), _part(bufs.idx, 0, per), _part(bufs.count, 0, per),
+                     bufs.pages if per == L else bufs.pages.layers(0, per), bufs.start, slots)
 
 
 def _compact(k, v, bufs, idx, count, l0, l1, slots, stream):
@@ -269,7 +284,8 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
     are packed behind the sequences in slots ``slots`` (int32 [B] on the device;
     None: sample b in slot b), from position bufs.start[b] on.  A sample that the
     cache has no room for keeps nothing: its start is -1, and bufs.missing, on
-    the device like start, tells how many pages were lacking.
+    the device like start, tells how many pages were lacking.  Arguments that the
+    compaction would refuse are refused before anything is queued.
 
     The score does not depend on the quotas: it is queued first, and the host
     works the quotas out from the labels and queues their upload while the
@@ -284,15 +300,16 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
     import torch
     if bufs.pages is None and slots is not None:
         raise ValueError("slots are those of a paged cache: make the buffers with pages")
-    # the rows are looked at after the sequences have been extended
-    if bufs.pages is not None and (v is None or v.shape != k.shape or v.dtype is not k.dtype):
-        raise ValueError("pages hold keys and values: v must match k")
+    L = k.shape[0]
+    chunked = chunks > 1 and side_stream is not None
+    per = (L + chunks - 1) // chunks if chunked else L    # layers of a chunk
+    if bufs.pages is not None:
+        _check_paged(q, k, v, lse_win, bufs, slots, per)
     policy = as_policy(policy)
     R = policy.R
-    L = k.shape[0]
     main = torch.cuda.current_stream()
     fused = _fused(bufs, scorer, lse_win)
-    if chunks <= 1 or side_stream is None:
+    if not chunked:
         if score_events is not None:
             score_events[0].record(main)
         _score(q, k, bufs, scorer, pool_k, scale, page, 0, L, stream=main, lse_win=lse_win, roles_dev=roles_dev,
@@ -304,7 +321,6 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
         return quota, kept
     quota, kept = _upload_quotas(policy, roles_host, budget, W, bufs, main)
     side_stream.wait_stream(main)         # the quota upload and earlier work
-    per = (L + chunks - 1) // chunks
     if score_events is not None:
         score_events[0].record(main)
     for l0 in range(0, L, per):

@@ -903,3 +903,57 @@ def test_a_sequence_from_prompt_to_end(K):
     step([3], 8, [two[1]])
     K.pages_free(cache)
     assert not cache.refs.any() and not cache.length.any()
+
+
+def _bad_values(v):
+    """Tensors of v's shape and type that cannot be packed: name -> tensor."""
+    off = torch.empty(v.numel() + 8, dtype=v.dtype, device="cuda")[1:v.numel() + 1].view(v.shape)
+    odd = torch.empty(v.shape[:-1] + (v.shape[-1] + 1,), dtype=v.dtype, device="cuda")[..., :-1]
+    apart = torch.empty(v.shape[:-1] + (2 * v.shape[-1],), dtype=v.dtype, device="cuda")[..., ::2]
+    far = torch.empty(v.shape, dtype=v.dtype, device="cuda").permute(4, 0, 1, 2, 3).contiguous().permute(1, 2, 3, 4, 0)
+    return dict(unaligned=off, odd_rows=odd, channels_apart=apart, channels_outermost=far, on_the_host=v.cpu())
+
+
+@pytest.mark.parametrize("chunks", [1, 2])
+def test_a_refused_evict_leaves_the_sequences_alone(K, chunks):
+    """Whatever is wrong with the values, the slots or the layers: nothing is queued, and no sequence is longer."""
+    from paper_2607_13205_amd import pipeline
+    WL, wl, inp = _workload("paged_refused")
+    alpha = WL.default_alpha(0.0)
+    k_cap = K.role_allocate(inp["roles"], 4, alpha, 0.2, wl.W)[2]
+    cache = pipeline.alloc_pages(wl.L, wl.Hkv, wl.d, 40, 5, 2 * k_cap, page=32)
+    bufs = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, k_cap, pages=cache)
+    side = torch.cuda.Stream() if chunks > 1 else None
+    bufs.score.fill_(7.0)
+    slots = dev([3, 1])
+
+    def refused(q=inp["q"], v=inp["v"], slots=slots, bufs=bufs, **kw):
+        with pytest.raises((ValueError, K.KveError)):
+            pipeline.evict(q, inp["k"], v, inp["roles"], inp["roles_t"], alpha, 0.2, wl.W, wl.pool_k, bufs,
+                           chunks=chunks, side_stream=side, slots=slots, **kw)
+        torch.cuda.synchronize()
+        assert not cache.length.any() and not cache.held.any() and not cache.refs.any(), "the sequences were extended"
+        assert (bufs.score == 7.0).all(), "the score was queued"
+
+    for bad in _bad_values(inp["v"]).values():
+        refused(v=bad)
+    for bad in (slots.long(), dev([3]), slots.cpu(), dev([3, 9, 1, 9])[::2]):
+        refused(slots=bad)
+    refused(q=inp["q"][:2].contiguous())                             # the layers of a first chunk, and no more
+    refused(lse_win=torch.zeros((2, wl.B, wl.Hq, wl.W), device="cuda"))
+    one = pipeline.alloc_pages(wl.L, wl.Hkv, wl.d, 40, 1, 2 * k_cap, page=32)
+    few = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, k_cap, pages=one)
+    few.score.fill_(7.0)
+    refused(slots=None, bufs=few)                                    # two samples, one slot
+    assert not one.length.any()
+    pipeline.evict(inp["q"], inp["k"], inp["v"], inp["roles"], inp["roles_t"], alpha, 0.2, wl.W, wl.pool_k, bufs,
+                   chunks=chunks, side_stream=side, slots=slots)     # and the step itself still runs
+    assert (cache.length[slots.long()] > 0).all()
+
+
+def test_more_samples_than_a_bookkeeping_call_takes(K):
+    from paper_2607_13205_amd import pipeline
+    cache = pipeline.alloc_pages(1, 1, 64, 8, 1100, 64)
+    with pytest.raises(ValueError, match="1025"):
+        pipeline.alloc_buffers(torch.zeros((1, 1025, 1, 16, 64), dtype=torch.bfloat16, device="cuda"), 1, 4, 1, 8,
+                               pages=cache)

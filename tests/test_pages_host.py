@@ -182,3 +182,44 @@ def test_evict_checks_what_goes_into_pages(kve):
             evict(v, object())
     with pytest.raises(ValueError, match="slots"):
         evict(k, None, slots=torch.zeros(1, dtype=torch.int32))
+
+
+def test_compact_of_no_rows_checks_the_views(kve):
+    """k_cap = 0 launches nothing, but what a call with rows would refuse is refused."""
+    call = _calls(kve, _cache(kve))["compact"]
+    dense = dict(layer=5 * 128 * 4, batch=5 * 128 * 2, head=5 * 128, token=128)
+    for bad in (dict(token=132), dict(head=4), dict(layer=1 << 41), dict(token=1 << 25)):
+        st = kve.Strides(**dict(dense, **bad))
+        for which in ("ks", "vs"):
+            _refused(kve, 1, call, cap=0, idx=0, **{which: ctypes.byref(st)})
+    _refused(kve, 1, call, cap=0, idx=0, v=P + 2)
+    _refused(kve, 1, call, cap=0, idx=0, k=P + 8)
+    assert call(cap=0, idx=0, k=0, v=0) == 0
+
+
+def test_evict_checks_before_it_queues(kve, monkeypatch):
+    """Whatever the compaction into pages would refuse is refused before the score is queued."""
+    import types
+
+    import torch
+    from paper_2607_13205_amd import pipeline
+    k = torch.zeros((2, 1, 1, 8, 64))
+    z = torch.zeros(1, dtype=torch.int32)
+    queued, refused = [], ValueError("slots of the wrong kind")
+    monkeypatch.setattr(pipeline, "_score", lambda *a, **kw: queued.append("score"))
+    monkeypatch.setattr(pipeline, "_upload_quotas", lambda *a, **kw: queued.append("quotas"))
+
+    def refuse(*a, **kw):
+        raise refused
+    monkeypatch.setattr(pipeline.kp, "check_compact", refuse)
+    bufs = types.SimpleNamespace(pages=types.SimpleNamespace(L=2), hist=None, start=z, k_cap=3,
+                                 idx=torch.zeros((2, 1, 1, 3), dtype=torch.int32),
+                                 count=torch.zeros((2, 1, 1), dtype=torch.int32))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: None)
+    with pytest.raises(ValueError, match="wrong kind"):
+        pipeline.evict(k, k, k, None, None, pipeline.Policy.role((1.0,)), 0.5, 4, 1, bufs, slots=z)
+    with pytest.raises(ValueError, match="layers"):
+        pipeline.evict(k[:1], k, k, None, None, pipeline.Policy.role((1.0,)), 0.5, 4, 1, bufs, slots=z)
+    with pytest.raises(ValueError, match="layers"):
+        pipeline.evict(k, k, k, None, None, pipeline.Policy.role((1.0,)), 0.5, 4, 1, bufs, slots=z, lse_win=k[:1])
+    assert not queued

@@ -222,7 +222,8 @@ kve_status_t kve_pages_read(const kve_pages_t* pages, kve_dtype_t dtype, int B, 
                             const int32_t* start, const int32_t* count, void* k_out, void* v_out,
                             void* stream);
 
-/* Workspace bytes kve_decode_pages needs for these shapes (0 if invalid). */
+/* Workspace bytes that suffice for kve_decode_pages with these shapes, and with
+ * fewer layers, samples, query heads or tokens (0 if invalid). */
 size_t kve_decode_pages_workspace_size(int L, int B, int Hq, int Hkv, int max_tokens, int d);
 
 /*

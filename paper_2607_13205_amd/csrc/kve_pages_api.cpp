@@ -214,7 +214,7 @@ kve_status_t kve_pages_read(const kve_pages_t* pages, kve_dtype_t dtype, int B, 
 size_t kve_decode_pages_workspace_size(int L, int B, int Hq, int Hkv, int max_tokens, int d) {
     if (L <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || max_tokens <= 0 || Hq % Hkv != 0) return 0;
     if ((d != 64 && d != 128) || (double)L * B * Hq > (double)kMaxGroups || max_tokens > (1 << 30)) return 0;
-    return kve::decode_pages_plan(L, B, Hq, Hkv, max_tokens, d).total;
+    return kve::decode_pages_size(L, B, Hq, Hkv, max_tokens, d);
 }
 
 kve_status_t kve_decode_pages(const void* q, kve_dtype_t dtype, const kve_pages_t* pages, int B, int Hq,

@@ -59,6 +59,14 @@ struct PagesPlan {
 // 78, 16 of 2000 15.0 and 16.3, 4 of 500 8.5 and 9.1, but 4 of 1639 12.5 and 10.4,
 // one of 1000 10.3 and 9.0.
 constexpr int kPagesMostResident = 4 * kDecodeUnits;  // workgroups, at four per compute unit
+constexpr int kPagesWhole = 4;                        // quanta up to which every sequence is one split
+
+// Workspace of a decode whose splits leave `parts` partial results.
+inline size_t decode_pages_bytes(size_t parts, int B, int d, PagesPlan* p) {
+    p->off_ml = align_up(parts * d * sizeof(float));
+    p->off_ranges = p->off_ml + align_up(parts * 2 * sizeof(float));
+    return p->off_ranges + align_up((size_t)B * 2 * sizeof(int32_t));  // every sequence's first split and count
+}
 
 inline PagesPlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens, int d) {
     PagesPlan p{};
@@ -66,18 +74,31 @@ inline PagesPlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens
     p.G = Hq / Hkv;
     const long long quanta = ((long long)max_tokens + kDecodeQuantum - 1) / kDecodeQuantum;
     const long long segs = (long long)p.pairs * B;
-    p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > 4 ? segs / 8 : 4);
+    p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > kPagesWhole ? segs / 8 : kPagesWhole);
     p.per_unit = !p.whole ? 4 : segs <= kDecodeUnits ? 1 : segs <= 2 * kDecodeUnits ? 2 : 4;
     const int share = p.pairs < kPagesMostResident ? kPagesMostResident / p.pairs : 1;
     long long groups = (long long)share + B;
     if (groups > B * quanta) groups = B * quanta;
     if (p.whole) groups = B;
     p.groups = (int)groups;
-    const size_t parts = p.whole ? 0 : (size_t)p.pairs * p.groups * p.G;
-    p.off_ml = align_up(parts * d * sizeof(float));
-    p.off_ranges = p.off_ml + align_up(parts * 2 * sizeof(float));
-    p.total = p.off_ranges + align_up((size_t)B * 2 * sizeof(int32_t));  // every sequence's first split and count
+    p.total = decode_pages_bytes(p.whole ? 0 : (size_t)p.pairs * p.groups * p.G, B, d, &p);
     return p;
+}
+
+// Workspace that suffices for this call and for every one of no more layers,
+// samples, query heads and tokens, whose sequences may be split where this call's
+// are not: the splits, at most share + B, of the largest call that has any.
+inline size_t decode_pages_size(int L, int B, int Hq, int Hkv, int max_tokens, int d) {
+    const long long quanta = ((long long)max_tokens + kDecodeQuantum - 1) / kDecodeQuantum;
+    long long pairs = (long long)L * Hkv, segs = pairs * B;
+    if (quanta <= kPagesWhole)
+        segs = 0;
+    else if (quanta <= kDecodeLongest && segs > 8 * quanta - 1)
+        segs = 8 * quanta - 1;  // more are whole
+    if (pairs > segs) pairs = segs;
+    const long long most = (pairs > kPagesMostResident ? pairs : kPagesMostResident) + segs;
+    PagesPlan p{};
+    return decode_pages_bytes((size_t)(most < segs * quanta ? most : segs * quanta) * (Hq / Hkv), B, d, &p);
 }
 
 }  // namespace kve

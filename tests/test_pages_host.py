@@ -223,3 +223,41 @@ def test_evict_checks_before_it_queues(kve, monkeypatch):
     with pytest.raises(ValueError, match="layers"):
         pipeline.evict(k, k, k, None, None, pipeline.Policy.role((1.0,)), 0.5, 4, 1, bufs, slots=z, lse_win=k[:1])
     assert not queued
+
+
+def test_decode_workspace_serves_smaller_calls(kve):
+    """One made for the largest batch, stack and bound serves what is left of them: the size never falls with L, B, Hq
+    or max_tokens."""
+    size = kve.decode_pages_workspace_size
+    assert size(1, 16, 32, 8, 2048, 128) >= size(1, 15, 32, 8, 2048, 128)
+    assert size(32, 4, 32, 8, 1639, 128) >= size(1, 4, 32, 8, 1639, 128)
+    Ls, Bs = (1, 2, 3, 5, 16, 31, 32, 33, 80, 129), (1, 2, 4, 15, 16, 17, 64, 100, 500)
+    tokens = (1, 128, 129, 512, 513, 1000, 1639, 2047, 2048, 2049, 5000, 1 << 17, 1 << 24)
+    for Hkv in (1, 3, 8):
+        for d in (64, 128):
+            for Hq in (Hkv, 4 * Hkv):
+                table = [[[size(L, B, Hq, Hkv, n, d) for n in tokens] for B in Bs] for L in Ls]
+                for a in range(len(Ls)):
+                    for b in range(len(Bs)):
+                        for c in range(len(tokens)):
+                            here = table[a][b][c]
+                            assert here > 0 and here <= size(Ls[a], Bs[b], 2 * Hq, Hkv, tokens[c], d)
+                            for at in ((a - 1, b, c), (a, b - 1, c), (a, b, c - 1)):
+                                if min(at) >= 0:
+                                    assert table[at[0]][at[1]][at[2]] <= here, (Ls[a], Bs[b], Hkv, tokens[c], at)
+    # short sequences need next to nothing however many they are, ordinary ones some megabytes
+    assert size(32, 1000, 32, 8, 512, 128) <= 1 << 14
+    assert size(32, 64, 32, 8, 2048, 128) <= 4 << 20
+
+
+def test_decode_takes_the_workspace_of_a_larger_call(kve):
+    """Refusals come before anything is launched: with the size of a larger call the next check is reached."""
+    size = kve.decode_pages_workspace_size
+    call = _calls(kve, _cache(kve, L=1, Hkv=8, S=64, M=64))["decode"]
+    for B, most, Bs in ((16, 2048, (1, 4, 15, 16)), (64, 1639, (1, 7, 30)), (200, 700, (1, 3, 6))):
+        have = size(1, B, 32, 8, most, 128)
+        for b in Bs:
+            _refused(kve, 1, call, B=b, Hq=32, most=most, wsb=have, ws=P + 16)      # not 3: the size suffices
+            assert "aligned" in kve.last_error()
+            _refused(kve, 1, call, B=b, Hq=32, most=most // 2, wsb=have, ws=P + 16)
+            assert "aligned" in kve.last_error()

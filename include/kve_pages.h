@@ -120,8 +120,10 @@ kve_status_t kve_pages_extend(const kve_pages_t* pages, const int32_t* seq, cons
 /*
  * Makes slot dst[i] a continuation of the sequence in slot src[i], i < n: the
  * full pages are shared, the rows of a partial last page are copied to a fresh
- * page, and pages that the source holds beyond its length are not passed on.  A
- * source may be named any number of times.
+ * page, and pages that the source holds beyond its length are not passed on.
+ * Page numbers outside [0, n_pages) are passed on as they are: rows that the
+ * source lacks are missing from the continuation too.  A source may be named any
+ * number of times.
  *
  * Entries are taken in order, the sources as they were before the call.  One
  * is refused, and its slot left as it is, when src or dst is outside [0, S),

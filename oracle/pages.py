@@ -147,7 +147,8 @@ class PageBook:
                 done.append(0)
                 continue
             full, rest = divmod(int(length0[a]), self.page)
-            need = 1 if rest else 0
+            last = int(table0[a, full]) if rest else -1
+            need = 1 if 0 <= last < self.n_pages else 0      # a page that is not there is passed on as such
             got = self._take(free, left, need)
             left -= need
             total += need
@@ -156,12 +157,14 @@ class PageBook:
                 continue
             for i in range(full):
                 self.table[b, i] = table0[a, i]
-                self.refs[table0[a, i]] += 1
+                if 0 <= table0[a, i] < self.n_pages:
+                    self.refs[table0[a, i]] += 1
             if rest:
-                self.table[b, full] = got[0]
+                self.table[b, full] = got[0] if need else last
+            if need:
                 self.refs[got[0]] = 1
-                copies.append((int(table0[a, full]), got[0], rest))
-            self.held[b], self.length[b] = full + need, length0[a]
+                copies.append((last, got[0], rest))
+            self.held[b], self.length[b] = full + (rest > 0), length0[a]
             done.append(1)
         return done, max(0, total - F), copies
 
@@ -169,5 +172,6 @@ class PageBook:
         for slot in seq:
             if 0 <= slot < self.S:
                 for i in range(self.held[slot]):
-                    self.refs[self.table[slot, i]] -= 1
+                    if 0 <= self.table[slot, i] < self.n_pages:
+                        self.refs[self.table[slot, i]] -= 1
                 self.held[slot] = self.length[slot] = 0

@@ -516,7 +516,9 @@ __global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagePool p, const in
     const bool valid = free && !named_before(s_dst, i, to);
     if (!valid) len = 0;
     const int full = len >> p.shift, rows = len & ((1 << p.shift) - 1);
-    const uint32_t need = rows != 0 ? 1u : 0u;
+    const int last = rows != 0 ? p.table[(size_t)from * p.M + full] : -1;
+    // a last page that is not there is passed on as such: a fresh one would hold another's rows
+    const uint32_t need = last >= 0 && last < p.n_pages ? 1u : 0u;
     uint32_t total;
     const uint32_t off = scan_exclusive(need, s_scan, total);
     // all sources are read (the scan's barrier); destinations may be written
@@ -526,12 +528,12 @@ __global__ __launch_bounds__(kPlanThreads) void fork_kernel(PagePool p, const in
         ForkPlan f{given ? full : -1, -1, -1, rows, from, to, {0, 0}};
         if (given) {
             if (need != 0) {
-                f.from = p.table[(size_t)from * p.M + full];
+                f.from = last;
                 f.to = list[off];
-                p.table[(size_t)to * p.M + full] = f.to;
                 p.refs[f.to] = 1;
             }
-            p.held[to] = full + need;
+            if (rows != 0) p.table[(size_t)to * p.M + full] = need != 0 ? f.to : last;
+            p.held[to] = full + (rows != 0);
             p.length[to] = len;
         }
         plan[i] = f;
@@ -558,7 +560,7 @@ __global__ __launch_bounds__(kThreads) void fork_copy(PagePool p, const ForkPlan
         }
         return;
     }
-    if (f.to < 0 || f.from < 0 || f.from >= p.n_pages) return;
+    if (f.to < 0) return;
     const int l = (part - 1) / nblk, blk = (part - 1) % nblk;
     const int page = 1 << p.shift;
     const int bytes = (D / 16 * 17) << p.shift;

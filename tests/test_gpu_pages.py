@@ -957,3 +957,35 @@ def test_more_samples_than_a_bookkeeping_call_takes(K):
     with pytest.raises(ValueError, match="1025"):
         pipeline.alloc_buffers(torch.zeros((1, 1025, 1, 16, 64), dtype=torch.bfloat16, device="cuda"), 1, 4, 1, 8,
                                pages=cache)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [-1, "n_pages", 1 << 30, -(1 << 31)])
+def test_fork_of_a_sequence_whose_last_page_is_missing(K, d, bad):
+    """The child has the rows that the parent has, and not what a recycled page held: read, attended to, extended and
+    freed like the parent."""
+    page = 32
+    pages, k, v = _filled(K, 2, 2, d, page, [75, 40], extra_slots=2, spare=4)
+    bad = pages.c.n_pages if bad == "n_pages" else bad
+    pages.table[0, 2] = bad
+    b = book(pages)
+    done, missing = K.pages_fork(pages, dev([0, 1]), dev([2, 3]))
+    want, lack, _ = b.fork([0, 1], [2, 3])
+    assert done.tolist() == want == [1, 1] and missing.item() == lack == 0
+    same_book(pages, b)
+    outs = [torch.full((2, 4, 2, 75, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in (0, 1)]
+    K.pages_read(pages, 75, k_out=outs[0], v_out=outs[1])
+    for got in outs:
+        assert torch.equal(got[:, :2], got[:, 2:]) and (got[:, 2, :, 64:] == 7.0).all()
+        assert not (got[:, 3, :, :40] == 7.0).all(-1).any()
+    q = normal((2, 1, 4, d), "bf16", 3).expand(2, 4, 4, d).contiguous().cuda()
+    out = K.decode_pages(q, pages)
+    assert torch.equal(out[:, 2], out[:, 0]) and torch.equal(out[:, 3], out[:, 1])
+    before = pages.pool.clone()
+    start, missing = K.pages_extend(pages, dev([3]), seq=dev([2]))
+    K.pages_append(k[:, :1, :, :3], v[:, :1, :, :3], pages, start, seq=dev([2]))
+    assert start.tolist() == [75] and missing.item() == 0 and torch.equal(before, pages.pool)
+    K.pages_free(pages)
+    b.extend([2], [3])
+    b.free(range(4))
+    same_book(pages, b)

@@ -170,3 +170,18 @@ def test_bookkeeping_invariants(seed):
             for i, p in enumerate(mine):
                 assert b.refs[p] == 1 or (i + 1) * page <= b.length[s]
         assert np.array_equal(refs, b.refs)
+
+
+@pytest.mark.parametrize("bad", [-1, 10, 1 << 30, -(1 << 31)])
+def test_fork_passes_a_missing_last_page_on(bad):
+    """Rows that the parent does not have are none of the child's either: no fresh page stands for them."""
+    b = _book()
+    b.extend([0, 1], [75, 40])
+    b.table[0, 2] = bad
+    refs = b.refs.copy()
+    done, missing, copies = b.fork([0, 1], [2, 3])
+    assert (done, missing, copies) == ([1, 1], 0, [(4, 5, 8)])
+    assert b.table[2, :3].tolist() == [0, 1, bad] and b.held[2] == 3 and b.length[2] == 75
+    assert (b.refs - refs).tolist() == [1, 1, 0, 1, 0, 1, 0, 0, 0, 0]
+    b.free([0, 1, 2, 3])
+    assert b.refs.tolist() == [0, 0, 1, 0, 0, 0, 0, 0, 0, 0]          # the page that nobody names any more

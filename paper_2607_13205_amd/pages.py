@@ -40,7 +40,8 @@ class Pages:
       length  int32 [S]         its tokens
 
     An empty cache has refs, held and length all zero (pipeline.alloc_pages makes
-    one)."""
+    one).  part: the pool holds some of the layers that share the bookkeeping
+    (``layers``), and pages_fork does not take it."""
     pool: object
     refs: object
     table: object
@@ -48,6 +49,7 @@ class Pages:
     length: object
     page: int
     d: int
+    part: bool = False
     c: object = field(init=False, repr=False, compare=False)      # kve_pages_t
     index: int = field(init=False, repr=False, compare=False)     # the device's
 
@@ -82,8 +84,12 @@ class Pages:
         return self.c.Hkv
 
     def layers(self, l0: int, l1: int) -> "Pages":
-        """The rows of layers [l0, l1), with the same bookkeeping."""
-        return Pages(self.pool[l0:l1], self.refs, self.table, self.held, self.length, self.page, self.d)
+        """The rows of layers [l0, l1), with the same bookkeeping: a decode step takes
+        layer after layer.  What changes the bookkeeping is called once for all of
+        them; pages_fork, which copies rows too, takes all layers only."""
+        pool = self.pool[l0:l1]
+        return Pages(pool, self.refs, self.table, self.held, self.length, self.page, self.d,
+                     self.part or pool.shape[0] != self.L)
 
 
 def _on(pages: Pages, stream):
@@ -174,7 +180,10 @@ def pages_extend(pages: Pages, add, seq=None, start=None, missing=None, workspac
 
 def pages_fork(pages: Pages, src, dst, done=None, missing=None, workspace=None, stream=None):
     """Slot dst[i] becomes a continuation of the sequence in slot src[i].  Returns
-    (done, missing): 1 per entry, 0 where it was refused, and the pages lacking."""
+    (done, missing): 1 per entry, 0 where it was refused, and the pages lacking.
+    Takes all layers of the cache: the others would lack the rows that are copied."""
+    if pages.part:
+        raise ValueError("a fork takes all layers of the cache")
     n = src.numel()
     st = _on(pages, stream)
     done, missing, _ws, at = _book(pages, n, done, missing, "done", workspace, stream)

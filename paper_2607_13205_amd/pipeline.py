@@ -114,7 +114,9 @@ def alloc_buffers(k, n_q_heads: int, W: int, R: int, k_cap: int, scorer: str = "
     by default: on the 32-layer N = 32768 step the counting adds more to the
     pool (about 100 us) than it takes off the top-k (about 25 us).  pages: a
     Pages of as many layers that the steps pack the kept rows into (evict's
-    ``slots``); there is no dense output then."""
+    ``slots``); there is no dense output then.  A step lengthens its sequences in
+    all layers of the cache: where these are some of them (Pages.layers), the
+    others' rows are the caller's to pack, at bufs.start (pages_compact)."""
     import torch
     L, B, Hkv, N, d = k.shape
     dev = k.device

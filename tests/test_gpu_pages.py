@@ -989,3 +989,18 @@ def test_fork_of_a_sequence_whose_last_page_is_missing(K, d, bad):
     b.extend([2], [3])
     b.free(range(4))
     same_book(pages, b)
+
+
+def test_fork_takes_all_layers(K):
+    """The bookkeeping is every layer's: a fork of some of them would leave the others without the copied rows."""
+    pages, _, _ = _filled(K, 3, 1, 64, 32, [40], extra_slots=1)
+    before = [getattr(pages, n).clone() for n in ("refs", "held", "length")]
+    for part in (pages.layers(0, 2), pages.layers(1, 3), pages.layers(0, 2).layers(0, 2), pages.layers(2, 3)):
+        with pytest.raises(ValueError, match="all layers"):
+            K.pages_fork(part, dev([0]), dev([1]))
+    for x, n in zip(before, ("refs", "held", "length")):
+        assert torch.equal(x, getattr(pages, n))
+    done, _ = K.pages_fork(pages.layers(0, 3), dev([0]), dev([1]))
+    assert done.tolist() == [1]
+    for a, b in zip(rows_of(pages, 0), rows_of(pages, 1)):
+        assert np.array_equal(a, b)

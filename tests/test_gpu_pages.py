@@ -1004,3 +1004,220 @@ def test_fork_takes_all_layers(K):
     assert done.tolist() == [1]
     for a, b in zip(rows_of(pages, 0), rows_of(pages, 1)):
         assert np.array_equal(a, b)
+
+
+# ---------------------------------------------------------------------------
+# more forms of the calls
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_select_within_one_sequence(K, d):
+    """Source and destination are one slot: the rows kept are moved behind the others."""
+    n, cap = 90, 37
+    pages, k, v = _filled(K, 2, 2, d, 32, [n, n], spare=8)
+    pages2 = K.Pages(pages.pool, pages.refs, torch.cat([pages.table, torch.full_like(pages.table, -1)], 1).contiguous(),
+                     pages.held, pages.length, 32, d)
+    r = np.random.default_rng(d)
+    both = dev([0, 1])
+    start, missing = K.pages_extend(pages2, dev([cap, cap]), seq=both)
+    assert start.tolist() == [n, n] and missing.item() == 0
+    idx = np.stack([np.sort(r.permutation(n)[:cap]) for _ in range(8)]).reshape(2, 2, 2, cap)
+    K.pages_select(pages2, both, dev(idx), dev(np.full((2, 2, 2), cap)), both, start)
+    for s in (0, 1):
+        for got, x in zip(rows_of(pages2, s), (k, v)):
+            base = O.mx4_round(x[:, s].double().cpu().numpy())
+            assert np.array_equal(got[:, :, :n], base)
+            assert np.array_equal(got[:, :, n:], np.take_along_axis(base, idx[:, s, ..., None], axis=2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_keys_and_values_of_different_layouts(K, dtype, which):
+    """One dense, the other token-major with room between its rows."""
+    L, B, Hkv, N, d = 2, 2, 3, 70, 64
+    x = {n: normal((L, B, Hkv, N, d), dtype, i) for i, n in enumerate("kv")}
+    at = {n: t.cuda() for n, t in x.items()}
+    wide = torch.zeros((L, B, N, Hkv, d + 8), dtype=TORCH[dtype], device="cuda")
+    at[which] = wide.permute(0, 1, 3, 2, 4)[..., :d]
+    at[which].copy_(x[which])
+    pages = make(K, L, Hkv, d, 32, 16, B, 5)
+    start, _ = K.pages_extend(pages, dev([N, N]))
+    K.pages_append(at["k"], at["v"], pages, start)
+    want = {n: O.mx4_round(t.double().numpy()) for n, t in x.items()}
+    for s in range(B):
+        for got, n in zip(rows_of(pages, s), "kv"):
+            assert np.array_equal(got, want[n][:, s])
+    start, _ = K.pages_extend(pages, dev([4, 4]))
+    idx = dev(np.broadcast_to([69, 0, 33, 5], (L, B, Hkv, 4)))
+    K.pages_compact(at["k"], at["v"], idx, dev(np.full((L, B, Hkv), 4)), pages, start)
+    for s in range(B):
+        for got, n in zip(rows_of(pages, s), "kv"):
+            assert np.array_equal(got[:, :, N:], want[n][:, s][:, :, [69, 0, 33, 5]])
+
+
+@pytest.mark.parametrize("chunks", [1, 2])
+def test_evict_of_strided_values_into_pages(K, chunks):
+    """Token-major values beside dense keys: the rows of the dense step."""
+    from paper_2607_13205_amd import pipeline
+    WL, wl, inp = _workload("paged_views")
+    alpha = WL.default_alpha(0.0)
+    k_cap = K.role_allocate(inp["roles"], 4, alpha, 0.2, wl.W)[2]
+    v = inp["v"].permute(0, 1, 3, 2, 4).contiguous().permute(0, 1, 3, 2, 4)
+    assert not v.is_contiguous()
+    side = torch.cuda.Stream() if chunks > 1 else None
+    caches = []
+    for values in (inp["v"], v):
+        cache = pipeline.alloc_pages(wl.L, wl.Hkv, wl.d, 40, wl.B, k_cap, page=32)
+        bufs = pipeline.alloc_buffers(inp["k"], wl.Hq, wl.W, 4, k_cap, pages=cache)
+        pipeline.evict(inp["q"], inp["k"], values, inp["roles"], inp["roles_t"], alpha, 0.2, wl.W, wl.pool_k, bufs,
+                       chunks=chunks, side_stream=side)
+        caches.append(cache)
+    assert caches[0].length.tolist() == caches[1].length.tolist() and caches[0].length.min() > 0
+    for s in range(wl.B):
+        for a, b in zip(rows_of(caches[0], s), rows_of(caches[1], s)):
+            assert np.array_equal(a, b)
+
+
+# ---------------------------------------------------------------------------
+# more forms of the decode
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 8, 9, 16])
+def test_decode_keeps_all_bits_of_the_weights(K, G, d, dtype):
+    """Results that hang on the last 8 of the 24 bits of a weight, and of a float32 query: two tokens in one wave's step,
+    in the steps of two waves, within a split and in different ones."""
+    from tests import paged_decode_cases as C
+    worst = 0.0
+    for n, at, most in ((2, (0, 1), 2), (2, (1, 0), 512), (64, (3, 45), 64), (200, (67, 94), 200),
+                        (2300, (130, 147), 2304), (2300, (5, 2200), 2304), (2300, (2299, 0), None)):
+        q, k, v, want = C.case(G, d, dtype, n, at)
+        pages = make(K, 1, 1, d, 32, 80, 1, 80)
+        start, _ = K.pages_extend(pages, dev([n]))
+        k, v = (torch.from_numpy(x).float()[None, None, None].cuda() for x in (k, v))
+        K.pages_append(k, v, pages, start)
+        out = K.decode_pages(torch.from_numpy(q).to(TORCH[dtype])[None, None].cuda(), pages, max_tokens=most, scale=1.0)
+        worst = max(worst, float(np.abs(out[0, 0].double().cpu().numpy() - want).max()))
+        assert worst <= C.BOUND, (n, at, worst / C.U)
+    report(f"paged decode, low bits of the weights, units of 2^-24: g{G} d{d} {dtype}", round(worst / C.U, 2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,d,n,most", [(4, 128, 64, 64), (4, 64, 600, 600), (8, 128, 600, 600), (16, 128, 64, 64),
+                                        (3, 128, 2500, 2500)])
+def test_decode_of_exact_logits_is_float32(K, G, d, n, most, dtype):
+    """Small whole numbers as queries and four-bit values with unit scales: the products are exact, what is left is the
+    softmax and the sums in float32.  With logits of at most X (in powers of two), of a weight: log2(e) rounded X / 2,
+    reference, product and difference X + X + 2 X, times ln 2, exp2 2, a factor and its product in either merge 3 each:
+    3.2 X + 8 units of 2^-24.  Of a sum: 32 tokens and three parts per step of a wave, the waves of a split and the
+    splits added: 96 steps + 16 + 32.  Both twice, for numerator and denominator, and the division 5."""
+    r = np.random.default_rng(n + G)
+    q = r.integers(-3, 4, (2, G, d)).astype(np.float64)
+    k, v = (r.choice([-1.0, 1.0], (2, n, d)) * O.E2M1[r.integers(0, 8, (2, n, d))] for _ in "kv")
+    k[..., ::32], v[..., ::32] = 4.0, -6.0                           # every block's unit is one
+    assert np.array_equal(O.mx4_round(k), k) and np.array_equal(O.mx4_round(v), v)
+    pages = make(K, 1, 2, d, 64, -(-n // 64), 1, -(-n // 64))
+    start, _ = K.pages_extend(pages, dev([n]))
+    K.pages_append(*(torch.from_numpy(x).float()[None, None].cuda() for x in (k, v)), pages, start)
+    out = K.decode_pages(torch.from_numpy(q.reshape(1, 1, 2 * G, d)).to(TORCH[dtype]).cuda(), pages, max_tokens=most,
+                         scale=2.0 ** -6)
+    out = out[0, 0].double().cpu().numpy().reshape(2, G, d)
+    x = q @ k.transpose(0, 2, 1) / 64.0
+    w = np.exp(x - x.max(-1, keepdims=True))
+    w /= w.sum(-1, keepdims=True)
+    steps = -(-min(n, 128) // 128) if most > 2048 else -(-n // (32 * 12))    # a split, or all waves of a unit
+    units = 2 * (3.2 * np.abs(x).max() * 1.4427 + 8 + 96 * steps + 48) + 5
+    err = np.abs(out - w @ v) / (w @ np.abs(v))
+    assert err.max() <= units * 2.0 ** -24, (err.max() * 2.0 ** 24, units)
+    report(f"paged decode, exact logits, err/bound: g{G} d{d} n{n} {dtype}", round(float(err.max() * 2.0 ** 24 / units), 4))
+
+
+@pytest.mark.parametrize("L,B,Hkv,G,d,dtype,longest,most", [
+    (1, 3, 64, 4, 128, "bf16", 2300, 2304),   # 16 splits a pair: one wave per row merges them
+    (5, 2, 16, 2, 128, "bf16", 2200, None),   # 12
+    (1, 2, 64, 9, 128, "bf16", 2200, None),   # the same for sixteen heads
+    (1, 2, 64, 1, 128, "f32", 2300, 2300),
+    (1, 2, 64, 3, 64, "f32", 2300, 2300),
+    (2, 20, 8, 4, 128, "f32", 300, 512),      # two sequences to a compute unit, of six waves
+    (2, 20, 8, 11, 128, "bf16", 300, 512),
+    (2, 20, 8, 4, 128, "bf16", 300, 512),     # of eight
+    (2, 20, 8, 2, 64, "f32", 300, 512),
+    (3, 40, 8, 2, 128, "f32", 200, 200),      # four
+    (3, 40, 8, 12, 128, "f32", 200, 200),
+    (1, 70, 1, 16, 128, "f32", 1500, None),   # splits of more sequences than a wave has lanes
+])
+def test_decode_of_every_workgroup_form(K, L, B, Hkv, G, d, dtype, longest, most):
+    """Ragged lengths, empty sequences and slots in any order, for both row sizes and query types."""
+    r = np.random.default_rng(L * B + d)
+    lengths = [longest, 0] + [int(r.integers(0, longest + 1)) for _ in range(B - 2)]
+    page = 64
+    pages = make(K, L, Hkv, d, page, sum(-(-n // page) for n in lengths) + 1, B, 40)
+    start, missing = K.pages_extend(pages, dev(lengths))
+    assert missing.item() == 0
+    g = torch.Generator(device="cuda").manual_seed(B)
+    k, v = (torch.randn((L, B, Hkv, longest, d), generator=g, device="cuda", dtype=torch.float32).bfloat16()
+            for _ in "kv")
+    K.pages_append(k, v, pages, start, n_new=dev(lengths))
+    order = r.permutation(B)
+    q = normal((L, B, Hkv * G, d), dtype, 78).cuda()
+    out = torch.full((L, B, Hkv * G, d), float("nan"), device="cuda")
+    K.decode_pages(q, pages, max_tokens=most, seq=dev(order), out=out)
+    assert torch.isfinite(out).all()
+    k, v = K.pages_read(pages, longest, seq=dev(order))
+    for l in sorted({0, L - 1}):
+        qn, on = q[l].double().cpu().numpy(), out[l].double().cpu().numpy()
+        kl, vl = k[l].double().cpu().numpy(), v[l].double().cpu().numpy()
+        for i, s in enumerate(order):
+            n = lengths[s]
+            want, mag, top = _decode_ref(qn[i], kl[i, :, :n], vl[i, :, :n], G)
+            check_decode(on[i], want, mag, top, f"sample {i} of {n} layer {l}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_decode_of_several_splits(K, dtype):
+    """A captured step whose bound makes splits, replayed while lengths cross a split's and a page's border: the search,
+    the ranges left for the merge and the merge itself, against the eager loop."""
+    B, Hkv, G, d, page, M, steps = 3, 2, 4, 128, 512, 6, 14
+    lengths = [2040, 120, 1]
+    qs = normal((steps, 1, B, Hkv * G, d), dtype, 1).cuda()
+    ks, vs = (normal((steps, 1, B, Hkv, 1, d), "bf16", s).cuda() for s in (2, 3))
+
+    def fresh():
+        pages = make(K, 1, Hkv, d, page, 16, B, M, seed=2)
+        start, _ = K.pages_extend(pages, dev(lengths))
+        x = normal((2, 1, B, Hkv, max(lengths), d), "bf16", 4).cuda()
+        K.pages_append(x[0], x[1], pages, start, n_new=dev(lengths))
+        most = M * page
+        size = K.decode_pages_workspace_size(1, B, Hkv * G, Hkv, most, d)
+        return pages, dict(out=torch.zeros((1, B, Hkv * G, d), device="cuda"), start=dev([0] * B), missing=dev([0]),
+                           ws_book=torch.empty(K.pages_workspace_size(16, B, B), dtype=torch.uint8, device="cuda"),
+                           ws=torch.full((size,), 255, dtype=torch.uint8, device="cuda"), seq=dev([2, 0, 1]),
+                           one=dev([1] * B), most=most)
+
+    pages, bufs = fresh()
+    want = []
+    for i in range(steps):
+        _step(K, pages, ks[i], vs[i], qs[i], **bufs)
+        want.append(bufs["out"].clone())
+    assert pages.length.tolist() == [n + steps for n in lengths]
+    for s, i in ((0, 1), (1, 2), (2, 0)):
+        k, v = rows_of(pages, s)
+        ref, mag, top = _decode_ref(qs[-1][0, i].double().cpu().numpy(), k[0], v[0], G)
+        check_decode(want[-1][0, i].cpu().numpy(), ref, mag, top)
+
+    pages, bufs = fresh()
+    other, obufs = fresh()
+    q, k, v = qs[0].clone(), ks[0].clone(), vs[0].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        _step(K, pages, k, v, q, **bufs)
+    for i in range(steps):
+        q.copy_(qs[i]); k.copy_(ks[i]); v.copy_(vs[i])
+        graph.replay()
+        if i % 4 == 0:
+            _step(K, other, ks[i], vs[i], qs[i], **obufs)
+            torch.cuda.synchronize()
+        assert torch.equal(bufs["out"], want[i]), i

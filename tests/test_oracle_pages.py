@@ -185,3 +185,22 @@ def test_fork_passes_a_missing_last_page_on(bad):
     assert (b.refs - refs).tolist() == [1, 1, 0, 1, 0, 1, 0, 0, 0, 0]
     b.free([0, 1, 2, 3])
     assert b.refs.tolist() == [0, 0, 1, 0, 0, 0, 0, 0, 0, 0]          # the page that nobody names any more
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 8, 9, 16])
+def test_low_bits_cases_tell_a_lost_part(G, dtype):
+    """The paged decode's cases are held exactly, and losing the last 8 of a weight's or a float32 query's 24 bits
+    moves every head by more than twice their bound."""
+    from tests import paged_decode_cases as C
+    q, k, v, want = C.case(G, 64, dtype, 70, (3, 45))
+    assert np.array_equal(O.mx4_round(k), k) and np.array_equal(O.mx4_round(v), v)
+    assert np.array_equal(q, q.astype(np.float32)) and (dtype == "f32" or np.array_equal(q, C.trunc(q, 8)))
+    x = k @ q.T
+    w = np.exp(x - x.max(0))
+    assert np.allclose(want, (w / w.sum(0)).T @ v, rtol=0, atol=1e-14)
+    differ = v[3] != v[45]
+    assert differ.any()
+    for a, w in C.planted(q[:, 0], dtype):
+        off = np.abs(C.result(a, v[3], v[45], w) - want)
+        assert (off[:, differ] > 2 * C.BOUND).all()

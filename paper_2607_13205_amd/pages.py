@@ -208,26 +208,36 @@ def pages_append(k, v, pages: Pages, start, n_new=None, seq=None, stream=None):
                                    ctypes.byref(pages.c), _on(pages, stream)))
 
 
+def _compact_args(k, v, idx, count, pages, start, seq):
+    B, N, kp, ks, vp, vs, dt = _rows(k, v, pages)
+    shape = (pages.c.L, B, pages.c.Hkv)
+    k_cap = idx.shape[-1]
+    return (kp, ks, vp, vs, dt, B, N, _ints(idx, shape + (k_cap,), "idx", pages), _ints(count, shape, "count", pages),
+            k_cap, _ints(start, (B,), "start", pages), _ints(seq, (B,), "seq", pages, True), ctypes.byref(pages.c))
+
+
 def pages_compact(k, v, idx, count, pages: Pages, start, seq=None, stream=None):
     """kv_compact into pages: rows idx[l, b, j, :count[l, b, j]] of k, v
     [L, B, Hkv, N, d] packed into positions start[b] on of the sequence in slot
     seq[b]."""
-    B, N, kp, ks, vp, vs, dt = _rows(k, v, pages)
-    shape = (pages.c.L, B, pages.c.Hkv)
-    k_cap = idx.shape[-1]
-    kb._check(LIB.kve_pages_compact(kp, ks, vp, vs, dt, B, N, _ints(idx, shape + (k_cap,), "idx", pages),
-                                    _ints(count, shape, "count", pages), k_cap,
-                                    _ints(start, (B,), "start", pages), _ints(seq, (B,), "seq", pages, True),
-                                    ctypes.byref(pages.c), _on(pages, stream)))
+    kb._check(LIB.kve_pages_compact(*_compact_args(k, v, idx, count, pages, start, seq), _on(pages, stream)))
 
 
 def check_compact(k, v, idx, count, pages: Pages, start, seq=None):
-    """Raises what pages_compact would raise for these arguments; nothing is launched."""
-    pages_compact(k, v, idx[..., :0], count, pages, start, seq)
-    B, k_cap = k.shape[1], idx.shape[-1]
-    _ints(idx, (pages.c.L, B, pages.c.Hkv, k_cap), "idx", pages)
+    """Raises what pages_compact would raise, launching nothing; returns the call's
+    arguments for run_compact (the tensors have to live until then)."""
+    args = _compact_args(k, v, idx, count, pages, start, seq)
+    st = _on(pages, None)
+    B, k_cap = args[5], args[9]
+    kb._check(LIB.kve_pages_compact(*args[:7], None, args[8], 0, *args[10:], st))    # of no rows: checks alone
     if pages.c.L * B * pages.c.Hkv * (k_cap // 64 + 1) >= 1 << 24:    # workgroups of 64 rows in one launch
         raise ValueError("too many rows for one call")
+    return args
+
+
+def run_compact(args, pages: Pages, stream=None):
+    """pages_compact with the arguments that check_compact returned."""
+    kb._check(LIB.kve_pages_compact(*args, _on(pages, stream)))
 
 
 def pages_select(pages: Pages, src, idx, count, dst, start, stream=None):

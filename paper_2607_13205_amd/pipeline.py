@@ -200,20 +200,22 @@ def _score(q, k, bufs, scorer, pool_k, scale, page, l0, l1, stream=None, lse_win
 
 def _check_paged(q, k, v, lse_win, bufs, slots, per):
     """Refuses a step into pages, in chunks of ``per`` layers, that a call behind
-    pages_extend would refuse: the sequences would be longer by rows never written."""
+    pages_extend would refuse: the sequences would be longer by rows never written.
+    Returns the arguments of the first chunk's compaction."""
     if v is None or v.shape != k.shape or v.dtype is not k.dtype:
         raise ValueError("pages hold keys and values: v must match k")
     L = k.shape[0]
     if any(t is not None and t.shape[0] != L for t in (q, lse_win)) or bufs.pages.L != L or \
             bufs.idx.shape[:3] != k.shape[:3]:
         raise ValueError("q, k, lse_win, the pages and the buffers must be of the same layers and samples")
-    kp.check_compact(_part(k, 0, per), _part(v, 0, per), _part(bufs.idx, 0, per), _part(bufs.count, 0, per),
-                     bufs.pages if per == L else bufs.pages.layers(0, per), bufs.start, slots)
+    return kp.check_compact(_part(k, 0, per), _part(v, 0, per), _part(bufs.idx, 0, per), _part(bufs.count, 0, per),
+                            bufs.pages if per == L else bufs.pages.layers(0, per), bufs.start, slots)
 
 
-def _compact(k, v, bufs, idx, count, l0, l1, slots, stream):
+def _compact(k, v, bufs, idx, count, l0, l1, slots, stream, args=None):
     """Compaction of layers [l0, l1): into the dense cache, or into pages, for which
-    the first layers' counts (all layers' and heads' are equal) make room."""
+    the first layers' counts (all layers' and heads' are equal) make room.  args:
+    of the first layers' compaction into pages (_check_paged)."""
     if bufs.pages is None:
         kb.kv_compact(k, v, idx, count, k_out=_part(bufs.k_out, l0, l1), v_out=_part(bufs.v_out, l0, l1),
                       stream=stream)
@@ -224,11 +226,12 @@ def _compact(k, v, bufs, idx, count, l0, l1, slots, stream):
             bufs.add.copy_(count[0, :, 0])
         kp.pages_extend(bufs.pages, bufs.add, seq=slots, start=bufs.start, missing=bufs.missing,
                         workspace=bufs.ws_pages, stream=stream)
-    pages = bufs.pages if l0 == 0 and l1 == bufs.pages.L else bufs.pages.layers(l0, l1)
-    kp.pages_compact(k, v, idx, count, pages, bufs.start, seq=slots, stream=stream)
+        kp.run_compact(args, bufs.pages, stream)
+        return
+    kp.pages_compact(k, v, idx, count, bufs.pages.layers(l0, l1), bufs.start, seq=slots, stream=stream)
 
 
-def _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=None, events=None, fused=False, slots=None):
+def _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=None, events=None, fused=False, slots=None, args=None):
     """Top-k and compaction of layers [l0, l1) on ``stream`` (None: current);
     ``events``, three torch.cuda.Event, are recorded before the top-k, between
     the two calls and after the compaction.  fused: the score call counted the
@@ -244,7 +247,7 @@ def _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=None, events=None, fused
                        workspace=bufs.ws_topk, stream=stream)
     if events is not None:
         events[1].record(stream)
-    _compact(_part(k, l0, l1), _part(v, l0, l1), bufs, idx, count, l0, l1, slots, stream)
+    _compact(_part(k, l0, l1), _part(v, l0, l1), bufs, idx, count, l0, l1, slots, stream, args)
     if events is not None:
         events[2].record(stream)
 
@@ -305,8 +308,7 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
     L = k.shape[0]
     chunked = chunks > 1 and side_stream is not None
     per = (L + chunks - 1) // chunks if chunked else L    # layers of a chunk
-    if bufs.pages is not None:
-        _check_paged(q, k, v, lse_win, bufs, slots, per)
+    args = None if bufs.pages is None else _check_paged(q, k, v, lse_win, bufs, slots, per)
     policy = as_policy(policy)
     R = policy.R
     main = torch.cuda.current_stream()
@@ -319,7 +321,8 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
         if score_events is not None:
             score_events[1].record(main)
         quota, kept = _upload_quotas(policy, roles_host, budget, W, bufs, main)
-        _select(k, v, roles_dev, bufs, W, R, 0, L, stream=main, events=select_events, fused=fused, slots=slots)
+        _select(k, v, roles_dev, bufs, W, R, 0, L, stream=main, events=select_events, fused=fused, slots=slots,
+                args=args)
         return quota, kept
     quota, kept = _upload_quotas(policy, roles_host, budget, W, bufs, main)
     side_stream.wait_stream(main)         # the quota upload and earlier work
@@ -332,7 +335,7 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
         done = torch.cuda.Event()
         done.record(main)
         side_stream.wait_event(done)
-        _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=side_stream, fused=fused, slots=slots)
+        _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=side_stream, fused=fused, slots=slots, args=args)
     if score_events is not None:
         score_events[1].record(main)
     main.wait_stream(side_stream)

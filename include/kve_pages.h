@@ -193,8 +193,9 @@ kve_status_t kve_pages_compact(const void* k, const kve_strides_t* k_strides, co
 /*
  * A second eviction: moves rows idx[l, b, j, m] of the sequence in slot src[b],
  * unchanged, to positions start[b] + m of the sequence in slot dst[b], for m <
- * min(count[l, b, j], k_cap).  Index values outside [0, length of the source) are
- * skipped.  The source keeps its rows (kve_pages_free returns its pages).  src
+ * min(count[l, b, j], k_cap).  Index values outside [0, length of the source) and
+ * rows without a page are skipped (the position's bytes are not written).  The
+ * source keeps its rows (kve_pages_free returns its pages).  src
  * and dst may name one slot when the rows read lie below start.
  *
  *   src, start, dst [B] int32 (device); idx, count as for kve_pages_compact
@@ -224,8 +225,8 @@ kve_status_t kve_pages_read(const kve_pages_t* pages, kve_dtype_t dtype, int B, 
                             const int32_t* start, const int32_t* count, void* k_out, void* v_out,
                             void* stream);
 
-/* Workspace bytes that suffice for kve_decode_pages with these shapes, and with
- * fewer layers, samples, query heads or tokens (0 if invalid). */
+/* Workspace bytes that suffice for kve_decode_pages with these shapes, and for
+ * any that have no more layers, samples, query heads and tokens (0 if invalid). */
 size_t kve_decode_pages_workspace_size(int L, int B, int Hq, int Hkv, int max_tokens, int d);
 
 /*
@@ -235,11 +236,14 @@ size_t kve_decode_pages_workspace_size(int L, int B, int Hq, int Hkv, int max_to
  * k_t and v_t the rows of KV head h / (Hq/Hkv) as kve_pages_read gives them.  A
  * sequence with n = 0 gives zeros; rows whose page number is invalid are left out.
  * A NaN row makes the heads that read it NaN.  Logits are float32: one that falls
- * below its range has no weight.
+ * below its range has no weight.  A weight may grow to 2^16 before the sums are
+ * rescaled, so n values of less than 2^112 / n each never overflow; larger ones may
+ * become infinite.
  *
  *   q          [L, B, Hq, d] bf16 or fp32 (device), 16-byte aligned
  *   max_tokens a bound of the lengths that the caller knows (at most M * page):
- *              the work is split by it
+ *              the work is split by it, and sequences under a bound of up to 2048
+ *              need no second kernel where they are many
  *   scale      softmax scale; 0 means 1/sqrt(d)
  *   seq        [B] int32 (device), or NULL: sample b is slot b
  *   out        [L, B, Hq, d] float32 (device)

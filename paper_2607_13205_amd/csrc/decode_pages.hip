@@ -624,6 +624,9 @@ hipError_t run_heads(const void* q, const PagePool& p, int B, int Hq, int max_to
     else
         launch(std::integral_constant<int, kWaves>{});
     // up to 16 splits: one wave per row; more: four, which cut the chain of loads in four
+    // (8 KV heads of 4 query heads; one sequence of 32000 in 128 splits 21.5 us with one
+    // wave and 17.2 with four, four layers of four of 8192 level, eight of them, up to 16
+    // splits, 54 and 56, sixteen 99 and 101).  The bound counts, not the splits there are.
     const int rows = plan.pairs * B * plan.G;
     if (!plan.whole && share > 16)
         hipLaunchKernelGGL((pages_merge<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, p.Hkv, B, plan.G,

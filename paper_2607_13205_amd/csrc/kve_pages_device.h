@@ -11,7 +11,6 @@ namespace kve {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // Slot of sample b, or -1.
 __device__ __forceinline__ int slot_of(const int32_t* seq, int b, int S) {

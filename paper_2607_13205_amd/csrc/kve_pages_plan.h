@@ -57,7 +57,10 @@ struct PagesPlan {
 // query heads, so and split: 32 sequences of 1000 tokens 11.7 and 17.2 us, of 2000
 // 17 and 22.2, 64 of 1000 17 and 22.9, 100 of 500 16.2 and 20.2, 120 of 2000 49 and
 // 78, 16 of 2000 15.0 and 16.3, 4 of 500 8.5 and 9.1, but 4 of 1639 12.5 and 10.4,
-// one of 1000 10.3 and 9.0.
+// one of 1000 10.3 and 9.0, 32 of 4000 28.2 and 33.  Lengths that differ, up to the
+// same ones: 100 of 2000 24.3 and 28.5, 64 of 2000 16.7 and 17.9, 64 of 1000 11.4
+// and 14.6, 32 of 2000 14.5 and 14.1, but 16 of 2000 14.2 and 12.1, 8 of 1000 10.2
+// and 9.1, 32 of 4000 21.4 and 18.2.
 constexpr int kPagesMostResident = 4 * kDecodeUnits;  // workgroups, at four per compute unit
 constexpr int kPagesWhole = 4;                        // quanta up to which every sequence is one split
 

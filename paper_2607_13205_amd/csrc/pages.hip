@@ -138,9 +138,14 @@ struct RowGrid {
     uint32_t rows;          // of all segments (Flat)
 };
 
-// Rows per segment up to which workgroups take several segments.  4096 segments,
-// appended: of 8 rows 7.0 us so and 8.5 with a workgroup each, of 16 10.8 and 9.9,
-// of 32 17.0 and 15.3 (the divisions per row).
+// Rows per segment up to which workgroups take several segments.  Captured calls,
+// so and with a workgroup each, 4096 segments of 128 channels: of one row appended
+// 5.6 and 7.1 us, read 4.9 and 7.1, selected 3.9 and 5.4; of 8 6.8 and 7.7, 6.3 and
+// 7.5, 4.3 and 5.8; of 16 10.9 and 9.6, 8.7 and 8.2, 6.5 and 7.6; of 32 17.2 and
+// 15.6 (the divisions per row), 14.1 and 12.6, level.  Few segments are the other
+// way round, since 64 rows to a workgroup leave most compute units idle: 128 of one
+// row appended 5.0 and 2.7 us, read 4.5 and 2.8, selected 3.4 and 3.0; the rule does
+// not look at their number.
 constexpr int kFlatRows = 8;
 
 struct RowAt {
@@ -256,7 +261,9 @@ __global__ __launch_bounds__(kThreads) void pack_rows(RowView kv, RowView vv, Ro
 // D / 32 lanes to a row, each a block of 32 channels (16 bytes of codes, one
 // scale byte) of a key and a value row.  The source rows are read once and their
 // sequence ends, as a rule: non-temporal loads (16 layers, 4 sequences, 4001 of
-// 16001 rows: 105 us, 5.3 TB/s read and written; 115 without).
+// 16001 rows: 105 us, 5.3 TB/s read and written; 115 without).  Rows of 64 channels
+// leave half of a workgroup without work; random rows of 16001 move at 3.6 TB/s
+// so, those of 128 at 3.8.
 template <int D, bool Flat>
 __global__ __launch_bounds__(kThreads) void select_rows(PagePool p, RowGrid g, const int32_t* __restrict__ src,
                                                         const int32_t* __restrict__ idx,
@@ -286,7 +293,8 @@ __global__ __launch_bounds__(kThreads) void select_rows(PagePool p, RowGrid g, c
 }
 
 // D / 8 lanes to a row, as in pack_rows.  Bound by HBM: 2 M rows of a pool of
-// 1.1 GB in 267 us, 5.0 TB/s read and written; 1.7 M rows just packed in 155 us.
+// 1.1 GB in 267 us, 5.0 TB/s read and written; 1.7 M rows just packed in 155 us;
+// as float32 0.4 M of them take 175 us, 2.8 TB/s (bf16: 44).
 // Non-temporal loads of the codes gain 8% on the former and lose 7% on the
 // latter; cached stores lose 30%.
 template <typename T, int D, bool Flat>
@@ -377,7 +385,9 @@ __device__ __forceinline__ uint32_t scan_exclusive(uint32_t x, uint32_t* s, uint
 // The first `want` free pages in ascending order into list; returns how many
 // there are (all free pages, where fewer than `want`).  Every wave takes 64
 // neighbouring pages per load: a ballot ranks them, and the tallies of a round
-// are summed by every wave for itself.
+// are summed by every wave for itself.  A round is 16384 pages and about 6.5 us: a
+// call passes over all full pages below the ones it takes (extend of 16 sequences
+// by a page: 10 us in an empty pool of 300000, 126 with its first 297000 full).
 __device__ __noinline__ int find_free(const int32_t* refs, int n_pages, int want, int32_t* list) {
     __shared__ uint32_t s_tally[kTallies];
     const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;

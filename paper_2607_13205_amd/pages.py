@@ -286,7 +286,7 @@ def decode_pages(q, pages: Pages, max_tokens: int | None = None, seq=None, scale
     """decode_attention over paged sequences: q [L, B, Hq, d] attends to the rows
     of the sequences in slots seq (slot b without it) -> float32 [L, B, Hq, d].
     max_tokens bounds the lengths (default: what the table can hold); the work is
-    split by it."""
+    split by it.  A workspace made for the largest call serves smaller ones."""
     torch = kb._torch()
     shape = q.shape
     if len(shape) != 4 or shape[0] != pages.c.L or shape[3] != pages.d or q.get_device() != pages.index or \

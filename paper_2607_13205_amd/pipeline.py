@@ -308,7 +308,9 @@ def evict(q, k, v, roles_host: np.ndarray, roles_dev, policy, budget: float, W: 
     L = k.shape[0]
     chunked = chunks > 1 and side_stream is not None
     per = (L + chunks - 1) // chunks if chunked else L    # layers of a chunk
-    args = None if bufs.pages is None else _check_paged(q, k, v, lse_win, bufs, slots, per)
+    args = None
+    if bufs.pages is not None:
+        args = _check_paged(q, k, v, lse_win if scorer == "snapkv" else None, bufs, slots, per)
     policy = as_policy(policy)
     R = policy.R
     main = torch.cuda.current_stream()

@@ -2,7 +2,8 @@
 all of a sequence's blocks or to those that a score over their bounds selects.
 
 A block is a page of ``page`` tokens of one layer and KV head, held as eight-bit floats (E4M3, largest value 448) with
-one power of two for its keys and one for its values: the smallest, 2^e, under which no finite element exceeds 448.
+one power of two for its keys and one for its values: the smallest, 2^e with e >= -100, under which no element exceeds
+448.
 Its bytes: key codes [page, d], value codes [page, d], then a tail of 128 + 2 d bytes: the two powers (plus 127) in
 its first two bytes, and from byte 128 on the smallest and the largest key code of each channel.  A pool is uint8
 [L, n_pages, Hkv, block bytes]; ``table`` names a sequence's pages, ``held`` counts them and ``length`` its tokens.
@@ -27,7 +28,7 @@ own = False
 DEV = "cuda"
 DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
 TAIL = 128            # bytes before a block's bounds
-LOWEST, HIGHEST = -117, 120   # powers of two that a block may have
+LOWEST, HIGHEST = -100, 119   # powers of two that a block may have
 
 
 def _case(name, op, **kw):

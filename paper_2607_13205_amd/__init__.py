@@ -22,6 +22,13 @@ The hot path runs in libkve.so (HIP); this package is its thin Python binding:
   pages_compact, pages_append               kept rows and new tokens packed into pages
   pages_select, pages_read                  rows moved between sequences, rows read back
   decode_pages   one decode query per head over paged sequences
+  Blocks         a paged cache of 8-bit rows, a scale per page and head (include/kve_blocks.h),
+                 and its calls, with pages_extend and pages_free:
+  blocks_append  new tokens written, keys and queries turned to their positions (Rotation)
+  blocks_compact kept rows written into blocks
+  blocks_read, blocks_bounds                rows, and the bounds of blocks' keys, read back
+  blocks_top     the blocks whose keys can score highest, for each query token
+  decode_blocks  one or a few query tokens over sequences, or over their chosen blocks
   pipeline.evict the whole step over resident tensors
 """
 
@@ -35,6 +42,9 @@ from .binding import (EXPORTED, KveError, decode_attention, decode_workspace_siz
 from .pages import (Pages, decode_pages, decode_pages_workspace_size, page_bytes, pages_append,  # noqa: F401
                     pages_compact, pages_extend, pages_fork, pages_free, pages_read, pages_select,
                     pages_workspace_size)
+from .blocks import (Blocks, Rotation, block_bytes, blocks_append, blocks_bounds, blocks_compact,  # noqa: F401
+                     blocks_read, blocks_top, blocks_top_workspace_size, decode_blocks,
+                     decode_blocks_workspace_size)
 from . import pipeline  # noqa: F401
 
 __all__ = ["snapkv_score", "snapkv_score_strided", "kv_compact_strided", "Strides", "h2o_score", "h2o_score_strided", "quest_score_strided", "role_allocate", "role_allocate_fair", "role_map",
@@ -43,4 +53,6 @@ __all__ = ["snapkv_score", "snapkv_score_strided", "kv_compact_strided", "Stride
            "quest_workspace_size", "role_probe", "snapkv_score_lse", "topk_workspace_size", "source_hash",
            "snapkv_score_noalloc", "role_hist_size", "snapkv_score_hist", "topk_select_hist",
            "Pages", "page_bytes", "pages_workspace_size", "pages_extend", "pages_fork", "pages_free", "pages_append",
-           "pages_compact", "pages_select", "pages_read", "decode_pages", "decode_pages_workspace_size"]
+           "pages_compact", "pages_select", "pages_read", "decode_pages", "decode_pages_workspace_size",
+           "Blocks", "Rotation", "block_bytes", "blocks_append", "blocks_compact", "blocks_read", "blocks_bounds",
+           "blocks_top", "blocks_top_workspace_size", "decode_blocks", "decode_blocks_workspace_size"]

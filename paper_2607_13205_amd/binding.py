@@ -48,6 +48,12 @@ EXPORTED_PAGES = (
     "kve_decode_pages_workspace_size", "kve_decode_pages",
 )
 
+#: every symbol include/kve_blocks.h declares (their Python side is blocks.py)
+EXPORTED_BLOCKS = (
+    "kve_block_bytes", "kve_blocks_append", "kve_blocks_compact", "kve_blocks_read", "kve_blocks_bounds",
+    "kve_blocks_top_workspace_size", "kve_blocks_top", "kve_decode_blocks_workspace_size", "kve_decode_blocks",
+)
+
 
 class Strides(ctypes.Structure):
     """kve_strides_t: element strides of a [layer, batch, head, token] view of
@@ -127,6 +133,17 @@ def _load():
         "kve_decode_pages_workspace_size": (c_size, [c_int] * 6),
         "kve_decode_pages": (c_int, [c_void, c_int, c_void, c_int, c_int, c_int, c_void, c_float, c_void, c_void,
                                      c_size, c_void]),
+        "kve_block_bytes": (c_size, [c_int] * 2),
+        "kve_blocks_append": (c_int, [c_void] * 4 + [c_int] * 3 + [c_void] * 7 + [c_int, c_void, c_void]),
+        "kve_blocks_compact": (c_int, [c_void] * 4 + [c_int] * 3 + [c_void, c_void, c_int] + [c_void] * 4),
+        "kve_blocks_read": (c_int, [c_void, c_int, c_int, c_int] + [c_void] * 6),
+        "kve_blocks_bounds": (c_int, [c_void, c_int, c_int, c_int] + [c_void] * 5),
+        "kve_blocks_top_workspace_size": (c_size, [c_int] * 6),
+        "kve_blocks_top": (c_int, [c_void, c_int, c_void] + [c_int] * 4 + [c_void, c_void] + [c_int] * 3 +
+                           [c_void, c_void, c_size, c_void]),
+        "kve_decode_blocks_workspace_size": (c_size, [c_int] * 6),
+        "kve_decode_blocks": (c_int, [c_void, c_int, c_void] + [c_int] * 4 + [c_void] * 3 +
+                              [c_int, c_float, c_void, c_void, c_size, c_void]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

@@ -1,0 +1,95 @@
+// The paged 8-bit cache: what its kernels and the C ABI share.  Plain C++.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kve_pages_plan.h"
+
+namespace kve {
+
+constexpr int kBlockMax = 128;    // tokens per block: 32, 64 or 128
+constexpr int kBlockScales = 128;  // bytes of a block's tail before its bounds
+constexpr int kBlockScaleMin = 27, kBlockScaleMax = 246;
+
+inline size_t block_bytes(int page, int d) { return (size_t)2 * page * d + kBlockScales + 2 * d; }
+
+// A rotation as kernels see it; cos null: none.
+struct BlockRotation {
+    const float *cos, *sin;
+    const int32_t* position;
+    int P, r, pairs;
+};
+
+// Blocks that `rows` rows can touch, wherever the first one lies.
+inline long long blocks_touched(long long rows, int page) { return rows == 0 ? 0 : (rows + page - 2) / page + 1; }
+
+constexpr int kBlocksQueryRows = 64;  // rows per workgroup that rotates queries
+
+// What query tokens see (kve_blocks.h): start null: the last T tokens.
+struct BlockView {
+    const int32_t *seq, *start;
+    int B, T, max_tokens;
+};
+
+// Plan of a decode over blocks.  Query tokens of a sample are taken `per` at a time,
+// an entry each: as many as the sixteen columns of a product hold heads for, or one
+// where each has its own blocks.  The entries' tokens are cut as PagesPlan's.
+struct BlocksPlan {
+    int pairs, G, per, tiles, entries, R;  // R: query rows of an entry, per * G
+    int groups;                            // workgroups per (layer, KV head)
+    bool whole;                            // one split per entry: nothing to merge
+    size_t off_ml, off_ranges, total;
+};
+
+// Workgroups that share a compute unit, by their LDS.
+constexpr int kBlocksPerUnit = 2;
+
+inline size_t decode_blocks_bytes(size_t parts, long long entries, int d, BlocksPlan* p) {
+    p->off_ml = align_up(parts * d * sizeof(float));
+    p->off_ranges = p->off_ml + align_up(parts * 2 * sizeof(float));
+    return p->off_ranges + align_up((size_t)entries * 2 * sizeof(int32_t));  // every entry's first split and count
+}
+
+// tokens: a bound of an entry's tokens.
+inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long long tokens, bool sparse, int d) {
+    BlocksPlan p{};
+    p.pairs = L * Hkv;
+    p.G = Hq / Hkv;
+    p.per = sparse ? 1 : kPagesMaxGroup / p.G;
+    if (p.per > T) p.per = T;
+    p.tiles = (T + p.per - 1) / p.per;
+    p.entries = B * p.tiles;
+    p.R = p.per * p.G;
+    const long long quanta = (tokens + kDecodeQuantum - 1) / kDecodeQuantum;
+    const long long segs = (long long)p.pairs * p.entries;
+    p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > kPagesWhole ? segs / 8 : kPagesWhole);
+    const int share = p.pairs < kBlocksPerUnit * kDecodeUnits ? kBlocksPerUnit * kDecodeUnits / p.pairs : 1;
+    long long groups = (long long)share + p.entries;
+    if (groups > p.entries * quanta) groups = p.entries * quanta;
+    if (p.whole) groups = p.entries;
+    p.groups = (int)groups;
+    p.total = decode_blocks_bytes(p.whole ? 0 : (size_t)p.pairs * p.groups * p.R, p.entries, d, &p);
+    return p;
+}
+
+// Workspace that suffices for this call and for every one of no more layers,
+// samples, query heads and query tokens: at most one round of workgroups, or one
+// of every pair, and one of every entry, of R rows each; the last entry of a
+// sample may have fewer query tokens than its rows, which at most doubles them.
+inline size_t decode_blocks_size(int L, int B, int Hq, int Hkv, int T, int d) {
+    const long long pairs = (long long)L * Hkv, G = Hq / Hkv;
+    const long long most = G * T < kPagesMaxGroup ? G * T : kPagesMaxGroup;
+    const long long round = pairs > kBlocksPerUnit * kDecodeUnits ? pairs : kBlocksPerUnit * kDecodeUnits;
+    BlocksPlan p{};
+    return decode_blocks_bytes((size_t)(round * most + pairs * B * G * T * (T > 1 ? 2 : 1)), (long long)B * T, d, &p);
+}
+
+// Blocks that max_tokens tokens can lie in.
+inline int top_blocks(int max_tokens, int page) { return (max_tokens + page - 1) / page; }
+
+inline size_t top_size(int L, int B, int Hkv, int T, int max_tokens, int page) {
+    return align_up((size_t)L * B * Hkv * T * top_blocks(max_tokens, page) * sizeof(uint32_t));
+}
+
+}  // namespace kve

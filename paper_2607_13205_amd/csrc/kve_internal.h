@@ -5,6 +5,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "kve_blocks_plan.h"
 #include "kve_decode_plan.h"
 #include "kve_pages_plan.h"
 #include "kve_quest_plan.h"
@@ -110,5 +111,20 @@ hipError_t launch_pages_read(const PagePool& p, int dtype, int d, int B, int T, 
                              const int32_t* start, const int32_t* count, void* k_out, void* v_out, hipStream_t st);
 hipError_t launch_decode_pages(const void* q, int dtype, const PagePool& p, int d, int B, int Hq, int max_tokens,
                                const int32_t* seq, float scale, float* out, void* ws, hipStream_t st);
+
+// The paged 8-bit cache (kve_blocks.h); p.L layers per call.  idx and count as for
+// launch_pages_pack; rot.cos null: no rotation; q_out null: no queries.
+hipError_t launch_blocks_write(const RowView& k, const RowView& v, const RowView& q, void* q_out, int Hq, int dtype,
+                               int d, int B, int N, const int32_t* idx, const int32_t* count, int cap,
+                               const int32_t* start, const int32_t* seq, const BlockRotation& rot, const PagePool& p,
+                               hipStream_t st);
+hipError_t launch_blocks_read(const PagePool& p, int dtype, int d, int B, int T, const int32_t* seq,
+                              const int32_t* start, const int32_t* count, void* k_out, void* v_out, hipStream_t st);
+hipError_t launch_blocks_bounds(const PagePool& p, int dtype, int d, int B, int n, const int32_t* seq,
+                                const int32_t* first, void* lo, void* hi, hipStream_t st);
+hipError_t launch_blocks_top(const void* q, int dtype, const PagePool& p, int d, const BlockView& view, int Hq, int k,
+                             int first, int last, int32_t* top, void* ws, hipStream_t st);
+hipError_t launch_decode_blocks(const void* q, int dtype, const PagePool& p, int d, const BlockView& view, int Hq,
+                                const int32_t* top, int k, float scale, float* out, void* ws, hipStream_t st);
 
 }  // namespace kve

@@ -92,6 +92,12 @@ class Pages:
                      self.part or pool.shape[0] != self.L)
 
 
+def _four_bit(pages):
+    """Refuses a cache of another format for a call on four-bit rows."""
+    if not isinstance(pages, Pages):
+        raise ValueError("the cache must be a Pages")
+
+
 def _on(pages: Pages, stream):
     """The stream to launch on; the cache's device must be the current one."""
     torch = kb._torch()
@@ -182,6 +188,7 @@ def pages_fork(pages: Pages, src, dst, done=None, missing=None, workspace=None, 
     """Slot dst[i] becomes a continuation of the sequence in slot src[i].  Returns
     (done, missing): 1 per entry, 0 where it was refused, and the pages lacking.
     Takes all layers of the cache: the others would lack the rows that are copied."""
+    _four_bit(pages)
     if pages.part:
         raise ValueError("a fork takes all layers of the cache")
     n = src.numel()
@@ -202,6 +209,7 @@ def pages_append(k, v, pages: Pages, start, n_new=None, seq=None, stream=None):
     """Packs the first n_new[b] (all without it) of the rows k, v [L, B, Hkv, T, d]
     into positions start[b] on of the sequence in slot seq[b]; views as for
     kv_compact_strided."""
+    _four_bit(pages)
     B, T, kp, ks, vp, vs, dt = _rows(k, v, pages)
     kb._check(LIB.kve_pages_append(kp, ks, vp, vs, dt, B, T, _ints(n_new, (B,), "n_new", pages, True),
                                    _ints(start, (B,), "start", pages), _ints(seq, (B,), "seq", pages, True),
@@ -209,6 +217,7 @@ def pages_append(k, v, pages: Pages, start, n_new=None, seq=None, stream=None):
 
 
 def _compact_args(k, v, idx, count, pages, start, seq):
+    _four_bit(pages)
     B, N, kp, ks, vp, vs, dt = _rows(k, v, pages)
     shape = (pages.c.L, B, pages.c.Hkv)
     k_cap = idx.shape[-1]
@@ -243,6 +252,7 @@ def run_compact(args, pages: Pages, stream=None):
 def pages_select(pages: Pages, src, idx, count, dst, start, stream=None):
     """A second eviction: rows idx[l, b, j, :count[l, b, j]] of the sequence in
     slot src[b] moved, unchanged, to positions start[b] on of slot dst[b]."""
+    _four_bit(pages)
     B, k_cap = src.numel(), idx.shape[-1]
     shape = (pages.L, B, pages.Hkv)
     kb._check(LIB.kve_pages_select(ctypes.byref(pages.c), B, _ints(src, (B,), "src", pages),
@@ -257,6 +267,7 @@ def pages_read(pages: Pages, T: int, seq=None, start=None, count=None, dtype=Non
     slots without it): T rows from start[b] (0), count[b] (T) of them.  Outputs
     are of ``dtype`` (bfloat16) unless given; rows that the sequence does not
     have stay as they were, zero in outputs made here."""
+    _four_bit(pages)
     torch = kb._torch()
     B = pages.c.S if seq is None else seq.numel()
     shape = (pages.c.L, B, pages.c.Hkv, T, pages.d)
@@ -287,6 +298,7 @@ def decode_pages(q, pages: Pages, max_tokens: int | None = None, seq=None, scale
     of the sequences in slots seq (slot b without it) -> float32 [L, B, Hq, d].
     max_tokens bounds the lengths (default: what the table can hold); the work is
     split by it.  A workspace made for the largest call serves smaller ones."""
+    _four_bit(pages)
     torch = kb._torch()
     shape = q.shape
     if len(shape) != 4 or shape[0] != pages.c.L or shape[3] != pages.d or q.get_device() != pages.index or \

@@ -14,6 +14,8 @@ Modules
                and the per-role mass diagnostics.
 ``pages``      the paged 4-bit cache: the row format, the page bookkeeping as
                sequential Python, decode over it.
+``blocks``     the paged 8-bit cache: the block format, rotation, block scores
+               and choice, attention.
 ``brute``      pure-Python loops over tiny inputs (an independent second
                reading used to pin ``reference``).
 
@@ -31,3 +33,4 @@ which group query heads into KV heads, have their own grouping pins.
 
 from .reference import *  # noqa: F401,F403
 from .pages import *  # noqa: F401,F403
+from .blocks import *  # noqa: F401,F403

@@ -173,6 +173,24 @@ def blocks_compact(k, v, idx, count, blocks: Blocks, start, seq=None, stream=Non
     kb._check(LIB.kve_blocks_compact(*_compact_args(k, v, idx, count, blocks, start, seq), _on(blocks, stream)))
 
 
+def check_compact(k, v, idx, count, blocks: Blocks, start, seq=None):
+    """Raises what blocks_compact would raise, launching nothing; returns the call's
+    arguments for run_compact (the tensors have to live until then)."""
+    args = _compact_args(k, v, idx, count, blocks, start, seq)
+    st = _on(blocks, None)
+    B, k_cap = args[5], args[9]
+    kb._check(LIB.kve_blocks_compact(*args[:7], None, args[8], 0, *args[10:], st))    # of no rows: checks alone
+    # workgroups, for the keys and the values of each block that the rows can touch, in one launch
+    if 2 * blocks.c.L * B * blocks.c.Hkv * ((k_cap + blocks.page - 2) // blocks.page + 1) >= 1 << 24:
+        raise ValueError("too many rows for one call")
+    return args
+
+
+def run_compact(args, blocks: Blocks, stream=None):
+    """blocks_compact with the arguments that check_compact returned."""
+    kb._check(LIB.kve_blocks_compact(*args, _on(blocks, stream)))
+
+
 def _outputs(blocks, shape, dtype, names, outs, stream):
     """(dtype, outputs) of a call that reads the cache: the caller's, or zeros."""
     torch = kb._torch()

@@ -3,7 +3,7 @@
 score (SnapKV windowed + pooled, H2O, or the one-shot Quest page bound)  ->
 role allocation (host)  ->
 per-role top-k  ->  K/V compaction, into a dense cache or into the pages of a
-4-bit one (``alloc_pages``).  Buffers are allocated once by ``EvictBuffers`` so
+4-bit (``alloc_pages``) or 8-bit one (``alloc_blocks``).  Buffers are allocated once by ``EvictBuffers`` so
 that repeated steps allocate nothing.
 
 ``Policy`` names how the budget is split over buckets: the role-conditional
@@ -18,6 +18,7 @@ from dataclasses import dataclass
 import numpy as np
 
 from . import binding as kb
+from . import blocks as kq
 from . import pages as kp
 
 
@@ -99,7 +100,7 @@ class EvictBuffers:
     k_cap: int
     copy_done: object = None   # event after the last quota upload from quota_host
     hist: object = None        # per-tile role histograms of the fused SnapKV epilogue, [L, words per layer]
-    pages: object = None       # the Pages that take the kept rows in place of k_out and v_out
+    pages: object = None       # the Pages or Blocks that take the kept rows in place of k_out and v_out
     add: object = None         # with pages: kept rows of each sample, int32 [B]
     start: object = None       # with pages: each sample's first position (-1: no room), int32 [B]
     missing: object = None     # with pages: pages that were lacking, int32 [1]
@@ -113,10 +114,11 @@ def alloc_buffers(k, n_q_heads: int, W: int, R: int, k_cap: int, scorer: str = "
     (snapkv_score_hist / topk_select_hist) and the histograms live here.  Off
     by default: on the 32-layer N = 32768 step the counting adds more to the
     pool (about 100 us) than it takes off the top-k (about 25 us).  pages: a
-    Pages of as many layers that the steps pack the kept rows into (evict's
+    Pages or Blocks of as many layers that the steps pack the kept rows into (evict's
     ``slots``); there is no dense output then.  A step lengthens its sequences in
     all layers of the cache: where these are some of them (Pages.layers), the
-    others' rows are the caller's to pack, at bufs.start (pages_compact)."""
+    others' rows are the caller's to pack, at bufs.start (pages_compact, or
+    blocks_compact)."""
     import torch
     L, B, Hkv, N, d = k.shape
     dev = k.device
@@ -170,6 +172,26 @@ def alloc_pages(L: int, Hkv: int, d: int, n_pages: int, slots: int, max_tokens: 
                     zeros(slots, -(-max_tokens // page)), zeros(slots), zeros(slots), page, d)
 
 
+def alloc_blocks(L: int, Hkv: int, d: int, n_pages: int, slots: int, max_tokens: int, page: int = 64,
+                 device="cuda") -> kq.Blocks:
+    """An empty paged 8-bit cache: n_pages blocks of ``page`` tokens (32, 64 or 128)
+    in each layer and head, for ``slots`` sequences of up to max_tokens tokens."""
+    import torch
+    nb = kq.block_bytes(page, d)
+    if nb == 0:
+        raise ValueError(f"page={page} must be 32, 64 or 128 and d={d} 64 or 128")
+
+    def zeros(*shape):
+        return torch.zeros(shape, dtype=torch.int32, device=device)
+    return kq.Blocks(torch.zeros((L, n_pages, Hkv, nb), dtype=torch.uint8, device=device), zeros(n_pages),
+                     zeros(slots, -(-max_tokens // page)), zeros(slots), zeros(slots), page, d)
+
+
+def _calls_of(cache):
+    """The module with the calls of a paged cache."""
+    return kq if isinstance(cache, kq.Blocks) else kp
+
+
 def _fused(bufs, scorer, lse_win):
     return bufs.hist is not None and scorer == "snapkv" and lse_win is None
 
@@ -208,8 +230,9 @@ def _check_paged(q, k, v, lse_win, bufs, slots, per):
     if any(t is not None and t.shape[0] != L for t in (q, lse_win)) or bufs.pages.L != L or \
             bufs.idx.shape[:3] != k.shape[:3]:
         raise ValueError("q, k, lse_win, the pages and the buffers must be of the same layers and samples")
-    return kp.check_compact(_part(k, 0, per), _part(v, 0, per), _part(bufs.idx, 0, per), _part(bufs.count, 0, per),
-                            bufs.pages if per == L else bufs.pages.layers(0, per), bufs.start, slots)
+    return _calls_of(bufs.pages).check_compact(_part(k, 0, per), _part(v, 0, per), _part(bufs.idx, 0, per),
+                                               _part(bufs.count, 0, per),
+                                               bufs.pages if per == L else bufs.pages.layers(0, per), bufs.start, slots)
 
 
 def _compact(k, v, bufs, idx, count, l0, l1, slots, stream, args=None):
@@ -226,9 +249,10 @@ def _compact(k, v, bufs, idx, count, l0, l1, slots, stream, args=None):
             bufs.add.copy_(count[0, :, 0])
         kp.pages_extend(bufs.pages, bufs.add, seq=slots, start=bufs.start, missing=bufs.missing,
                         workspace=bufs.ws_pages, stream=stream)
-        kp.run_compact(args, bufs.pages, stream)
+        _calls_of(bufs.pages).run_compact(args, bufs.pages, stream)
         return
-    kp.pages_compact(k, v, idx, count, bufs.pages.layers(l0, l1), bufs.start, seq=slots, stream=stream)
+    compact = kq.blocks_compact if isinstance(bufs.pages, kq.Blocks) else kp.pages_compact
+    compact(k, v, idx, count, bufs.pages.layers(l0, l1), bufs.start, seq=slots, stream=stream)
 
 
 def _select(k, v, roles_dev, bufs, W, R, l0, l1, stream=None, events=None, fused=False, slots=None, args=None):

@@ -1,0 +1,873 @@
+"""The paged 8-bit cache on the GPU against its oracle: what blocks hold, rotated
+queries, bounds and chosen blocks value for value, attention within the error that
+float32 sums can have."""
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import oracle as O  # noqa: E402
+from tests.parity import report  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+U = 2.0 ** -24  # half a step of float32, relative
+
+
+@pytest.fixture(scope="module")
+def K():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2607_13205_amd.build import ensure_built
+    ensure_built()
+    import paper_2607_13205_amd as K
+    return K
+
+
+def dev(x, dtype=torch.int32):
+    return torch.as_tensor(np.ascontiguousarray(x)).to(dtype).cuda()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def normal(shape, dtype, seed, scale=1.0):
+    return (scale * torch.randn(shape, generator=torch.Generator().manual_seed(seed))).to(TORCH[dtype])
+
+
+def make(K, L, Hkv, d, page, n_pages, S, M, seed=0):
+    """An empty cache whose pool and table hold anything, NaN codes and scales of 255 among it."""
+    g = np.random.default_rng(seed)
+    pool = g.integers(0, 256, (L, n_pages, Hkv, K.block_bytes(page, d)), dtype=np.uint8)
+    pool[..., 2 * page * d:2 * page * d + 2] = g.choice([255, 0, 1, 254, 127], pool.shape[:-1] + (2,))
+    z = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = dev(g.integers(-(1 << 31), 1 << 31, (S, M)))
+    return K.Blocks(torch.from_numpy(pool).cuda(), z(n_pages), table, z(S), z(S), page, d)
+
+
+class Model:
+    """The oracle's picture of a cache: BlockRows per (slot, layer, head)."""
+
+    def __init__(self, cache):
+        self.c = cache
+        self.rows = {}
+
+    def at(self, slot, l, j):
+        return self.rows.setdefault((slot, l, j), O.BlockRows(self.c.page, self.c.d, self.c.table.shape[1]))
+
+    def write(self, slot, start, k, v):
+        """k, v [L, Hkv, n, d], float64."""
+        for l in range(k.shape[0]):
+            for j in range(k.shape[1]):
+                self.at(slot, l, j).write(start, k[l, j], v[l, j])
+
+    def same(self, slot, n):
+        """The cache's bytes of a slot's first n rows, its scales and its bounds are the model's."""
+        c = self.c
+        nb = -(-n // c.page)
+        if nb == 0:
+            return
+        raw = c.pool[:, c.table[slot, :nb].long()].cpu().numpy()
+        for l in range(c.L):
+            for j in range(c.Hkv):
+                m = self.at(slot, l, j)
+                k, v, s, b = O.block_unpack(raw[l, :, j], c.page, c.d)
+                for x, codes in ((0, k), (1, v)):
+                    got = O.e4m3_values(codes).reshape(-1, c.d)[:n]
+                    want = m.code[x, :nb].reshape(-1, c.d)[:n]
+                    assert np.array_equal(s[:, x], m.s[x, :nb]), (slot, l, j, x)
+                    assert np.array_equal(got, want, equal_nan=True), (slot, l, j, x)
+                    assert np.array_equal(np.signbit(got[want == 0]), np.signbit(want[want == 0]))
+                assert np.array_equal(O.e4m3_values(b[:, 0]), m.bound[0, :nb], equal_nan=True), (slot, l, j)
+                assert np.array_equal(O.e4m3_values(b[:, 1]), m.bound[1, :nb], equal_nan=True), (slot, l, j)
+
+
+def filled(K, L, Hkv, d, page, lengths, seed=0, spare=3, dtype="bf16", extra_slots=0, scale=1.0):
+    """(cache, k, v float64 [L, B, Hkv, T, d] as held) with one sequence per length, in slots in order."""
+    S, n_pages = len(lengths) + extra_slots, sum(-(-n // page) for n in lengths) + spare
+    M = max(1, max(-(-n // page) for n in lengths) + 1)
+    cache = make(K, L, Hkv, d, page, n_pages, S, M, seed)
+    B, T = len(lengths), max(max(lengths), 1)
+    start, missing = K.pages_extend(cache, dev(lengths), seq=dev(range(B)))
+    assert start.tolist() == [0] * B and missing.item() == 0
+    k, v = normal((L, B, Hkv, T, d), dtype, seed + 1, scale).cuda(), normal((L, B, Hkv, T, d), dtype, seed + 2).cuda()
+    K.blocks_append(k, v, cache, start, n_new=dev(lengths), seq=dev(range(B)))
+    k, v = K.blocks_read(cache, T, seq=dev(range(B)), dtype=torch.float32)
+    return cache, host(k), host(v)
+
+
+# ---------------------------------------------------------------------------
+# what blocks hold
+# ---------------------------------------------------------------------------
+
+def hard_rows(dtype, d, page):
+    """Blocks of rows that meet every border of the format; each block's largest magnitude is its first element."""
+    r = np.random.default_rng(5)
+    mid = (O.E4M3[1:] + O.E4M3[:-1]) / 2
+    blocks = []
+    for top, unit in ((448.0, 1.0), (448.0, 2.0 ** 70), (448.0, 2.0 ** -90), (256.0, 1.0), (447.0, 2.0 ** 3),
+                      (449.0, 1.0), (450.0, 2.0 ** 10), (225.0, 1.0)):
+        x = r.choice(np.concatenate([mid, O.E4M3, mid * (1 + 2.0 ** -20), mid * (1 - 2.0 ** -20)]), (page, d))
+        x *= r.choice([-1.0, 1.0], x.shape)
+        x[0, 0] = top
+        blocks.append(np.clip(x, -top, top) * unit)
+    blocks += [np.zeros((page, d)), np.full((page, d), -0.0), np.full((page, d), 2.0 ** -120),
+               r.standard_normal((page, d)) * 2.0 ** -105, np.full((page, d), 3.3e38), r.standard_normal((page, d)) * 1e38,
+               r.standard_normal((page, d)) * 2.0 ** r.integers(-30, 30, (page, d))]
+    bad = r.standard_normal((page, d))
+    bad[3, 5], bad[7, 6], bad[9, 7], bad[page - 1, d - 1] = np.nan, np.inf, -np.inf, np.nan
+    only = np.full((page, d), np.inf)
+    blocks += [bad, only]
+    x = torch.from_numpy(np.concatenate(blocks)).clamp(-3.38e38, 3.38e38).to(TORCH[dtype])
+    x[-page:] = float("inf")
+    x[-2 * page + 7, 6], x[-2 * page + 9, 7] = float("inf"), -float("inf")
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(64, 32), (64, 128), (128, 64), (128, 32), (128, 128), (64, 64)])
+def test_blocks_hold_the_nearest(K, dtype, d, page):
+    x = hard_rows(dtype, d, page)
+    n = len(x) - 5                                                  # the last block is not full
+    cache = make(K, 1, 1, d, page, len(x) // page + 2, 1, len(x) // page + 1)
+    start, _ = K.pages_extend(cache, dev([n]))
+    k, v = x[:n][None, None, None].cuda(), x.flip(0)[:n][None, None, None].cuda()
+    K.blocks_append(k, v, cache, start)
+    m = Model(cache)
+    with np.errstate(over="ignore"):
+        m.write(0, 0, host(k)[:, 0], host(v)[:, 0])
+    m.same(0, n)
+    for dt in ("bf16", "f32"):
+        gk, gv = K.blocks_read(cache, n, dtype=TORCH[dt])
+        wk, wv = m.at(0, 0, 0).values(n)
+        assert np.array_equal(host(gk)[0, 0, 0], wk, equal_nan=True) and np.array_equal(host(gv)[0, 0, 0], wv, equal_nan=True)
+        nb = -(-n // page)
+        lo, hi = K.blocks_bounds(cache, nb, dtype=TORCH[dt])
+        wl, wh = m.at(0, 0, 0).bounds()
+        assert np.array_equal(host(lo)[0, 0, 0], wl[:nb], equal_nan=True)
+        assert np.array_equal(host(hi)[0, 0, 0], wh[:nb], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 64), ("f32", 64, 32), ("bf16", 64, 128), ("f32", 128, 128)])
+def test_rows_written_piece_by_piece(K, dtype, d, page):
+    """Blocks keep what they held, rounded again where the scale rises; a NaN stays one."""
+    r = np.random.default_rng(d + page)
+    L, Hkv, B = 2, 3, 3
+    M = 6
+    cache = make(K, L, Hkv, d, page, B * M, B, M, seed=4)
+    m = Model(cache)
+    at = [0] * B
+    for step, T in enumerate((1, 1, 1, 7, page - 2, 1, 2 * page + 3, 1, 40, 1)):
+        new = [int(r.integers(0, T + 1)) if T > 1 else 1 for _ in range(B)]
+        start, missing = K.pages_extend(cache, dev(new))
+        assert missing.item() == 0 and start.tolist() == at
+        k = normal((L, B, Hkv, T, d), dtype, 100 + step) * 2.0 ** dev(r.integers(-12, 30, (L, B, Hkv, 1, 1))).cpu()
+        v = normal((L, B, Hkv, T, d), dtype, 200 + step) * 2.0 ** dev(r.integers(-12, 30, (L, B, Hkv, 1, 1))).cpu()
+        k, v = k.to(TORCH[dtype]).cuda(), v.to(TORCH[dtype]).cuda()
+        if step == 3:
+            k[:, 0, :, 0, 1], v[:, 0, :, 0, 2] = float("nan"), float("inf")
+        K.blocks_append(k, v, cache, start, n_new=dev(new))
+        for b in range(B):
+            m.write(b, at[b], host(k)[:, b, :, :new[b]], host(v)[:, b, :, :new[b]])
+            at[b] += new[b]
+        for b in range(B):
+            m.same(b, at[b])
+
+
+@pytest.mark.parametrize("dtype,d,r,pairs,T,Hq,Hkv,P", [
+    ("bf16", 128, 128, False, 1, 8, 2, 5000),
+    ("bf16", 128, 128, True, 1, 3, 3, 17),
+    ("bf16", 128, 48, False, 70, 4, 1, 1000),
+    ("f32", 64, 16, True, 33, 2, 2, 300),
+    ("f32", 64, 64, False, 5, 5, 1, 40),
+    ("f32", 128, 112, False, 129, 2, 1, 200000),
+    ("bf16", 64, 32, True, 200, 6, 2, 4000),
+])
+@pytest.mark.parametrize("major", ["head", "token"])
+def test_rotation(K, dtype, d, r, pairs, T, Hq, Hkv, P, major):
+    """Keys are held, and queries given, as the nearest to the exact rotation; positions in any order, those outside
+    the table make NaN rows."""
+    L, B, page = 2, 3, 64
+    rng = np.random.default_rng(T)
+
+    def rows(H, seed):
+        x = normal((L, B, H, T, d) if major == "head" else (L, B, T, H, d), dtype, seed, 3.0).cuda()
+        return x if major == "head" else x.permute(0, 1, 3, 2, 4)
+    k, v, q = rows(Hkv, 1), rows(Hkv, 2), rows(Hq, 3)
+    freq = 10000.0 ** (-np.arange(r // 2) / (r // 2))
+    angle = torch.arange(P, dtype=torch.float64)[:, None] * torch.from_numpy(freq)
+    cos, sin = torch.cos(angle).float(), torch.sin(angle).float()
+    pos = rng.integers(0, P, (B, T))
+    pos[0, 0], pos[0, -1], pos[1, 0], pos[2, -1] = P - 1, 0, -1, P
+    M = T // page + 3
+    cache = make(K, L, Hkv, d, page, B * M, B, M)
+    K.pages_extend(cache, dev([5, 0, 63]))
+    old = normal((L, B, Hkv, 63, d), dtype, 9).cuda()
+    K.blocks_append(old, old, cache, dev([0, 0, 0]), n_new=dev([5, 0, 63]))
+    start, _ = K.pages_extend(cache, dev([T] * B))
+    out = torch.full((L, B, Hq, T, d), float("inf"), dtype=TORCH[dtype], device="cuda")
+    got = K.blocks_append(k, v, cache, start, rotation=K.Rotation(cos.cuda(), sin.cuda(), pairs), position=dev(pos), q=q,
+                          q_out=out)
+    assert got is out
+    m = Model(cache)
+    cn, sn = cos.double().numpy(), sin.double().numpy()
+    bits = 8 if dtype == "bf16" else 24
+    for b in range(B):
+        n0 = [5, 0, 63][b]
+        m.write(b, 0, host(old)[:, b, :, :n0], host(old)[:, b, :, :n0])
+        m.write(b, n0, O.rotate(host(k)[:, b], cn, sn, pos[b], pairs), host(v)[:, b])
+        m.same(b, n0 + T)
+        want = O.round_to(O.rotate(host(q)[:, b], cn, sn, pos[b], pairs), bits)
+        assert np.array_equal(host(out)[:, b], want, equal_nan=True)
+    # without queries, the same cache
+    again = make(K, L, Hkv, d, page, B * M, B, M)
+    K.pages_extend(again, dev([5, 0, 63]))
+    K.blocks_append(old, old, again, dev([0, 0, 0]), n_new=dev([5, 0, 63]))
+    K.pages_extend(again, dev([T] * B))
+    assert K.blocks_append(k, v, again, start, rotation=K.Rotation(cos.cuda(), sin.cuda(), pairs), position=dev(pos)) is None
+    assert torch.equal(again.pool, cache.pool)
+
+
+def test_append_drops_what_has_no_place(K):
+    """Refused starts, positions without a page, page numbers outside the pool, slots outside: nothing is written there,
+    and nothing but the rows' blocks anywhere."""
+    L, Hkv, d, page = 1, 2, 64, 32
+    cache, _, _ = filled(K, L, Hkv, d, page, [40, 10, 33, 5], spare=4)
+    cache.table[2, 1] = 1 << 30
+    cache.table[3, 0] = -5
+    cache.held[1] = 1 << 30                                          # more than the table's row: cut to it
+    before = cache.pool.clone()
+    T = 70
+    x = normal((L, 6, Hkv, T, d), "bf16", 9).cuda()
+    K.blocks_append(x, x, cache, dev([-1, 60, 20, 0, 0, (1 << 31) - 1]), seq=dev([0, 1, 2, 3, 4, 0]),
+                    n_new=dev([70, 2, 30, 30, 9, 70]))
+    torch.cuda.synchronize()
+    changed = (before != cache.pool).any(-1)[0].cpu().numpy()        # [n_pages, Hkv]
+    allowed = {int(cache.table[2, 0])} | {int(x) for x in cache.table[1, 1:3].tolist() if 0 <= x < cache.c.n_pages}
+    assert set(np.nonzero(changed.any(1))[0].tolist()) <= allowed
+    assert changed[int(cache.table[2, 0])].all()
+    before = cache.pool.clone()
+    K.blocks_append(x, x, cache, dev([0] * 6), seq=dev([-1, 4, 1 << 30, -(1 << 31), 0, 0]), n_new=dev([70, 70, 70, 70, 0, -3]))
+    assert torch.equal(before, cache.pool)
+
+
+CASES = [  # L, B, Hkv, N, d, page, cap, dtype
+    (1, 1, 1, 1, 64, 32, 1, "bf16"),
+    (2, 3, 2, 77, 128, 32, 50, "bf16"),
+    (1, 2, 3, 400, 64, 128, 300, "bf16"),
+    (1, 2, 2, 150, 128, 64, 149, "f32"),
+    (2, 1, 1, 333, 64, 64, 200, "f32"),
+]
+
+
+@pytest.mark.parametrize("L,B,Hkv,N,d,page,cap,dtype", CASES)
+@pytest.mark.parametrize("major", ["head", "token"])
+def test_compact(K, L, B, Hkv, N, d, page, cap, dtype, major):
+    r = np.random.default_rng(N)
+    shape = (L, B, Hkv, N, d) if major == "head" else (L, B, N, Hkv, d)
+    k, v = normal(shape, dtype, 1).cuda(), normal(shape, dtype, 2).cuda()
+    if major == "token":
+        k, v = k.permute(0, 1, 3, 2, 4), v.permute(0, 1, 3, 2, 4)
+    S, M = B + 2, -(-(cap + 37) // page) + 1
+    cache = make(K, L, Hkv, d, page, B * M + 2, S, M, seed=3)
+    slots = r.permutation(S)[:B]
+    seq = dev(slots)
+    have = r.integers(0, 37, B)
+    K.pages_extend(cache, dev(have), seq=seq)                        # some rows are there already
+    old = normal((L, B, Hkv, 40, d), dtype, 5, 0.3).cuda()
+    K.blocks_append(old, old, cache, dev([0] * B), n_new=dev(have), seq=seq)
+    start, _ = K.pages_extend(cache, dev([cap] * B), seq=seq)
+    idx = np.stack([np.sort(r.permutation(N)[:cap]) for _ in range(L * B * Hkv)]).reshape(L, B, Hkv, cap)
+    count = np.full((L, B, Hkv), cap)
+    count[-1, -1, -1] = cap + 9                                      # more than the row holds: cut
+    if cap > 8:
+        idx[0, -1, 0, 2], idx[0, -1, 0, 5] = -1, N                   # rows of zeros
+    K.blocks_compact(k, v, dev(idx), dev(count), cache, start, seq=seq)
+    m = Model(cache)
+    kn, vn = host(k), host(v)
+    for b in range(B):
+        m.write(int(slots[b]), 0, host(old)[:, b, :, :have[b]], host(old)[:, b, :, :have[b]])
+        rows = []
+        for x in (kn, vn):
+            t = idx[:, b][..., None]
+            got = np.take_along_axis(x[:, b], np.clip(t, 0, N - 1), axis=2)
+            rows.append(np.where((t >= 0) & (t < N), got, 0.0))
+        m.write(int(slots[b]), int(start[b]), *rows)
+        m.same(int(slots[b]), int(start[b]) + cap)
+
+
+def test_compact_counts_differ(K):
+    """A head with fewer rows leaves the positions behind them as they were."""
+    cache = make(K, 1, 2, 64, 32, 4, 1, 4)
+    start, _ = K.pages_extend(cache, dev([40]))
+    k, v = normal((1, 1, 2, 50, 64), "bf16", 1).cuda(), normal((1, 1, 2, 50, 64), "bf16", 2).cuda()
+    idx = dev(np.tile(np.arange(40), (1, 1, 2, 1)))
+    K.blocks_compact(k, v, idx, dev([[[40, 33]]]), cache, start)
+    m = Model(cache)
+    m.at(0, 0, 0).write(0, host(k)[0, 0, 0, :40], host(v)[0, 0, 0, :40])
+    m.at(0, 0, 1).write(0, host(k)[0, 0, 1, :33], host(v)[0, 0, 1, :33])
+    m.same(0, 33)
+    K.blocks_compact(k, v, idx, dev([[[0, -1]]]), cache, start)
+    m.same(0, 33)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_read_ranges(K, dtype):
+    """Rows and blocks from anywhere; what a sequence lacks stays as it was."""
+    lengths, page, d = [100, 0, 33, 64], 32, 64
+    cache, k, v = filled(K, 2, 2, d, page, lengths, extra_slots=1)
+    cache.table[3, 1] = -7                                            # a page that is missing
+    seq = [2, 0, 4, 9, 3, 0, 1]
+    first, count, T = [5, 90, 0, 0, 10, -1, 0], [40, 3, 9, 9, 50, 9, 9], 50
+    mark = torch.full((2, 7, 2, T, d), 7.0, dtype=TORCH[dtype], device="cuda")
+    a, b = mark.clone(), mark.clone()
+    K.blocks_read(cache, T, seq=dev(seq), start=dev(first), count=dev(count), k_out=a, v_out=b)
+    for got, want in ((host(a), k), (host(b), v)):
+        for i, s in enumerate(seq):
+            n = lengths[s] if s < 4 else 0
+            for t in range(T):
+                p = first[i] + t
+                there = first[i] >= 0 and t < count[i] and p < n and not (s == 3 and 32 <= p < 64)
+                assert np.array_equal(got[:, i, :, t], want[:, s, :, p] if there else np.full((2, 2, d), 7.0)), (i, t)
+    nb, f = 4, [1, 2, 0, 0, 0, -1, 0]
+    a, b = mark[..., :nb, :].clone(), mark[..., :nb, :].clone()
+    K.blocks_bounds(cache, nb, seq=dev(seq), first=dev(f), lo_out=a, hi_out=b)
+    for i, s in enumerate(seq):
+        n = lengths[s] if s < 4 else 0
+        for t in range(nb):
+            blk = f[i] + t
+            there = f[i] >= 0 and blk * page < n and not (s == 3 and blk == 1)
+            rows = k[:, s, :, blk * page:min(n, (blk + 1) * page)] if there else None
+            assert np.array_equal(host(a)[:, i, :, t], rows.min(2) if there else np.full((2, 2, d), 7.0)), (i, t)
+            assert np.array_equal(host(b)[:, i, :, t], rows.max(2) if there else np.full((2, 2, d), 7.0)), (i, t)
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+
+def check(got, want, mag, top, n, d, what=""):
+    """The bound of float32 arithmetic.  A logit is a sum of d exact products (float32 queries: three of each) and a
+    softmax exponent: off by at most (d + 8) U of the magnitudes' sum `top`, and 6 U from exp2, its argument's
+    rounding aside; numerator and denominator feel that each, and the rounding of sums whose longest chain is n / 32
+    steps of a wave, 32 tokens within one, and 32 of merges."""
+    bound = (2 * ((d + 8) * top + 6) + 2 * (n / 32 + 64)) * U * mag + 1e-30
+    assert np.isfinite(got).all(), what
+    err = np.abs(got - want)
+    assert np.all(err <= bound), (what, float((err / bound).max()))
+    return float((err / bound).max())
+
+
+def check_decode(cache, k, v, q, out, lengths, order, most=None, start=None, top=None, scale=None, layers=None, samples=None):
+    """out against the oracle, everything float64: k, v [L, slots, Hkv, N, d], q and out [L, B, Hq, T, d]."""
+    L, B, Hq, T, d = q.shape
+    G, worst = Hq // cache.Hkv, 0.0
+    scale = 1.0 / np.sqrt(d) if scale is None else scale
+    most = cache.table.shape[1] * cache.page if most is None else most
+    for l in range(L) if layers is None else layers:
+        for i in range(B) if samples is None else samples:
+            s = int(order[i])
+            length = lengths[s] if 0 <= s < len(lengths) else 0
+            for t in range(T):
+                n = O.rows_seen(length, T, t, most, None if start is None else start[i])
+                for j in range(cache.Hkv):
+                    rows = np.arange(n)
+                    if top is not None:
+                        at = [b * cache.page + np.arange(cache.page) for b in top[l, i, j, t]
+                              if 0 <= b < cache.table.shape[1]]
+                        rows = np.concatenate(at + [np.zeros(0, dtype=np.int64)]).astype(np.int64)
+                        rows = rows[rows < n]
+                    hs = slice(j * G, (j + 1) * G)
+                    want, mag, x = O.attend(q[l, i, hs, t], k[l, s, j][rows] if n else np.zeros((0, d)),
+                                            v[l, s, j][rows] if n else np.zeros((0, d)), scale)
+                    worst = max(worst, check(out[l, i, hs, t], want, mag, x, len(rows), d, (l, i, t, j, len(rows))))
+    return worst
+
+
+@pytest.mark.parametrize("Hkv,G,d,page,lengths,T,most,dtype,qs", [
+    (2, 4, 128, 64, [0, 1, 2, 31, 32, 33, 63, 64, 65, 127, 300], 1, None, "bf16", 1.0),
+    (2, 1, 64, 32, [0, 1, 31, 32, 33, 95, 96, 97, 1000], 1, None, "bf16", 1.0),
+    (1, 8, 128, 128, [5, 128, 129, 700, 0], 1, 700, "bf16", 3.0),
+    (1, 16, 64, 64, [5, 64, 129, 1500], 1, 1501, "bf16", 1.0),
+    (3, 3, 128, 32, [77, 0, 500], 1, 400, "f32", 1.0),
+    (1, 5, 64, 128, [1, 200, 4000], 1, None, "f32", 1.0),
+    (1, 16, 128, 32, [130, 2100], 1, None, "f32", 0.01),
+    (2, 4, 128, 64, [0, 1, 3, 4, 5, 64, 66, 130, 700], 4, None, "bf16", 1.0),
+    (1, 1, 64, 32, [0, 1, 20, 33, 40, 300], 16, None, "bf16", 1.0),
+    (1, 3, 64, 32, [0, 2, 33, 40, 300], 7, 290, "f32", 1.0),           # five tokens to an entry, then two
+    (2, 16, 128, 64, [64, 65, 200], 3, None, "bf16", 1.0),
+    (1, 2, 128, 128, [5, 140, 900], 40, None, "bf16", 1.0),
+    (1, 8, 64, 64, [3, 30000], 2, None, "bf16", 1.0),
+    (1, 12, 128, 64, [9000], 1, None, "bf16", 2.0),
+])
+def test_decode(K, Hkv, G, d, page, lengths, T, most, dtype, qs):
+    L, B, Hq = (2 if max(lengths) < 5000 else 1), len(lengths), Hkv * G
+    cache, k, v = filled(K, L, Hkv, d, page, lengths, seed=G, extra_slots=1)
+    order = np.random.default_rng(G).permutation(B + 1)[:B]              # one of the slots may be the empty one
+    q = normal((L, B, Hq, T, d), dtype, 77, qs).cuda()
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    K.decode_blocks(q, cache, max_tokens=most, seq=dev(order), out=out)
+    k = np.concatenate([k, k[:, :1]], 1), np.concatenate([v, v[:, :1]], 1)
+    w = check_decode(cache, *k, host(q), host(out), lengths + [0], order, most=most)
+    report(f"block decode worst err/bound g{G} d{d} T{T} {dtype} x{qs:g}", round(w, 4))
+
+
+def test_decode_of_one_token_without_its_axis(K):
+    cache, k, v = filled(K, 1, 2, 128, 64, [100, 200])
+    q = normal((1, 2, 6, 128), "bf16", 1).cuda()
+    a, b = K.decode_blocks(q, cache), K.decode_blocks(q[:, :, :, None].contiguous(), cache)
+    assert a.shape == q.shape and torch.equal(a, b[:, :, :, 0])
+    assert torch.equal(K.blocks_top(q, cache, 2), K.blocks_top(q[:, :, :, None].contiguous(), cache, 2))
+
+
+@pytest.mark.parametrize("T,G,start", [(5, 2, [0, 3, 60, 95, -1, 200]), (1, 4, [0, 10, 99, 98, -5, (1 << 31) - 1]),
+                                       (3, 16, [0, 31, 63, 97, -1, 1 << 30])])
+def test_decode_behind_given_starts(K, T, G, start):
+    """Drafts of different lengths behind a padded append: token t sees start + t + 1 rows at most."""
+    lengths = [100, 4, 62, 100, 50, 100]
+    cache, k, v = filled(K, 1, 2, 64, 32, lengths)
+    q = normal((1, 6, 2 * G, T, 64), "bf16", 8).cuda()
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    K.decode_blocks(q, cache, start=dev(start), out=out)
+    check_decode(cache, k, v, host(q), host(out), lengths, range(6), start=start)
+    top = K.blocks_top(q, cache, 2, start=dev(start))
+    out.fill_(float("nan"))
+    K.decode_blocks(q, cache, start=dev(start), top=top, out=out)
+    check_decode(cache, k, v, host(q), host(out), lengths, range(6), start=start, top=top.cpu().numpy())
+
+
+@pytest.mark.parametrize("G,d", [(1, 64), (4, 128), (8, 64), (16, 128)])
+def test_decode_of_large_values_under_rising_logits(K, G, d):
+    """Each token's logit is above the one before, by 90 in all, over values around 2^100."""
+    n = 500
+    cache, _, _ = filled(K, 1, 1, d, 32, [n], seed=G)
+    k = torch.zeros((1, 1, 1, n, d))
+    k[..., 0] = torch.linspace(0.5, 6.0, n)
+    v = normal((1, 1, 1, n, d), "f32", 5, 2.0 ** 100)
+    K.blocks_append(k.cuda(), v.cuda(), cache, dev([0]))
+    q = torch.zeros((1, 1, G, 1, d))
+    q[..., 0] = 15.0 * np.sqrt(d)
+    q[..., 1:] = normal((1, 1, G, 1, d - 1), "f32", 6)
+    q = q.bfloat16().cuda()
+    kk, vv = (host(x) for x in K.blocks_read(cache, n, dtype=torch.float32))
+    check_decode(cache, kk, vv, host(q), host(K.decode_blocks(q, cache)), [n], [0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,d,n,drowned,most", [(1, 64, 150, 70, None), (4, 128, 150, 70, 150), (8, 64, 600, 520, None),
+                                                (16, 128, 3000, 2500, None), (3, 128, 40, 39, 40)])
+def test_decode_of_logits_below_float32(K, G, d, n, drowned, most, dtype):
+    """The first `drowned` logits leave float32 downwards: they have no weight, and the others share it."""
+    cache, _, _ = filled(K, 1, 1, d, 32, [n], seed=G)
+    k = torch.zeros((1, 1, 1, n, d))
+    k[..., :drowned, 0] = -6.0
+    v = normal((1, 1, 1, n, d), "f32", 5)
+    K.blocks_append(k.cuda(), v.cuda(), cache, dev([0]))
+    q = torch.zeros((1, 1, G, d))
+    q[..., 0] = 2.0 ** 127
+    out = host(K.decode_blocks(q.to(TORCH[dtype]).cuda(), cache, max_tokens=most))
+    rest = host(K.blocks_read(cache, n, dtype=torch.float32)[1])[0, 0, 0, drowned:]
+    check(out[0, 0], np.tile(rest.mean(0), (G, 1)), np.tile(np.abs(rest).mean(0), (G, 1)), 0.0, n, d)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,d", [(1, 64), (2, 128), (4, 64), (5, 128), (8, 128), (9, 64), (16, 128)])
+def test_decode_keeps_all_bits_of_the_weights(K, G, d, dtype):
+    """Results that hang on the low bits of the weights and of float32 queries, at the bound of float32."""
+    from tests import paged_decode_cases as C
+    for n, at in ((40, (3, 17)), (300, (5, 290)), (3000, (100, 2900))):
+        q, k, v, want = C.case(G, d, dtype, n, at)
+        cache = make(K, 1, 1, d, 32, n // 32 + 2, 1, n // 32 + 2)
+        start, _ = K.pages_extend(cache, dev([n]))
+        K.blocks_append(torch.from_numpy(k).float()[None, None, None].cuda(),
+                        torch.from_numpy(v).float()[None, None, None].cuda(), cache, start)
+        gk, gv = K.blocks_read(cache, n, dtype=torch.float32)
+        assert np.array_equal(host(gk)[0, 0, 0], k) and np.array_equal(host(gv)[0, 0, 0], v)
+        qt = torch.from_numpy(q).to(TORCH[dtype])[None, None].cuda()
+        for most in (n, None):
+            got = host(K.decode_blocks(qt, cache, max_tokens=most, scale=1.0))[0, 0]
+            assert np.abs(got - want).max() <= C.BOUND, (n, most)
+        every = dev(np.arange(-(-n // 32)))[None, None, None, None]
+        got = host(K.decode_blocks(qt, cache, max_tokens=n, scale=1.0, top=every))[0, 0]
+        assert np.abs(got - want).max() <= C.BOUND, n
+
+
+def test_decode_leaves_out_missing_pages_and_passes_nan_on(K):
+    Hkv, G, d, page = 2, 4, 128, 32
+    lengths = [100, 100, 100, 100, 20]
+    cache, k, v = filled(K, 1, Hkv, d, page, lengths)
+    q = normal((1, 5, Hkv * G, 1, d), "bf16", 4).cuda()
+    cache.table[0, 1] = -1
+    cache.table[1, 0], cache.table[1, 3] = cache.c.n_pages, 1 << 30
+    cache.table[2, :4] = -1
+    cache.pool[0, int(cache.table[3, 2]), 0, 5 * d + 9] = 0x7F               # a key of KV head 0
+    cache.pool[0, int(cache.table[4, 0]), 1, page * d + 7 * d + 3] = 0xFF    # a value of head 1
+    out = host(K.decode_blocks(q, cache))[0, :, :, 0]
+    qn = host(q)[0, :, :, 0]
+    keep = [np.r_[0:32, 64:100], np.r_[32:96], np.r_[0:0], np.r_[0:100], np.r_[0:20]]
+    for s in range(5):
+        for j in range(Hkv):
+            hs = slice(j * G, (j + 1) * G)
+            if (s, j) == (3, 0):
+                assert np.isnan(out[s, hs]).all()
+                continue
+            want, mag, x = O.attend(qn[s, hs], k[0, s, j][keep[s]], v[0, s, j][keep[s]], 1 / np.sqrt(d))
+            got = out[s, hs]
+            if (s, j) == (4, 1):
+                assert np.isnan(got[:, 3]).all()
+                got, want, mag = (np.delete(a, 3, 1) for a in (got, want, mag))
+            check(got, want, mag, x, 100, d, (s, j))
+
+
+@pytest.mark.parametrize("G,T,most", [(2, 8, None), (4, 4, 130), (3, 5, None), (1, 16, 130), (5, 6, None)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masked_rows_of_any_content_do_not_matter(K, G, T, most, dtype):
+    """A row of NaN keys and values that a later draft brought, and bytes behind the sequence: tokens that do not see
+    them give what they gave."""
+    d, page, n = 64, 32, 130
+    cache, k, v = filled(K, 1, 1, d, page, [n])
+    q = normal((1, 1, G, T, d), dtype, 5).cuda()
+    clean = host(K.decode_blocks(q, cache, max_tokens=most))
+    check_decode(cache, k, v, host(q), clean, [n], [0], most=most)
+    last, tail = int(cache.table[0, 3]), int(cache.table[0, 4])
+    cache.pool[0, tail, 0, 2 * d:page * d] = 0x7F                        # keys and values of rows 130 on
+    cache.pool[0, tail, 0, (page + 2) * d:2 * page * d] = 0xFF
+    assert np.array_equal(host(K.decode_blocks(q, cache, max_tokens=most)), clean)
+    cache.pool[0, last, 0, 31 * d + 4] = 0x7F                            # row 127, which the last three tokens see
+    cache.pool[0, last, 0, (page + 31) * d:(page + 32) * d] = 0xFF
+    out = host(K.decode_blocks(q, cache, max_tokens=most))
+    assert np.isnan(out[..., T - 3:, :]).all() and np.array_equal(out[..., :T - 3, :], clean[..., :T - 3, :])
+    cache.pool[0, last, 0, 31 * d + 4] = 0                               # its values alone
+    out = host(K.decode_blocks(q, cache, max_tokens=most))
+    assert np.isnan(out[..., T - 3:, :]).all() and np.array_equal(out[..., :T - 3, :], clean[..., :T - 3, :])
+
+
+@pytest.mark.parametrize("L,B,Hkv,G,page,longest,most,T", [
+    (1, 150, 1, 2, 32, 700, None, 1),     # more sequences than a wave has lanes, several splits each
+    (1, 64, 2, 4, 64, 200, 200, 1),
+    (130, 2, 8, 1, 64, 2300, None, 1),    # more (layer, KV head) pairs than resident workgroups
+    (40, 30, 1, 4, 128, 1100, 1100, 1),
+    (3, 50, 2, 4, 32, 500, 500, 2),
+    (2, 100, 1, 11, 64, 300, 320, 1),
+    (1, 90, 1, 8, 32, 2000, 2048, 3),
+])
+def test_decode_of_many_sequences_and_pairs(K, L, B, Hkv, G, page, longest, most, T):
+    """Ragged lengths with empty sequences among them, slots named twice and in any order."""
+    r = np.random.default_rng(B)
+    d, Hq = 64, Hkv * G
+    lengths = [longest] + [int(r.integers(0, longest + 1)) if r.random() < 0.8 else 0 for _ in range(B - 1)]
+    cache, k, v = filled(K, L, Hkv, d, page, lengths, seed=B)
+    order = np.concatenate([r.permutation(B)[:B - 1], [0]])
+    q = normal((L, B, Hq, T, d), "bf16", 78).cuda()
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    K.decode_blocks(q, cache, max_tokens=most, seq=dev(order), out=out)
+    check_decode(cache, k, v, host(q), host(out), lengths, order, most=most, layers=sorted({0, L // 2, L - 1}))
+    assert torch.isfinite(out).all()
+
+
+def test_decode_of_thousands_of_samples(K):
+    """More samples than lengths are kept in LDS for, on few slots, some of them outside the cache, beside long ones."""
+    B, G, d = 4500, 2, 64
+    lengths = [2600, 1, 0, 33, 300, 64, 900]
+    cache, k, v = filled(K, 1, 1, d, 32, lengths)
+    r = np.random.default_rng(8)
+    order = r.integers(-1, len(lengths) + 1, B)
+    order[[0, 63, 64, B - 1]] = 0
+    q = normal((1, B, G, 1, d), "bf16", 79).cuda()
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    K.decode_blocks(q, cache, seq=dev(order), out=out)
+    assert torch.isfinite(out).all()
+    some = sorted({0, 1, 62, 63, 64, 65, B - 2, B - 1, *r.integers(0, B, 150).tolist()})
+    check_decode(cache, k, v, host(q), host(out), lengths, order, samples=some)
+
+
+# ---------------------------------------------------------------------------
+# block choice
+# ---------------------------------------------------------------------------
+
+def want_top(cache, q, lengths, order, k, first, last, most=None, start=None, missing=()):
+    """The oracle's choice from the cache's own bounds; missing: (slot, block) without a page."""
+    L, B, Hq, T, d = q.shape
+    G = Hq // cache.Hkv
+    most = cache.table.shape[1] * cache.page if most is None else most
+    lo, hi = (host(x) for x in
+              cache_bounds(cache, max(1, max(-(-n // cache.page) for n in lengths)), len(lengths)))
+    out = np.full((L, B, cache.Hkv, T, k), -1)
+    for i in range(B):
+        s = int(order[i])
+        length = lengths[s] if 0 <= s < len(lengths) else 0
+        for t in range(T):
+            nb = -(-O.rows_seen(length, T, t, most, None if start is None else start[i]) // cache.page)
+            if nb == 0:
+                continue
+            gone = [b for x, b in missing if x == s]
+            for l in range(L):
+                for j in range(cache.Hkv):
+                    sc = O.block_scores(q[l, i, j * G:(j + 1) * G, t], lo[l, s, j, :nb], hi[l, s, j, :nb])
+                    out[l, i, j, t] = O.top_blocks(sc, k, first, last, gone)
+    return out
+
+
+def same_top(top, want, what=""):
+    got = top.cpu().numpy()
+    assert got.shape == want.shape, what
+    bad = np.argwhere((got != want).any(-1))
+    if len(bad):
+        at = tuple(bad[0])
+        raise AssertionError(f"{what}: {len(bad)} lists differ; {at}: {got[at].tolist()[:40]} != {want[at].tolist()[:40]}")
+
+
+def cache_bounds(cache, nb, slots):
+    import paper_2607_13205_amd as K
+    return K.blocks_bounds(cache, nb, seq=dev(range(slots)), dtype=torch.float32)
+
+
+@pytest.mark.parametrize("Hkv,G,d,page,lengths,T,k,first,last,most,dtype", [
+    (2, 4, 128, 32, [0, 1, 32, 33, 300, 1000], 1, 4, 1, 1, None, "bf16"),
+    (1, 1, 64, 64, [64, 65, 2000, 700], 1, 1, 0, 0, None, "f32"),
+    (3, 2, 64, 32, [900, 31, 96], 3, 5, 0, 2, None, "bf16"),
+    (1, 8, 128, 128, [5000, 0, 129], 2, 7, 2, 0, 4000, "f32"),
+    (1, 5, 64, 32, [40000], 1, 64, 1, 1, None, "bf16"),          # more blocks than a workgroup has threads
+    (2, 16, 128, 32, [500, 17], 1, 40, 3, 4, None, "bf16"),      # more than there are
+    (1, 20, 64, 32, [1500], 1, 9, 1, 1, None, "bf16"),           # heads beyond what decode takes
+])
+def test_top(K, Hkv, G, d, page, lengths, T, k, first, last, most, dtype):
+    L, B, Hq = 2, len(lengths), Hkv * G
+    cache, _, _ = filled(K, L, Hkv, d, page, lengths, seed=G)
+    order = np.random.default_rng(k).permutation(B)
+    q = normal((L, B, Hq, T, d), dtype, 31).cuda()
+    top = K.blocks_top(q, cache, k, first=first, last=last, max_tokens=most, seq=dev(order))
+    same_top(top, want_top(cache, host(q), lengths, order, k, first, last, most))
+
+
+def test_top_ties_nan_and_missing_pages(K):
+    """Equal scores go to the lower block, NaN and missing ones come last, forced ones first."""
+    d, page, n = 64, 32, 32 * 300
+    cache, _, _ = filled(K, 1, 1, d, page, [n, n])
+    x = torch.zeros((1, 2, 1, n, d))
+    x[:, :, :, :, 0] = (torch.arange(n) // page % 3).float()          # three values, a hundred blocks each
+    K.blocks_append(x.cuda(), x.cuda(), cache, dev([0, 0]))
+    q = torch.zeros((1, 2, 2, 1, d))
+    q[..., 0] = 1.0
+    q[0, 1] *= -0.0                                                    # all scores zero
+    q = q.bfloat16().cuda()
+    for k, first, last in ((50, 0, 0), (130, 1, 1), (250, 3, 0), (299, 0, 2), (2, 1, 1)):
+        top = K.blocks_top(q, cache, k, first=first, last=last)
+        same_top(top, want_top(cache, host(q), [n, n], [0, 1], k, first, last), k)
+    assert K.blocks_top(q, cache, 5, first=0, last=0)[0, 1, 0, 0].tolist() == [0, 1, 2, 3, 4]
+    gone = [(0, 2), (0, 5), (0, 299), (1, 0)]
+    for s, b in gone:
+        cache.table[s, b] = -1 if b % 2 else 1 << 30
+    cache.pool[0, int(cache.table[0, 8]), 0, 2 * page * d + 128] = 0x7F   # a NaN among the bounds of block 8
+    for k, first, last in ((60, 0, 0), (4, 0, 1), (298, 0, 0), (297, 0, 0)):
+        top = K.blocks_top(q, cache, k, first=first, last=last)
+        same_top(top, want_top(cache, host(q), [n, n], [0, 1], k, first, last, missing=gone), k)
+    qn = q.clone()
+    qn[0, 0, 1, 0, 7] = float("nan")
+    assert K.blocks_top(qn, cache, 3, first=0, last=1)[0, 0, 0, 0].tolist() == [0, 1, 299]
+
+
+@pytest.mark.parametrize("Hkv,G,d,page,lengths,T,k,dtype", [
+    (2, 4, 128, 32, [0, 1, 33, 300, 2000], 1, 5, "bf16"),
+    (1, 8, 128, 64, [9000, 64, 65], 1, 30, "bf16"),
+    (2, 3, 64, 32, [700, 900], 4, 6, "f32"),
+    (1, 16, 64, 128, [3000, 100], 2, 4, "bf16"),
+    (1, 1, 128, 32, [20000], 1, 100, "f32"),
+])
+def test_decode_over_chosen_blocks(K, Hkv, G, d, page, lengths, T, k, dtype):
+    L, B, Hq = 2, len(lengths), Hkv * G
+    cache, kk, vv = filled(K, L, Hkv, d, page, lengths, seed=G)
+    order = np.random.default_rng(k).permutation(B)
+    q = normal((L, B, Hq, T, d), dtype, 31).cuda()
+    for most in (None, max(lengths)):
+        top = K.blocks_top(q, cache, k, max_tokens=most, seq=dev(order))
+        out = torch.full(q.shape, float("nan"), device="cuda")
+        K.decode_blocks(q, cache, max_tokens=most, seq=dev(order), top=top, out=out)
+        check_decode(cache, kk, vv, host(q), host(out), lengths, order, most=most, top=top.cpu().numpy())
+    full = -(-max(lengths) // page)
+    every = K.blocks_top(q, cache, full, seq=dev(order))
+    check_decode(cache, kk, vv, host(q), host(K.decode_blocks(q, cache, seq=dev(order), top=every)), lengths, order)
+
+
+def test_decode_over_lists_of_any_content(K):
+    """Holes, blocks that the sequence or the table lacks, blocks named twice, any order."""
+    lengths, page = [200, 100, 70], 32
+    cache, kk, vv = filled(K, 1, 2, 64, page, lengths)
+    q = normal((1, 3, 4, 2, 64), "bf16", 3).cuda()
+    r = np.random.default_rng(1)
+    for k in (1, 3, 40):
+        top = r.choice([-1, 0, 1, 2, 3, 4, 5, 6, 7, 8, 1 << 30, -(1 << 31), 2], (1, 3, 2, 2, k))
+        top[0, 0, 0, 0] = -1                                            # nothing
+        out = torch.full(q.shape, float("nan"), device="cuda")
+        K.decode_blocks(q, cache, top=dev(top), out=out)
+        check_decode(cache, kk, vv, host(q), host(out), lengths, range(3), top=top)
+        assert not out[0, 0, :2, 0].any()
+
+
+# ---------------------------------------------------------------------------
+# the calls together
+# ---------------------------------------------------------------------------
+
+def test_corrupt_bookkeeping_stays_in_bounds(K):
+    """Lengths, held counts and tables of any content: every call returns, and writes nothing outside its outputs."""
+    r = np.random.default_rng(2)
+    L, Hkv, d, page, S, M, n_pages = 2, 2, 64, 32, 6, 5, 9
+    odd = np.array([0, 1, -1, 5, 40, 1 << 30, -(1 << 31), (1 << 31) - 1])
+    for seed in range(6):
+        cache = make(K, L, Hkv, d, page, n_pages, S, M, seed)
+        cache.table.copy_(dev(r.choice(np.concatenate([odd, np.arange(9)]), (S, M))))
+        cache.held.copy_(dev(r.choice(odd, S)))
+        cache.length.copy_(dev(r.choice(odd, S)))
+        seq, start = dev(r.choice(np.arange(-1, 7), 4)), dev(r.choice(odd, 4))
+        x = normal((L, 4, Hkv, 50, d), "bf16", seed).cuda()
+        q = normal((L, 4, 6, 3, d), "bf16", seed).cuda()
+        K.blocks_append(x, x, cache, start, n_new=dev(r.choice(odd, 4)), seq=seq)
+        K.blocks_compact(x, x, dev(r.choice(odd, (L, 4, Hkv, 50))), dev(r.choice(odd, (L, 4, Hkv))), cache, start, seq=seq)
+        K.blocks_read(cache, 70, seq=seq, start=start, count=dev(r.choice(odd, 4)))
+        K.blocks_bounds(cache, 9, seq=seq, first=start)
+        top = K.blocks_top(q, cache, 3, seq=seq, start=start)
+        assert int(top.max()) < M and int(top.min()) >= -1
+        K.decode_blocks(q, cache, seq=seq, start=start)
+        K.decode_blocks(q, cache, seq=seq, start=start, top=dev(r.choice(odd, (L, 4, Hkv, 3, 4))))
+        torch.cuda.synchronize()
+
+
+def test_captured_decode_loop(K):
+    """Room, append with rotation, choice and attention, layer after layer, captured once and replayed: every step is
+    the eager one's, with the program's own work between the replays."""
+    L, B, Hq, Hkv, d, page = 2, 3, 8, 2, 128, 32
+    lengths, steps = [70, 5, 500], 40
+    P = 700
+    angle = torch.arange(P, dtype=torch.float64)[:, None] * 1000.0 ** (-torch.arange(64) / 64.0)
+    rot = K.Rotation(torch.cos(angle).float().cuda(), torch.sin(angle).float().cuda())
+
+    def build():
+        cache, _, _ = filled(K, L, Hkv, d, page, lengths, spare=12)
+        pos = dev(lengths)[:, None].contiguous()
+        one = torch.ones(B, dtype=torch.int32, device="cuda")
+        x = [torch.zeros((L, B, h, 1, d), dtype=torch.bfloat16, device="cuda") for h in (Hkv, Hkv, Hq)]
+        start, missing = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        ws = torch.empty(K.pages_workspace_size(cache.c.n_pages, cache.c.S, B), dtype=torch.uint8, device="cuda")
+        wd = torch.empty(K.decode_blocks_workspace_size(1, B, Hq, Hkv, 1, d), dtype=torch.uint8, device="cuda")
+        wt = torch.empty(K.blocks_top_workspace_size(1, B, Hkv, 1, cache.c.M * page, page), dtype=torch.uint8, device="cuda")
+        outs = [[torch.zeros((1, B, Hq, 1, d), device="cuda") for _ in range(2)] for _ in range(L)]
+        tops = [torch.zeros((1, B, Hkv, 1, 3), dtype=torch.int32, device="cuda") for _ in range(L)]
+        qo = [torch.zeros((1, B, Hq, 1, d), dtype=torch.bfloat16, device="cuda") for _ in range(L)]
+        layers = [cache.layers(l, l + 1) for l in range(L)]
+
+        def step():
+            K.pages_extend(cache, one, start=start, missing=missing, workspace=ws)
+            for l in range(L):
+                K.blocks_append(x[0][l:l + 1], x[1][l:l + 1], layers[l], start, rotation=rot, position=pos,
+                                q=x[2][l:l + 1], q_out=qo[l])
+                K.blocks_top(qo[l], layers[l], 3, out=tops[l], workspace=wt)
+                K.decode_blocks(qo[l], layers[l], top=tops[l], out=outs[l][0], workspace=wd)
+                K.decode_blocks(qo[l], layers[l], out=outs[l][1], workspace=wd)
+            pos.add_(1)
+        return cache, x, step, outs, tops
+    eager, graph = build(), build()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        graph[2]()
+    for i in range(steps):
+        new = [normal(t.shape, "bf16", 1000 + 3 * i + e, 1.0 + i / 10) for e, t in enumerate(eager[1])]
+        for b in (eager, graph):
+            for t, y in zip(b[1], new):
+                t.copy_(y)
+        eager[2]()
+        g.replay()
+        if i % 3 == 0:
+            torch.cuda.synchronize()
+            torch.randn(1000, 1000, device="cuda").sum().item()
+        for l in range(L):
+            assert torch.equal(eager[4][l], graph[4][l]) and torch.equal(eager[3][l][1], graph[3][l][1]), i
+            assert torch.equal(eager[3][l][0], graph[3][l][0]) and torch.isfinite(eager[3][l][0]).all(), i
+    assert eager[0].length.tolist() == [n + steps for n in lengths]
+    used = eager[0].refs.bool()
+    assert torch.equal(used, graph[0].refs.bool())
+    for s, n in enumerate(lengths):
+        a, b = (K.blocks_read(c, n + steps, seq=dev([s])) for c in (eager[0], graph[0]))
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_calls_on_another_stream(K):
+    """Everything on a stream of its own, outputs and workspaces made by the calls among it, equals the current one."""
+    lengths = [300, 70]
+    cache, _, _ = filled(K, 1, 2, 64, 32, lengths, spare=8)
+    q, k = normal((1, 2, 4, 1, 64), "bf16", 1).cuda(), normal((1, 2, 2, 1, 64), "bf16", 2).cuda()
+    cos, sin = torch.ones((400, 32), device="cuda"), torch.zeros((400, 32), device="cuda")
+    rot, pos = K.Rotation(cos, sin), dev([[300], [70]])
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    start, _ = K.pages_extend(cache, dev([1, 1]), stream=s)
+    qo = K.blocks_append(k, k, cache, start, rotation=rot, position=pos, q=q, stream=s)
+    top = K.blocks_top(qo, cache, 4, stream=s)
+    a = K.decode_blocks(qo, cache, top=top, stream=s)
+    b = K.decode_blocks(qo, cache, stream=s)
+    r = K.blocks_read(cache, 301, stream=s)
+    lo, hi = K.blocks_bounds(cache, 10, stream=s)
+    s.synchronize()
+    assert torch.equal(qo, q)
+    assert torch.equal(top, K.blocks_top(q, cache, 4))
+    assert torch.equal(a, K.decode_blocks(q, cache, top=top)) and torch.equal(b, K.decode_blocks(q, cache))
+    assert all(torch.equal(x, y) for x, y in zip(r, K.blocks_read(cache, 301)))
+    assert all(torch.equal(x, y) for x, y in zip((lo, hi), K.blocks_bounds(cache, 10)))
+
+
+@pytest.mark.parametrize("chunks,dtype,d", [(1, "bf16", 128), (3, "bf16", 64), (1, "f32", 64)])
+def test_evict_into_blocks_keeps_the_rows_of_the_dense_step(K, chunks, dtype, d):
+    from paper_2607_13205_amd import pipeline
+    L, B, Hq, Hkv, N, W = 4, 2, 4, 2, 600, 16
+    r = np.random.default_rng(1)
+    q, k, v = (normal((L, B, h, n, d), dtype, i).cuda() for i, (h, n) in enumerate(((Hq, W), (Hkv, N), (Hkv, N))))
+    roles = r.integers(0, 4, (B, N)).astype(np.int8)
+    rd = torch.from_numpy(roles).cuda()
+    alpha, budget = (0.1, 0.4, 0.4, 0.1), 0.2
+    cap = 160
+    dense = pipeline.alloc_buffers(k, Hq, W, 4, cap)
+    pipeline.evict(q, k, v, roles, rd, alpha, budget, W, 5, dense)
+    cache = pipeline.alloc_blocks(L, Hkv, d, 20, 5, 400, page=32)
+    bufs = pipeline.alloc_buffers(k, Hq, W, 4, cap, pages=cache)
+    slots = dev([3, 1])
+    kw = dict(chunks=chunks, side_stream=torch.cuda.Stream()) if chunks > 1 else {}
+    _, kept = pipeline.evict(q, k, v, roles, rd, alpha, budget, W, 5, bufs, slots=slots, **kw)
+    assert cache.length.tolist() == [0, kept[1], 0, kept[0], 0] and bufs.missing.item() == 0
+    m = Model(cache)
+    for b, s in enumerate((3, 1)):
+        n = int(kept[b])
+        m.write(s, 0, host(dense.k_out)[:, b, :, :n], host(dense.v_out)[:, b, :, :n])
+        m.same(s, n)
+    K.pages_free(cache, slots)
+    assert not cache.refs.any() and not cache.length.any()
+
+
+@pytest.mark.parametrize("d,page", [(64, 32), (128, 128)])
+def test_blocks_beyond_four_gigabytes(K, d, page):
+    """Blocks at the pool's far end, a table and sources beyond 32-bit byte offsets."""
+    Hkv = 8
+    n_pages = (5 << 30) // (Hkv * K.block_bytes(page, d))
+    z = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    pool = torch.empty((1, n_pages, Hkv, K.block_bytes(page, d)), dtype=torch.uint8, device="cuda")
+    lengths = [300, 3 * page]
+    cache = K.Blocks(pool, z(n_pages), z(2, 12), z(2), z(2), page, d)
+    ids = [[n_pages - 1 - 3 * i for i in range(12)], [n_pages // 2 - i for i in range(12)]]
+    cache.table.copy_(dev(ids))
+    cache.held.copy_(dev([12, 12]))
+    cache.length.copy_(dev(lengths))
+    k, v = normal((1, 2, Hkv, 400, d), "bf16", 1).cuda(), normal((1, 2, Hkv, 400, d), "bf16", 2).cuda()
+    K.blocks_append(k, v, cache, dev([0, 0]), n_new=dev(lengths))
+    m = Model(cache)
+    for s in (0, 1):
+        m.write(s, 0, host(k)[:, s, :, :lengths[s]], host(v)[:, s, :, :lengths[s]])
+        m.same(s, lengths[s])
+    kk, vv = (host(x) for x in K.blocks_read(cache, 400, dtype=torch.float32))
+    q = normal((1, 2, 2 * Hkv, 1, d), "bf16", 3).cuda()
+    check_decode(cache, kk, vv, host(q), host(K.decode_blocks(q, cache)), lengths, [0, 1])
+    top = K.blocks_top(q, cache, 2)
+    same_top(top, want_top(cache, host(q), lengths, [0, 1], 2, 1, 1))
+    check_decode(cache, kk, vv, host(q), host(K.decode_blocks(q, cache, top=top)), lengths, [0, 1], top=top.cpu().numpy())

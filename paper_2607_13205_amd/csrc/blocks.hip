@@ -73,49 +73,80 @@ __device__ __forceinline__ float to_odd(double y) {
     return __uint_as_float(bits | 1u);
 }
 
-// Eight channels of a rotated row, exact to 53 bits.  row: its first byte; pos:
-// position, outside [0, P) for none.
-template <typename T, int D>
-struct Turn {
-    double y[8];
-    __device__ __forceinline__ void load(const char* row, int part, int pos, const BlockRotation& r) {
-        Eight<T> own;
-        own.template load<false>(row, part);
-        const bool there = pos >= 0 && pos < r.P;
-        const int half = r.r / 2;
-        if (8 * part >= r.r || !there) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = there ? (double)own.get(e) : (double)__uint_as_float(0x7fc00000u);
-            return;
-        }
-        const size_t base = (size_t)pos * half;
-        if (r.pairs) {
-            const f32x4 c = *reinterpret_cast<const f32x4*>(r.cos + base + 4 * part);
-            const f32x4 s = *reinterpret_cast<const f32x4*>(r.sin + base + 4 * part);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const double a = own.get(2 * i), b = own.get(2 * i + 1), co = c[i], si = s[i];
-                y[2 * i] = fma(a, co, -(b * si));
-                y[2 * i + 1] = fma(b, co, a * si);
-            }
-            return;
-        }
-        const int parts = half / 8;
-        const bool low = part < parts;
-        Eight<T> other;
-        other.template load<false>(row, low ? part + parts : part - parts);
-        const size_t at = base + 8 * (low ? part : part - parts);
-        f32x4 c[2], s[2];
+// A lane of a row takes two pieces of eight channels, `a` and `b`, which hold all
+// of its pairs.  The lanes' a, and their b, lie side by side where they can, so that a
+// load or store of a wave covers whole lines.
+struct Pieces {
+    int a, b;
+    bool turned;
+};
+
+template <int D>
+__device__ __forceinline__ Pieces pieces_of(int part, const BlockRotation& r, bool turn) {
+    const int n = turn ? r.r / 16 : 0;  // lanes whose pieces are turned
+    if (part >= n) return Pieces{n + part, D / 16 + part, false};
+    return r.pairs ? Pieces{2 * part, 2 * part + 1, true} : Pieces{part, part + n, true};
+}
+
+// The angles of a lane's eight pairs at a position; none outside [0, P).
+struct Angles {
+    f32x4 cos[2], sin[2];
+    bool there;
+    __device__ __forceinline__ void load(int part, int pos, const BlockRotation& r, bool turned) {
+        there = pos >= 0 && pos < r.P;
+        if (!turned || !there) return;
+        const size_t at = (size_t)pos * (r.r / 2) + 8 * part;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            c[i] = *reinterpret_cast<const f32x4*>(r.cos + at + 4 * i);
-            s[i] = *reinterpret_cast<const f32x4*>(r.sin + at + 4 * i);
+            cos[i] = *reinterpret_cast<const f32x4*>(r.cos + at + 4 * i);
+            sin[i] = *reinterpret_cast<const f32x4*>(r.sin + at + 4 * i);
         }
+    }
+};
+
+// Two pieces of a row.  Rounded: how a turned channel, exact to 53 bits, becomes a float.
+template <typename T>
+struct Sixteen {
+    Eight<T> a, b;
+    template <bool Once>
+    __device__ __forceinline__ void load(const char* row, const Pieces& at) {
+        a.template load<Once>(row, at.a);
+        b.template load<Once>(row, at.b);
+    }
+    __device__ __forceinline__ void floats(float (&x)[16]) const {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const double a = own.get(e), b = other.get(e), co = c[e / 4][e % 4], si = s[e / 4][e % 4];
-            y[e] = fma(a, co, low ? -(b * si) : b * si);
+            x[e] = a.get(e);
+            x[8 + e] = b.get(e);
         }
+    }
+    template <typename Rounded>
+    __device__ __forceinline__ void turn(const Angles& g, bool pairs, bool turned, Rounded rounded, float (&x)[16]) const {
+        floats(x);
+        if (!g.there) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(0x7fc00000u);
+            return;
+        }
+        if (!turned) return;
+        float y[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // pair i: channels i of the two pieces, or neighbours of one
+            const double u = pairs ? x[2 * i] : x[i], w = pairs ? x[2 * i + 1] : x[8 + i];
+            const double c = g.cos[i / 4][i % 4], s = g.sin[i / 4][i % 4];
+            const float lo = rounded(fma(u, c, -(w * s))), hi = rounded(fma(w, c, u * s));
+            y[i] = lo;
+            y[8 + i] = hi;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[2 * i] = pairs ? y[i] : x[2 * i];
+            x[2 * i + 1] = pairs ? y[8 + i] : x[2 * i + 1];
+        }
+        if (!pairs)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = y[e];
     }
 };
 
@@ -148,56 +179,102 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float factor) {
     return codes4(x[0], x[1], x[2], x[3], 1.0f);
 }
 
+// x of lane ^ 16, or ^ 32, beside x: the two results of a swap with itself hold both.
+template <typename F>
+__device__ __forceinline__ uint32_t over_halves(uint32_t x, F f) {
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return f(b[0], b[1]);
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
+}
+
+// Largest x of a wave, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    x = max(x, dpp<0xb1>(x));   // lanes 1 0 3 2
+    x = max(x, dpp<0x4e>(x));   // lanes 2 3 0 1
+    x = max(x, dpp<0x141>(x));  // mirrored within eight
+    x = max(x, dpp<0x140>(x));  // within sixteen
+    return over_halves(x, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+
+// f over the lanes of a wave that hold the same pieces of its rows, ROW lanes to a row.
+template <int ROW, typename F>
+__device__ __forceinline__ float over_rows(float x, F f) {
+    auto g = [&](uint32_t a, uint32_t b) { return __float_as_uint(f(__uint_as_float(a), __uint_as_float(b))); };
+    uint32_t y = __float_as_uint(x);
+    if constexpr (ROW == 4) y = g(y, dpp<0x124>(y));  // rotated by four, then by eight
+    y = g(y, dpp<0x128>(y));
+    return __uint_as_float(over_halves(y, g));
+}
+
 // What a call writes.
 struct WriteGrid {
-    int B, T, N, nblk, nq;       // nblk: blocks per segment; nq: rows of queries
-    unsigned blocks;             // workgroups that take blocks; those behind them take queries
+    int B, T, N, nblk, heads;  // nblk: blocks per segment; heads: of the queries
+    unsigned blocks, tokens;   // workgroups that take blocks, those behind them take queries; B T
 };
 
-// Row `in` of a step of kThreads / (D / 8).
 template <int D>
 struct Lanes {
-    static constexpr int kRow = D / 8;                // lanes to a row
-    static constexpr int kStep = kThreads / kRow;     // rows per step
-    static constexpr int kInWave = kWave / kRow;
+    static constexpr int kRow = D / 16;            // lanes to a row
+    static constexpr int kStep = kThreads / kRow;  // rows per step
 };
 
+// kHeads heads of the queries of Lanes::kStep tokens, whose angles are loaded once.
+template <typename T, int D>
+__device__ __forceinline__ void turn_queries(const RowView& view, char* out, const WriteGrid& g, unsigned x,
+                                             const BlockRotation& rot) {
+    using Ln = Lanes<D>;
+    const unsigned sets = (unsigned)(g.heads + kBlocksQueryHeads - 1) / kBlocksQueryHeads;
+    const unsigned y = x / sets, h0 = (x - y * sets) * kBlocksQueryHeads;
+    const unsigned groups = (g.tokens + Ln::kStep - 1) / Ln::kStep, l = y / groups;
+    const unsigned token = (y - l * groups) * Ln::kStep + threadIdx.x / Ln::kRow;
+    if (token >= g.tokens) return;
+    const int part = threadIdx.x % Ln::kRow;
+    const Pieces at = pieces_of<D>(part, rot, true);
+    const unsigned b = token / (unsigned)g.T, t = token - b * g.T;
+    const char* row = view.base + (size_t)l * view.s_layer + (size_t)b * view.s_batch + (size_t)t * view.s_token;
+    const int pos = rot.position[token];
+    Sixteen<T> raw[kBlocksQueryHeads];
+#pragma unroll
+    for (int h = 0; h < kBlocksQueryHeads; ++h)
+        raw[h].template load<false>(row + (size_t)min((int)h0 + h, g.heads - 1) * view.s_head, at);
+    Angles angles;
+    angles.load(part, pos, rot, at.turned);
+#pragma unroll
+    for (int h = 0; h < kBlocksQueryHeads; ++h) {
+        if ((int)h0 + h >= g.heads) break;
+        float z[16];
+        raw[h].turn(angles, rot.pairs, at.turned, [](double v) { return sizeof(T) == 2 ? to_odd(v) : (float)v; }, z);
+        char* o = out + ((((size_t)l * g.B + b) * g.heads + h0 + h) * g.T + t) * (D * sizeof(T));
+        Eight<T>::store(o, at.a, *reinterpret_cast<const float(*)[8]>(z));
+        Eight<T>::store(o, at.b, *reinterpret_cast<const float(*)[8]>(z + 8));
+    }
+}
+
 // A workgroup takes the keys or the values of one block of a segment (layer, sample,
-// KV head), both and the heads of a page side by side: ITEMS rows per lane group.
-// Behind them, kBlocksQueryRows rotated rows of the queries.
+// KV head), both and the heads of a page side by side: ITEMS rows per lane group.  A
+// decode step's call is a chain of memory latencies (slot, place, page, the block's
+// scale), so everything is loaded as soon as its address is known: the new rows and
+// their angles beside the look-up of the block.
 template <typename T, int D, int ITEMS, bool Gather>
 __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv, RowView qv, char* __restrict__ q_out,
-                                                         int Hq, WriteGrid g, const int32_t* __restrict__ idx,
+                                                         WriteGrid g, const int32_t* __restrict__ idx,
                                                          const int32_t* __restrict__ count,
                                                          const int32_t* __restrict__ start,
                                                          const int32_t* __restrict__ seq, BlockRotation rot,
                                                          PagePool p) {
     using Ln = Lanes<D>;
-    const int part = threadIdx.x % Ln::kRow, in = threadIdx.x / Ln::kRow;
     if constexpr (!Gather) {
-        if (blockIdx.x >= g.blocks) {
-            const unsigned first = (blockIdx.x - g.blocks) * kBlocksQueryRows;
-#pragma unroll 1
-            for (int i = 0; i < kBlocksQueryRows; i += Ln::kStep) {
-                const unsigned row = first + i + in;
-                if (row >= (unsigned)g.nq) return;
-                const unsigned lbh = row / (unsigned)g.T, t = row - lbh * g.T;
-                const unsigned lb = lbh / (unsigned)Hq, h = lbh - lb * Hq;
-                const unsigned l = lb / (unsigned)g.B, b = lb - l * g.B;
-                Turn<T, D> x;
-                x.load(qv.base + (size_t)l * qv.s_layer + (size_t)b * qv.s_batch + (size_t)h * qv.s_head +
-                           (size_t)t * qv.s_token,
-                       part, rot.position[(size_t)b * g.T + t], rot);
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = sizeof(T) == 2 ? to_odd(x.y[e]) : (float)x.y[e];
-                Eight<T>::store(q_out + (size_t)row * (D * sizeof(T)), part, y);
-            }
-            return;
-        }
+        if (blockIdx.x >= g.blocks) return turn_queries<T, D>(qv, q_out, g, blockIdx.x - g.blocks, rot);
     }
     __shared__ uint32_t s_top[kWaves];
-    __shared__ float s_lo[kWaves][D], s_hi[kWaves][D];
+    __shared__ float s_ends[2][kWaves][D];
+    const int part = threadIdx.x % Ln::kRow, in = threadIdx.x / Ln::kRow;
     const unsigned role = blockIdx.x & 1, x2 = blockIdx.x >> 1;
     const unsigned x1 = x2 / (unsigned)p.Hkv, lb = x1 / (unsigned)g.nblk;
     const int j = (int)(x2 - x1 * p.Hkv), i = (int)(x1 - lb * g.nblk);
@@ -206,60 +283,63 @@ __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv,
     const int slot = slot_of(seq, b, p.S), s0 = start[b];
     const int n = Gather ? min(count[seg], g.T) : count != nullptr ? min(count[b], g.T) : g.T;
     if (slot < 0 || s0 < 0 || n <= 0) return;
-    const int limit = held_of(p, slot) << p.shift;  // positions that there are
-    if (s0 >= limit) return;
-    const int at = (s0 >> p.shift) + i;             // block of the sequence
+    const int at = min((s0 >> p.shift) + i, p.M);   // block of the sequence
+    const int page = p.table[(size_t)slot * p.M + min(at, p.M - 1)], held = held_of(p, slot);
     const long long pos0 = (long long)at << p.shift;
     const int r0 = (int)max(0LL, s0 - pos0), r1 = (int)min((long long)1 << p.shift, s0 + (long long)n - pos0);
-    if (pos0 >= limit || r1 <= r0) return;
-    const int pg = p.table[(size_t)slot * p.M + at];
-    if (pg < 0 || pg >= p.n_pages) return;
-    char* block = block_at<D>(p, l, pg, j);
+    if (r1 <= r0) return;
+
+    const bool turn = !Gather && role == 0 && rot.cos != nullptr;
+    const Pieces pc = pieces_of<D>(part, rot, turn);
+    const RowView& view = role == 0 ? kv : vv;
+    const char* base = view.base + (size_t)l * view.s_layer + (size_t)b * view.s_batch + (size_t)j * view.s_head;
+    Sixteen<T> raw[ITEMS];
+    int from[ITEMS];  // Gather: the source row; else the row's position for its angles
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+        const int row = it * Ln::kStep + in;
+        const int m = (int)(pos0 + min(max(row, r0), r1 - 1) - s0);
+        from[it] = Gather ? idx[seg * g.T + m] : m;
+    }
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+        const bool there = it * Ln::kStep + in >= r0 && it * Ln::kStep + in < r1;
+        if (there && (!Gather || (from[it] >= 0 && from[it] < g.N)))
+            raw[it].template load<Gather>(base + (size_t)from[it] * view.s_token, pc);
+        else
+            raw[it] = Sixteen<T>{};
+    }
+    Angles angles[ITEMS];
+    if (turn) {
+#pragma unroll
+        for (int it = 0; it < ITEMS; ++it) from[it] = rot.position[(size_t)b * g.T + from[it]];
+#pragma unroll
+        for (int it = 0; it < ITEMS; ++it) angles[it].load(part, from[it], rot, pc.turned);
+    }
+    if (at >= held || page < 0 || page >= p.n_pages) return;
+    char* block = block_at<D>(p, l, page, j);
     char* tail = block + tail_at<D>(p.shift);
     char* codes = block + ((size_t)(role * D) << p.shift);
     const int old = r0 > 0 ? scale_of((uint8_t)tail[role]) : 0;
 
-    // the rows, their largest magnitude
-    float x[ITEMS][8];
+    // the rows' largest magnitude
+    float x[ITEMS][16];
     uint32_t top = 0;
-    const RowView& view = role == 0 ? kv : vv;
-    const char* base = view.base + (size_t)l * view.s_layer + (size_t)b * view.s_batch + (size_t)j * view.s_head;
 #pragma unroll
     for (int it = 0; it < ITEMS; ++it) {
-        const int row = it * Ln::kStep + in;
-        if (row < r0 || row >= r1) continue;
-        const int m = (int)(pos0 + row - s0);
-        if (Gather) {
-            const int t = idx[seg * g.T + m];
-            if (t >= 0 && t < g.N) {
-                Eight<T> raw;
-                raw.template load<true>(base + (size_t)t * view.s_token, part);
+        if (it * Ln::kStep + in < r0 || it * Ln::kStep + in >= r1) continue;
+        if (turn)
+            raw[it].turn(angles[it], rot.pairs, pc.turned, to_odd, x[it]);
+        else
+            raw[it].floats(x[it]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[it][e] = raw.get(e);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[it][e] = 0.0f;
-            }
-        } else if (role == 0 && rot.cos != nullptr) {
-            Turn<T, D> y;
-            y.load(base + (size_t)m * view.s_token, part, rot.position[(size_t)b * g.T + m], rot);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[it][e] = to_odd(y.y[e]);
-        } else {
-            Eight<T> raw;
-            raw.template load<false>(base + (size_t)m * view.s_token, part);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[it][e] = raw.get(e);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 16; ++e) {
             const uint32_t bits = __float_as_uint(x[it][e]) & 0x7fffffffu;
             top = max(top, bits < 0x7f800000u ? bits : 0u);
         }
     }
-#pragma unroll
-    for (int s = 1; s < kWave; s <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, s));
     const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
+    top = wave_max(top);
     if (lane == 0) s_top[wv] = top;
     __syncthreads();
 #pragma unroll
@@ -269,9 +349,9 @@ __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv,
     // rows under another scale: 2^-60 of it is zero like any smaller share
     const float factor = scale_float(127 - min(s - old, 60));
 
-    float lo[8], hi[8];
+    float lo[16], hi[16];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 16; ++e) {
         lo[e] = INFINITY;
         hi[e] = -INFINITY;
     }
@@ -279,56 +359,66 @@ __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv,
     for (int it = 0; it < ITEMS; ++it) {
         const int row = it * Ln::kStep + in;
         if (row >= r1) continue;
-        u32x2* at8 = reinterpret_cast<u32x2*>(codes + (size_t)row * D) + part;
+        char* here = codes + (size_t)row * D;
         if (row < r0) {
             if (s == old) continue;
-            u32x2 w = *at8;
-            w[0] = rescale4(w[0], factor);
-            w[1] = rescale4(w[1], factor);
-            *at8 = w;
+            u32x4* sixteen = reinterpret_cast<u32x4*>(here) + part;
+            u32x4 w = *sixteen;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = rescale4(w[e], factor);
+            *sixteen = w;
             continue;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 16; ++e) {
             x[it][e] = bounded(x[it][e], most);
             lo[e] = lower(lo[e], x[it][e]);
             hi[e] = higher(hi[e], x[it][e]);
         }
-        u32x2 w;
-        w[0] = codes4(x[it][0], x[it][1], x[it][2], x[it][3], scale);
-        w[1] = codes4(x[it][4], x[it][5], x[it][6], x[it][7], scale);
-        *at8 = w;
+        u32x2 w[2];
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            w[h / 2][h % 2] = codes4(x[it][4 * h], x[it][4 * h + 1], x[it][4 * h + 2], x[it][4 * h + 3], scale);
+        reinterpret_cast<u32x2*>(here)[pc.a] = w[0];
+        reinterpret_cast<u32x2*>(here)[pc.b] = w[1];
     }
     if (threadIdx.x == 0) tail[role] = (char)s;
     if (role != 0) return;
     // bounds: rounding keeps the order, so the bounds of the codes are the codes of the bounds
+    if (r1 - r0 > 1) {
 #pragma unroll
-    for (int st = Ln::kRow; st < kWave; st <<= 1)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            lo[e] = lower(lo[e], __shfl_xor(lo[e], st));
-            hi[e] = higher(hi[e], __shfl_xor(hi[e], st));
+        for (int e = 0; e < 16; ++e) {
+            lo[e] = over_rows<Ln::kRow>(lo[e], lower);
+            hi[e] = over_rows<Ln::kRow>(hi[e], higher);
         }
-    if (lane < Ln::kRow)
+    }
+    // a wave's, or a single row's
+    if (r1 - r0 > 1 ? lane < Ln::kRow : in == r0 % Ln::kStep) {
+        const int w = r1 - r0 > 1 ? wv : 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s_lo[wv][8 * part + e] = lo[e];
-            s_hi[wv][8 * part + e] = hi[e];
+        for (int e = 0; e < 16; ++e) {
+            const int ch = 8 * (e < 8 ? pc.a : pc.b) + e % 8;
+            s_ends[0][w][ch] = lo[e];
+            s_ends[1][w][ch] = hi[e];
         }
+    }
     __syncthreads();
     // four channels of one bound to a thread
     if (threadIdx.x >= 2 * D / 4) return;
     const int ch = threadIdx.x * 4 % D;
     const bool upper = threadIdx.x * 4 >= D;
     uint32_t* out = reinterpret_cast<uint32_t*>(tail + kBlockScales) + threadIdx.x;
-    float y[4], was[4];
+    float was[4];
     if (r0 > 0) floats4(rescale4(*out, factor), 1.0f, was);
+    float y[4];
+    const int waves = r1 - r0 > 1 ? kWaves : 1;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        y[e] = upper ? s_hi[0][ch + e] : s_lo[0][ch + e];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w)
-            y[e] = upper ? higher(y[e], s_hi[w][ch + e]) : lower(y[e], s_lo[w][ch + e]);
+        y[e] = s_ends[upper][0][ch + e];
+        for (int w = 1; w < waves; ++w) {
+            const float z = s_ends[upper][w][ch + e];
+            y[e] = upper ? higher(y[e], z) : lower(y[e], z);
+        }
         // in units of the scale: old bounds are codes already
         if (r0 > 0) y[e] = upper ? higher(y[e], was[e] * scale) : lower(y[e], was[e] * scale);
     }
@@ -344,77 +434,96 @@ struct ReadGrid {
     uint32_t rows;  // of all segments
 };
 
-// D / 8 lanes to a row, rows of all segments one after the other.  Bounds: row m is
-// block first + m's bound, else the row at position first + m.
+// D / 8 lanes to a row, kReadItems rows to a lane, those of all segments one after the
+// other.  Bounds: row m is block first + m's bound, else the row at position first + m.
+constexpr int kReadItems = 2;
 template <typename T, int D, bool Bounds>
 __global__ __launch_bounds__(kThreads) void read_blocks(PagePool p, ReadGrid g, const int32_t* __restrict__ seq,
                                                         const int32_t* __restrict__ first,
                                                         const int32_t* __restrict__ count, char* __restrict__ a_out,
                                                         char* __restrict__ b_out) {
-    using Ln = Lanes<D>;
-    const int part = threadIdx.x % Ln::kRow;
-    const uint32_t at = blockIdx.x * (uint32_t)Ln::kStep + threadIdx.x / Ln::kRow;
-    if (at >= g.rows) return;
-    const uint32_t seg = at / (uint32_t)g.cap, m = at - seg * g.cap;
-    const uint32_t lb = seg / (uint32_t)p.Hkv, j = seg - lb * p.Hkv;
-    const uint32_t l = lb / (uint32_t)g.B, b = lb - l * g.B;
-    const int slot = slot_of(seq, b, p.S);
-    if (slot < 0 || (count != nullptr && (int)m >= count[b])) return;
-    const int from = first != nullptr ? first[b] : 0;
-    const int len = length_of(p, slot), end = Bounds ? (len + (1 << p.shift) - 1) >> p.shift : len;
-    if (from < 0 || (long long)from + m >= end) return;
-    const int pos = from + (int)m, blk = Bounds ? pos : pos >> p.shift;
-    const int pg = p.table[(size_t)slot * p.M + blk];
-    if (pg < 0 || pg >= p.n_pages) return;
-    const char* block = block_at<D>(p, l, pg, j);
-    const char* tail = block + tail_at<D>(p.shift);
-    const int tok = pos & ((1 << p.shift) - 1);
-    const char* rows[2] = {Bounds ? tail + kBlockScales : block + (size_t)tok * D,
-                           Bounds ? tail + kBlockScales + D : block + ((size_t)D << p.shift) + (size_t)tok * D};
-    const u32x2 a = reinterpret_cast<const u32x2*>(rows[0])[part], c = reinterpret_cast<const u32x2*>(rows[1])[part];
-    const uint32_t scales = *reinterpret_cast<const uint16_t*>(tail);
-    const size_t out = (size_t)at * (D * sizeof(T));
+    constexpr int kRow = D / 8, kStep = kThreads / kRow;
+    const int part = threadIdx.x % kRow;
+    const uint32_t at0 = blockIdx.x * (uint32_t)(kStep * kReadItems) + threadIdx.x / kRow;
+    const char* block[kReadItems];
+    int tok[kReadItems];
+#pragma unroll
+    for (int it = 0; it < kReadItems; ++it) {
+        const uint32_t at = at0 + it * kStep;
+        block[it] = nullptr;
+        if (at >= g.rows) continue;
+        const uint32_t seg = at / (uint32_t)g.cap, m = at - seg * g.cap;
+        const uint32_t lb = seg / (uint32_t)p.Hkv, j = seg - lb * p.Hkv;
+        const uint32_t l = lb / (uint32_t)g.B, b = lb - l * g.B;
+        const int slot = slot_of(seq, b, p.S);
+        if (slot < 0 || (count != nullptr && (int)m >= count[b])) continue;
+        const int from = first != nullptr ? first[b] : 0;
+        const int len = length_of(p, slot), end = Bounds ? (len + (1 << p.shift) - 1) >> p.shift : len;
+        if (from < 0 || (long long)from + m >= end) continue;
+        const int pos = from + (int)m, blk = Bounds ? pos : pos >> p.shift;
+        const int pg = p.table[(size_t)slot * p.M + blk];
+        tok[it] = pos & ((1 << p.shift) - 1);
+        if (pg >= 0 && pg < p.n_pages) block[it] = block_at<D>(p, l, pg, j);
+    }
+    u32x2 a[kReadItems], c[kReadItems];
+    uint32_t scales[kReadItems];
+#pragma unroll
+    for (int it = 0; it < kReadItems; ++it) {
+        if (block[it] == nullptr) continue;
+        const char* tail = block[it] + tail_at<D>(p.shift);
+        const char* rows[2] = {Bounds ? tail + kBlockScales : block[it] + (size_t)tok[it] * D,
+                               Bounds ? tail + kBlockScales + D : block[it] + ((size_t)D << p.shift) + (size_t)tok[it] * D};
+        a[it] = reinterpret_cast<const u32x2*>(rows[0])[part];
+        c[it] = reinterpret_cast<const u32x2*>(rows[1])[part];
+        scales[it] = *reinterpret_cast<const uint16_t*>(tail);
+    }
     auto give = [&](char* o, u32x2 w, uint32_t s) {
         float x[8];
         const float unit = scale_float(scale_of((uint8_t)s));
         floats4(w[0], unit, *reinterpret_cast<float(*)[4]>(x));
         floats4(w[1], unit, *reinterpret_cast<float(*)[4]>(x + 4));
-        Eight<T>::store(o + out, part, x);
+        Eight<T>::store(o, part, x);
     };
-    if (a_out != nullptr) give(a_out, a, scales);
-    if (b_out != nullptr) give(b_out, c, Bounds ? scales : scales >> 8);
+#pragma unroll
+    for (int it = 0; it < kReadItems; ++it) {
+        if (block[it] == nullptr) continue;
+        const size_t out = (size_t)(at0 + it * kStep) * (D * sizeof(T));
+        if (a_out != nullptr) give(a_out + out, a[it], scales[it]);
+        if (b_out != nullptr) give(b_out + out, c[it], Bounds ? scales[it] : scales[it] >> 8);
+    }
 }
 
 template <typename T, int D, int ITEMS>
-void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, int Hq, const WriteGrid& g,
+void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, const WriteGrid& g,
                unsigned groups, const int32_t* idx, const int32_t* count, const int32_t* start, const int32_t* seq,
                const BlockRotation& rot, const PagePool& p, hipStream_t st) {
     if (idx != nullptr)
-        hipLaunchKernelGGL((write_blocks<T, D, ITEMS, true>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out, Hq,
+        hipLaunchKernelGGL((write_blocks<T, D, ITEMS, true>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out,
                            g, idx, count, start, seq, rot, p);
     else
-        hipLaunchKernelGGL((write_blocks<T, D, ITEMS, false>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out, Hq,
+        hipLaunchKernelGGL((write_blocks<T, D, ITEMS, false>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out,
                            g, idx, count, start, seq, rot, p);
 }
 
 template <typename T, int D>
-void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, int Hq, const WriteGrid& g,
+void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, const WriteGrid& g,
                unsigned groups, const int32_t* idx, const int32_t* count, const int32_t* start, const int32_t* seq,
                const BlockRotation& rot, const PagePool& p, hipStream_t st) {
     constexpr int kStep = Lanes<D>::kStep;
     if (p.shift == 5)
-        run_write<T, D, 32 / kStep>(k, v, q, q_out, Hq, g, groups, idx, count, start, seq, rot, p, st);
+        run_write<T, D, (32 + kStep - 1) / kStep>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
     else if (p.shift == 6)
-        run_write<T, D, 64 / kStep>(k, v, q, q_out, Hq, g, groups, idx, count, start, seq, rot, p, st);
+        run_write<T, D, 64 / kStep>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
     else
-        run_write<T, D, 128 / kStep>(k, v, q, q_out, Hq, g, groups, idx, count, start, seq, rot, p, st);
+        run_write<T, D, 128 / kStep>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
 }
 
 template <typename T, int D, bool Bounds>
 void run_read(const PagePool& p, int B, int cap, const int32_t* seq, const int32_t* first, const int32_t* count,
               void* a, void* b, hipStream_t st) {
     const ReadGrid g{B, cap, (uint32_t)p.L * B * p.Hkv * (uint32_t)cap};
-    const unsigned groups = (g.rows + Lanes<D>::kStep - 1) / Lanes<D>::kStep;
+    constexpr unsigned kRows = kThreads / (D / 8) * kReadItems;
+    const unsigned groups = (g.rows + kRows - 1) / kRows;
     hipLaunchKernelGGL((read_blocks<T, D, Bounds>), dim3(groups), dim3(kThreads), 0, st, p, g, seq, first, count,
                        static_cast<char*>(a), static_cast<char*>(b));
 }
@@ -437,15 +546,17 @@ hipError_t launch_blocks_write(const RowView& k, const RowView& v, const RowView
                                const int32_t* start, const int32_t* seq, const BlockRotation& rot, const PagePool& p,
                                hipStream_t st) {
     if (cap == 0) return hipSuccess;
-    WriteGrid g{B, cap, N, (int)blocks_touched(cap, 1 << p.shift), 0, 0};
+    WriteGrid g{B, cap, N, (int)blocks_touched(cap, 1 << p.shift), Hq, 0, (unsigned)B * cap};
     g.blocks = 2u * p.L * B * p.Hkv * g.nblk;
-    if (q_out != nullptr) g.nq = p.L * B * Hq * cap;
-    const unsigned groups = g.blocks + (unsigned)(g.nq + kBlocksQueryRows - 1) / kBlocksQueryRows;
+    const unsigned step = d == 128 ? Lanes<128>::kStep : Lanes<64>::kStep;
+    const unsigned groups =
+        g.blocks + (q_out == nullptr ? 0u : (unsigned)p.L * ((g.tokens + step - 1) / step) *
+                                                ((unsigned)(Hq + kBlocksQueryHeads - 1) / kBlocksQueryHeads));
     char* o = static_cast<char*>(q_out);
-    if (dtype == 0 && d == 128) run_write<__bf16, 128>(k, v, q, o, Hq, g, groups, idx, count, start, seq, rot, p, st);
-    if (dtype == 0 && d == 64) run_write<__bf16, 64>(k, v, q, o, Hq, g, groups, idx, count, start, seq, rot, p, st);
-    if (dtype == 1 && d == 128) run_write<float, 128>(k, v, q, o, Hq, g, groups, idx, count, start, seq, rot, p, st);
-    if (dtype == 1 && d == 64) run_write<float, 64>(k, v, q, o, Hq, g, groups, idx, count, start, seq, rot, p, st);
+    if (dtype == 0 && d == 128) run_write<__bf16, 128>(k, v, q, o, g, groups, idx, count, start, seq, rot, p, st);
+    if (dtype == 0 && d == 64) run_write<__bf16, 64>(k, v, q, o, g, groups, idx, count, start, seq, rot, p, st);
+    if (dtype == 1 && d == 128) run_write<float, 128>(k, v, q, o, g, groups, idx, count, start, seq, rot, p, st);
+    if (dtype == 1 && d == 64) run_write<float, 64>(k, v, q, o, g, groups, idx, count, start, seq, rot, p, st);
     return hipGetLastError();
 }
 

@@ -3,9 +3,10 @@
 //
 // With up and down the sums over the group's heads of max(q, 0) and min(q, 0) a
 // block's score is <up, hi> + <down, lo>: two products of d channels whatever the
-// number of heads, which is why the kernel reads 2 d bytes per block and does little
-// else.  They are summed in 64 bits, so that the order of the sum does not decide
-// which of two blocks is chosen.
+// number of heads.  They are summed in 64 bits, so that the order of the sum does not
+// decide which of two blocks is chosen.
+#include <type_traits>
+
 #include "kve_blocks_device.h"
 #include "kve_device.h"
 #include "kve_internal.h"
@@ -14,14 +15,15 @@ namespace kve {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
 constexpr int kScored = 64;              // blocks per workgroup of top_scores
-constexpr uint32_t kForced = 0xffffffffu;  // key of the first and last blocks: above every score's
+
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 // What a call chooses.
 struct TopGrid {
     BlockView view;
-    int Hq, G, k, first, last, most;  // most: blocks that max_tokens can lie in
+    int Hq, G, k, first, last, pitch;  // pitch: keys of a segment in the workspace
 };
 
 struct Segment {
@@ -41,131 +43,254 @@ __device__ __forceinline__ Segment segment_of(const PagePool& p, const TopGrid& 
     return x;
 }
 
+// x of the lane that a step of a sum over sixteen lanes adds.
+template <int CTRL>
+__device__ __forceinline__ double row_move(double x) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, 0xf, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), CTRL, 0xf, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// Sum over the LANES lanes (8 or 16) of a block, in every lane.
+template <int LANES>
+__device__ __forceinline__ double row_sum(double x) {
+    x += row_move<0xb1>(x);   // lanes 1 0 3 2
+    x += row_move<0x4e>(x);   // lanes 2 3 0 1
+    x += row_move<0x141>(x);  // mirrored within eight
+    if constexpr (LANES == 16) x += row_move<0x140>(x);  // within sixteen
+    return x;
+}
+
+// Code K of a dword as a double times 2^-1016, but NaN codes as +-480: an E4M3's bits,
+// denormal or not, are the top bits of a double's exponent and mantissa as they are.
+// Three full-rate instructions, where the conversions from float take a quarter of the rate.
+template <int K>
+__device__ __forceinline__ double tiny(uint32_t w) {
+    const int top = (int)(w << (24 - 8 * K)) >> 7;
+    return __builtin_bit_cast(double, (uint64_t)((uint32_t)top & 0x80fe0000u) << 32);
+}
+constexpr double kUp = 0x1p800, kDown = 0x1p216;  // what brings products of such doubles back to scale, in two steps
+
+// Not 0 if one of four codes is NaN.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+template <int W>
+__device__ __forceinline__ double add4(const double (&up)[8], const double (&down)[8], uint32_t lo, uint32_t hi,
+                                       double sum) {
+    sum = fma(up[4 * W], tiny<0>(hi), fma(down[4 * W], tiny<0>(lo), sum));
+    sum = fma(up[4 * W + 1], tiny<1>(hi), fma(down[4 * W + 1], tiny<1>(lo), sum));
+    sum = fma(up[4 * W + 2], tiny<2>(hi), fma(down[4 * W + 2], tiny<2>(lo), sum));
+    return fma(up[4 * W + 3], tiny<3>(hi), fma(down[4 * W + 3], tiny<3>(lo), sum));
+}
+
 // Keys of kScored blocks of a segment.  D / 8 lanes to a block, eight channels of
-// both bounds each.
+// both bounds each, and all of a lane's blocks looked up and loaded together.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, PagePool p, TopGrid g, int chunks,
                                                        uint32_t* __restrict__ keys) {
-    constexpr int kRow = D / 8, kStep = kThreads / kRow;
+    constexpr int kRow = D / 8, kStep = kThreads / kRow, kItems = kScored / kStep;
+    __shared__ __attribute__((aligned(16))) double s_up[2][D];
     const unsigned seg = blockIdx.x / (unsigned)chunks;
     const int chunk = (int)(blockIdx.x - seg * chunks);
     const Segment x = segment_of(p, g, seg);
     if (x.blocks <= g.k || chunk * kScored >= x.blocks) return;  // all are taken, or none here
     const int part = threadIdx.x % kRow, in = threadIdx.x / kRow;
+    int page[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const int at = chunk * kScored + i * kStep + in;
+        page[i] = at < x.blocks ? p.table[(size_t)x.slot * p.M + at] : -1;
+    }
+    // the heads' sums: a thread to each channel of either
+    if (threadIdx.x < 2 * D) {
+        const int c = threadIdx.x % D;
+        const bool lower = threadIdx.x >= D;
+        const T* row = q + ((((size_t)x.l * g.view.B + x.b) * g.Hq + (size_t)x.j * g.G) * g.view.T + x.t) * D + c;
+        double sum = 0.0;
+#pragma unroll 4
+        for (int h = 0; h < g.G; ++h) {
+            const float y = (float)row[(size_t)h * g.view.T * D];
+            sum += (lower ? y > 0.0f : y < 0.0f) ? 0.0 : (double)y;
+        }
+        s_up[lower][c] = sum * kUp;
+    }
+    u32x2 lo[kItems], hi[kItems];
+    uint8_t unit[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        // a block without a page: any page's bounds, and not their score
+        const int pg = page[i] >= 0 && page[i] < p.n_pages ? page[i] : 0;
+        const char* tail = block_at<D>(p, x.l, pg, x.j) + tail_at<D>(p.shift);
+        lo[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales)[part];
+        hi[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales + D)[part];
+        unit[i] = (uint8_t)tail[0];
+    }
+    __syncthreads();
     double up[8], down[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) up[e] = down[e] = 0.0;
-    const T* rows = q + ((((size_t)x.l * g.view.B + x.b) * g.Hq + (size_t)x.j * g.G) * g.view.T + x.t) * D + 8 * part;
-#pragma unroll 1
-    for (int h = 0; h < g.G; ++h)
+    for (int e = 0; e < 8; ++e) {
+        up[e] = s_up[0][8 * part + e];
+        down[e] = s_up[1][8 * part + e];
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double y = (double)(float)rows[(size_t)h * g.view.T * D + e];
-            up[e] += y < 0.0 ? 0.0 : y;
-            down[e] += y > 0.0 ? 0.0 : y;
-        }
-#pragma unroll 1
-    for (int i = 0; i < kScored; i += kStep) {
-        const int at = chunk * kScored + i + in;
-        const bool there = at < x.blocks;
-        const int pg = there ? p.table[(size_t)x.slot * p.M + at] : -1;
-        const bool ok = pg >= 0 && pg < p.n_pages;
-        double sum = 0.0;
-        float unit = 0.0f;
-        if (ok) {
-            const char* tail = block_at<D>(p, x.l, pg, x.j) + tail_at<D>(p.shift);
-            const u32x2 lo = reinterpret_cast<const u32x2*>(tail + kBlockScales)[part];
-            const u32x2 hi = reinterpret_cast<const u32x2*>(tail + kBlockScales + D)[part];
-            unit = scale_float(scale_of((uint8_t)tail[0]));
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                float a[4], c[4];
-                floats4(lo[w], 1.0f, a);
-                floats4(hi[w], 1.0f, c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    sum = fma(up[4 * w + e], (double)c[e], fma(down[4 * w + e], (double)a[e], sum));
-            }
-        }
-#pragma unroll
-        for (int s = 1; s < kRow; s <<= 1) sum += __shfl_xor(sum, s);
-        if (part == 0 && there) {
-            const bool forced = at < g.first || at >= x.blocks - g.last;
-            keys[(size_t)seg * g.most + at] = forced ? kForced : ok ? score_key((float)(sum * (double)unit)) : 0u;
+    for (int i = 0; i < kItems; ++i) {
+        double sum = add4<1>(up, down, lo[i][1], hi[i][1], add4<0>(up, down, lo[i][0], hi[i][0], 0.0));
+        if ((nan_codes(lo[i][0]) | nan_codes(lo[i][1]) | nan_codes(hi[i][0]) | nan_codes(hi[i][1])) != 0)
+            sum = __builtin_nan("");
+        sum = row_sum<kRow>(sum);
+        const int at = chunk * kScored + i * kStep + in;
+        if (part == 0 && at < x.blocks) {
+            const bool ok = page[i] >= 0 && page[i] < p.n_pages;
+            const double score = sum * kDown * (double)scale_float(scale_of(unit[i]));
+            keys[(size_t)seg * g.pitch + at] = ok ? score_key((float)score) : 0u;
         }
     }
 }
 
-// Sum over the threads before, and over all in `total`.  s: kWaves words of LDS.
+// Exclusive sum over the threads of a workgroup of kSelect, and over all in `total`.
+// s: kSelectWaves words of LDS, free again behind the next barrier.
+constexpr int kSelect = 1024, kSelectWaves = kSelect / kWave;
 __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* s, uint32_t& total) {
     const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
-    uint32_t inc = x;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const uint32_t y = (uint32_t)__shfl_up((int)inc, d);
-        inc += lane >= d ? y : 0u;
-    }
-    __syncthreads();
+    auto step = [](uint32_t v, auto ctrl, auto rows) {
+        return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf,
+                                                         false);
+    };
+    auto wave = [&](uint32_t v) {
+        v = step(v, Int<0x111>{}, Int<0xf>{});
+        v = step(v, Int<0x112>{}, Int<0xf>{});
+        v = step(v, Int<0x114>{}, Int<0xf>{});
+        v = step(v, Int<0x118>{}, Int<0xf>{});
+        v = step(v, Int<0x142>{}, Int<0xa>{});
+        return step(v, Int<0x143>{}, Int<0xc>{});
+    };
+    const uint32_t inc = wave(x);
     if (lane == kWave - 1) s[w] = inc;
     __syncthreads();
-    uint32_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int e = 0; e < kWaves; ++e) {
-        before += e < w ? s[e] : 0u;
-        total += s[e];
-    }
+    const uint32_t sums = wave(lane < kSelectWaves ? s[lane] : 0u);
+    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, kSelectWaves - 1);
+    const uint32_t before = w > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, __builtin_amdgcn_readfirstlane(w) - 1)
+                                  : 0u;
     return before + inc - x;
 }
 
-// One workgroup per segment: the k-th highest key digit by digit, then the blocks
-// above it and the first of those equal to it in ascending order.
-__global__ __launch_bounds__(kThreads) void top_select(PagePool p, TopGrid g, const uint32_t* __restrict__ keys,
-                                                       int32_t* __restrict__ top) {
-    __shared__ uint32_t s_hist[256], s_scan[kWaves], s_pick[2];
+// One workgroup per segment.  The blocks that are not forced compete for the places
+// that the forced ones leave: the lowest key that gets one is found in digits of 11
+// bits, from the highest bit in which the keys differ on (keys of one sign and a few
+// binades, as scores are, spread over the digits of the first pass, and the counts in
+// LDS do not collide), until all that share its digits get one.
+__global__ __launch_bounds__(kSelect) void top_select(PagePool p, TopGrid g, const uint32_t* __restrict__ keys,
+                                                      int32_t* __restrict__ top) {
+    constexpr int kBits = 11, kBins = 1 << kBits, kTile = 4 * kSelect;
+    __shared__ uint32_t s_hist[kBins], s_scan[2][kSelectWaves], s_ends[2][kSelectWaves], s_pick[3];
     const unsigned seg = blockIdx.x;
     const Segment x = segment_of(p, g, seg);
     int32_t* out = top + (size_t)seg * g.k;
-    const int n = x.blocks;
+    const int n = x.blocks, tid = threadIdx.x;
     if (n <= g.k) {
-        for (int i = threadIdx.x; i < g.k; i += kThreads) out[i] = i < n ? i : -1;
+        for (int i = tid; i < g.k; i += kSelect) out[i] = i < n ? i : -1;
         return;
     }
-    const uint32_t* key = keys + (size_t)seg * g.most;
-    uint32_t prefix = 0, want = (uint32_t)g.k;  // of the keys that share the prefix, the want-th highest
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        s_hist[threadIdx.x] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const uint32_t y = key[i];
-            if (shift == 24 || (y >> (shift + 8)) == prefix) atomicAdd(&s_hist[(y >> shift) & 255u], 1u);
+    const uint32_t* key = keys + (size_t)seg * g.pitch;
+    const int open0 = g.first, open1 = n - g.last;  // blocks that compete
+    uint32_t want = (uint32_t)(g.k - g.first - g.last);
+    // four neighbouring keys of a tile; the first tile is loaded once
+    const u32x4 mine = tid * 4 < n ? *reinterpret_cast<const u32x4*>(key + tid * 4) : zero16();
+    auto load = [&](int i0) {
+        if (i0 == 0) return mine;
+        return i0 + tid * 4 < n ? *reinterpret_cast<const u32x4*>(key + i0 + tid * 4) : zero16();
+    };
+    auto each = [&](auto&& body) {
+        for (int i0 = 0; i0 < n; i0 += kTile) {
+            const u32x4 y = load(i0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = i0 + tid * 4 + e;
+                if (i >= open0 && i < open1) body(y[e]);
+            }
         }
-        __syncthreads();
-        // thread e: digit 255 - e, the counts above it
-        const uint32_t mine = s_hist[255 - threadIdx.x];
-        uint32_t total;
-        const uint32_t above = scan(mine, s_scan, total);
-        if (above < want && above + mine >= want) {
-            s_pick[0] = 255u - threadIdx.x;
-            s_pick[1] = want - above;
-        }
-        __syncthreads();
-        prefix = prefix << 8 | s_pick[0];
-        want = s_pick[1];
+    };
+    for (int i = tid; i < kBins; i += kSelect) s_hist[i] = 0;
+    uint32_t least = 0xffffffffu, most = 0;
+    each([&](uint32_t y) {
+        least = min(least, y);
+        most = max(most, y);
+    });
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        least = min(least, (uint32_t)__shfl_xor((int)least, d));
+        most = max(most, (uint32_t)__shfl_xor((int)most, d));
     }
-    // in ascending order: keys above the prefix, and the first `want` equal to it
+    const int lane = tid & (kWave - 1);
+    if (lane == 0) {
+        s_ends[0][tid / kWave] = least;
+        s_ends[1][tid / kWave] = most;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) {
+        least = min(least, s_ends[0][w]);
+        most = max(most, s_ends[1][w]);
+    }
+    // `prefix`: the bits from `shift` on of the lowest key that gets a place
+    int shift = least < most ? 32 - __builtin_clz(least ^ most) : 0;
+    uint32_t prefix = shift < 32 ? most >> shift : 0u;
+    bool done = want == 0 || shift == 0;
+    while (!done) {
+        const int low = max(0, shift - kBits), bits = shift - low;
+        each([&](uint32_t y) {
+            if (shift == 32 || y >> shift == prefix) atomicAdd(&s_hist[(y >> low) & ((1u << bits) - 1)], 1u);
+        });
+        __syncthreads();
+        // thread e: digits kBins - 1 - 2 e and the one below it
+        const uint32_t a = s_hist[kBins - 1 - 2 * tid], b = s_hist[kBins - 2 - 2 * tid];
+        uint32_t total;
+        const uint32_t above = scan(a + b, s_scan[0], total);
+        if (above < want && above + a + b >= want) {
+            const bool first = above + a >= want;
+            s_pick[0] = (uint32_t)(kBins - 1 - 2 * tid - !first);
+            s_pick[1] = want - (first ? above : above + a);
+            s_pick[2] = first ? a : b;
+        }
+        // the next pass counts from zero
+        s_hist[kBins - 1 - 2 * tid] = 0;
+        s_hist[kBins - 2 - 2 * tid] = 0;
+        __syncthreads();
+        prefix = prefix << bits | s_pick[0];
+        want = s_pick[1];
+        shift = low;
+        done = low == 0 || s_pick[2] == want;
+        if (!done) __syncthreads();  // s_pick and s_scan are read
+    }
+    // in ascending order: forced ones, keys above the prefix, and the first `want` that
+    // have it; both are counted in one sum, 16 bits each per tile
     uint32_t placed = 0, equal = 0;
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
-        const int i = i0 + (int)threadIdx.x;
-        const uint32_t y = i < n ? key[i] : 0u;
-        const bool same = i < n && y == prefix;
-        uint32_t sames, takes;
-        const uint32_t rank = scan(same ? 1u : 0u, s_scan, sames);
-        const bool take = i < n && (y > prefix || (same && equal + rank < want));
-        const uint32_t at = scan(take ? 1u : 0u, s_scan, takes);
-        if (take) out[placed + at] = i;
-        placed += takes;
-        equal += sames;
+    for (int i0 = 0, turn = 0; i0 < n; i0 += kTile, turn ^= 1) {
+        const u32x4 y = load(i0);
+        uint32_t own = 0;
+        bool take[4], same[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = i0 + tid * 4 + e;
+            const bool competes = i >= open0 && i < open1;
+            const uint32_t h = shift < 32 ? y[e] >> shift : 0u;
+            take[e] = i < n && (!competes || h > prefix);
+            same[e] = competes && h == prefix;
+            own += (take[e] ? 1u : 0u) + (same[e] ? 0x10000u : 0u);
+        }
+        uint32_t total;
+        const uint32_t before = scan(own, s_scan[turn], total);
+        uint32_t at = placed + (before & 0xffffu), ties = equal + (before >> 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = same[e] && ties < want;
+            if (take[e] || in) out[at + min(ties, want)] = i0 + tid * 4 + e;
+            at += take[e] ? 1u : 0u;
+            ties += same[e] ? 1u : 0u;
+        }
+        placed += total & 0xffffu;
+        equal += total >> 16;
     }
 }
 
@@ -173,11 +298,12 @@ __global__ __launch_bounds__(kThreads) void top_select(PagePool p, TopGrid g, co
 
 hipError_t launch_blocks_top(const void* q, int dtype, const PagePool& p, int d, const BlockView& view, int Hq, int k,
                              int first, int last, int32_t* top, void* ws, hipStream_t st) {
-    const TopGrid g{view, Hq, Hq / p.Hkv, k, first, last, top_blocks(view.max_tokens, 1 << p.shift)};
+    const int most = top_blocks(view.max_tokens, 1 << p.shift);
+    const TopGrid g{view, Hq, Hq / p.Hkv, k, first, last, top_pitch(most)};
     const unsigned segs = (unsigned)p.L * view.B * p.Hkv * view.T;
     uint32_t* keys = static_cast<uint32_t*>(ws);
-    if (g.most > k) {
-        const int chunks = (g.most + kScored - 1) / kScored;
+    if (most > k) {
+        const int chunks = (most + kScored - 1) / kScored;
         const dim3 grid(segs * (unsigned)chunks), block(kThreads);
         if (dtype == 0 && d == 128)
             hipLaunchKernelGGL((top_scores<__bf16, 128>), grid, block, 0, st, static_cast<const __bf16*>(q), p, g,
@@ -192,7 +318,7 @@ hipError_t launch_blocks_top(const void* q, int dtype, const PagePool& p, int d,
             hipLaunchKernelGGL((top_scores<float, 64>), grid, block, 0, st, static_cast<const float*>(q), p, g,
                                chunks, keys);
     }
-    hipLaunchKernelGGL(top_select, dim3(segs), dim3(kThreads), 0, st, p, g, keys, top);
+    hipLaunchKernelGGL(top_select, dim3(segs), dim3(kSelect), 0, st, p, g, keys, top);
     return hipGetLastError();
 }
 

@@ -68,7 +68,7 @@ kve_status_t write_common(const char* fn, const void* k, const kve_strides_t* k_
             return fail(KVE_ERR_INVALID_ARG, "%s: q or q_out not 16-byte aligned", fn);
         const double rows = (double)blocks->L * B * Hq * cap;
         if (rows > (double)(1 << 30)) return fail(KVE_ERR_UNSUPPORTED, "%s: shape too large", fn);
-        groups += rows / kve::kBlocksQueryRows + 1;
+        groups += (double)blocks->L * ((long long)B * cap / 32 + 1) * (Hq / kve::kBlocksQueryHeads + 1);
     }
     if (groups > (double)kMaxGroups) return fail(KVE_ERR_UNSUPPORTED, "%s: shape too large", fn);
     if (cap == 0) return ok();  // nothing to do, but what would be refused with rows has been

@@ -24,7 +24,7 @@ struct BlockRotation {
 // Blocks that `rows` rows can touch, wherever the first one lies.
 inline long long blocks_touched(long long rows, int page) { return rows == 0 ? 0 : (rows + page - 2) / page + 1; }
 
-constexpr int kBlocksQueryRows = 64;  // rows per workgroup that rotates queries
+constexpr int kBlocksQueryHeads = 4;  // heads per workgroup that rotates queries, of 32 tokens or more
 
 // What query tokens see (kve_blocks.h): start null: the last T tokens.
 struct BlockView {
@@ -88,8 +88,11 @@ inline size_t decode_blocks_size(int L, int B, int Hq, int Hkv, int T, int d) {
 // Blocks that max_tokens tokens can lie in.
 inline int top_blocks(int max_tokens, int page) { return (max_tokens + page - 1) / page; }
 
+// Keys from one segment's first to the next one's: four are loaded at once.
+inline int top_pitch(int blocks) { return (blocks + 3) / 4 * 4; }
+
 inline size_t top_size(int L, int B, int Hkv, int T, int max_tokens, int page) {
-    return align_up((size_t)L * B * Hkv * T * top_blocks(max_tokens, page) * sizeof(uint32_t));
+    return align_up((size_t)L * B * Hkv * T * top_pitch(top_blocks(max_tokens, page)) * sizeof(uint32_t));
 }
 
 }  // namespace kve

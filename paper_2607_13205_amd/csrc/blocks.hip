@@ -73,8 +73,8 @@ __device__ __forceinline__ float to_odd(double y) {
     return __uint_as_float(bits | 1u);
 }
 
-// A lane of a row takes two pieces of eight channels, `a` and `b`, which hold all
-// of its pairs.  The lanes' a, and their b, lie side by side where they can, so that a
+// A lane of a turned row takes two pieces of eight channels, `a` and `b`, which hold
+// all of its pairs; they lie beside those of its neighbours where they can, so that a
 // load or store of a wave covers whole lines.
 struct Pieces {
     int a, b;
@@ -82,8 +82,8 @@ struct Pieces {
 };
 
 template <int D>
-__device__ __forceinline__ Pieces pieces_of(int part, const BlockRotation& r, bool turn) {
-    const int n = turn ? r.r / 16 : 0;  // lanes whose pieces are turned
+__device__ __forceinline__ Pieces pieces_of(int part, const BlockRotation& r) {
+    const int n = r.r / 16;  // lanes whose pieces are turned
     if (part >= n) return Pieces{n + part, D / 16 + part, false};
     return r.pairs ? Pieces{2 * part, 2 * part + 1, true} : Pieces{part, part + n, true};
 }
@@ -104,25 +104,57 @@ struct Angles {
     }
 };
 
-// Two pieces of a row.  Rounded: how a turned channel, exact to 53 bits, becomes a float.
+// How a turned channel becomes a float: as it is rounded once more, to an E4M3 or to
+// bfloat16 (Odd and Half), or as the result itself (Float).
+enum class Turned { Odd, Half, Float };
+
+// Two pieces of a row.
 template <typename T>
 struct Sixteen {
     Eight<T> a, b;
-    template <bool Once>
     __device__ __forceinline__ void load(const char* row, const Pieces& at) {
-        a.template load<Once>(row, at.a);
-        b.template load<Once>(row, at.b);
+        a.template load<false>(row, at.a);
+        b.template load<false>(row, at.b);
     }
-    __device__ __forceinline__ void floats(float (&x)[16]) const {
+    // Pair i of a row's pieces: channels i of the two, or neighbours of one.
+    __device__ __forceinline__ static void pair(const float (&x)[16], bool pairs, int i, float& u, float& w) {
+        u = pairs ? x[2 * i] : x[i];
+        w = pairs ? x[2 * i + 1] : x[8 + i];
+    }
+    // Turned in 32 bits with the products' errors: y is off by less than three steps of
+    // float32 (u c - p is rounded once, and the sum with the exact error of p once, each by
+    // half a step, where the error is not what is left of it).  That decides every later
+    // rounding unless a border of one lies within three steps: borders of E4M3 end in 16
+    // zero bits, those of bfloat16 in a one and 15 zeros.  Returns whether all are decided;
+    // 64 bits otherwise (a chunk of 1003 tokens, 32 and 8 heads: 25.6 us with 64 bits
+    // throughout).
+    template <Turned How>
+    __device__ __forceinline__ static bool fast(const float (&x)[16], const Angles& g, bool pairs, float (&y)[16]) {
+        uint32_t border = 0xffffu;
+        float clear = INFINITY, most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float u, w;
+            pair(x, pairs, i, u, w);
+            const float c = g.cos[i / 4][i % 4], s = g.sin[i / 4][i % 4];
+            const float p = w * s, q = u * s, ep = fmaf(w, s, -p), eq = fmaf(u, s, -q);
+            const float lo = fmaf(u, c, -p) - ep, hi = fmaf(w, c, q) + eq;
+            constexpr uint32_t kAt = How == Turned::Half ? 0x8003u : 3u;
+            border = min(border, min((__float_as_uint(lo) + kAt) & 0xffffu, (__float_as_uint(hi) + kAt) & 0xffffu));
+            clear = fminf(clear, fminf(fmaf(-4.0f, fabsf(ep), fabsf(lo)), fmaf(-4.0f, fabsf(eq), fabsf(hi))));
+            most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
+            y[i] = lo;
+            y[8 + i] = hi;
+        }
+        return border > 6 && clear > 0x1p-90f && most < 0x1p120f;
+    }
+    template <Turned How>
+    __device__ __forceinline__ void turn(const Angles& g, bool pairs, bool turned, float (&x)[16]) const {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             x[e] = a.get(e);
             x[8 + e] = b.get(e);
         }
-    }
-    template <typename Rounded>
-    __device__ __forceinline__ void turn(const Angles& g, bool pairs, bool turned, Rounded rounded, float (&x)[16]) const {
-        floats(x);
         if (!g.there) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(0x7fc00000u);
@@ -130,23 +162,22 @@ struct Sixteen {
         }
         if (!turned) return;
         float y[16];
+        if (How == Turned::Float || !fast<How>(x, g, pairs, y)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // pair i: channels i of the two pieces, or neighbours of one
-            const double u = pairs ? x[2 * i] : x[i], w = pairs ? x[2 * i + 1] : x[8 + i];
-            const double c = g.cos[i / 4][i % 4], s = g.sin[i / 4][i % 4];
-            const float lo = rounded(fma(u, c, -(w * s))), hi = rounded(fma(w, c, u * s));
-            y[i] = lo;
-            y[8 + i] = hi;
+            for (int i = 0; i < 8; ++i) {
+                float u, w;
+                pair(x, pairs, i, u, w);
+                const double c = g.cos[i / 4][i % 4], s = g.sin[i / 4][i % 4];
+                const double lo = fma((double)u, c, -((double)w * s)), hi = fma((double)w, c, (double)u * s);
+                y[i] = How == Turned::Float ? (float)lo : to_odd(lo);
+                y[8 + i] = How == Turned::Float ? (float)hi : to_odd(hi);
+            }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[2 * i] = pairs ? y[i] : x[2 * i];
-            x[2 * i + 1] = pairs ? y[8 + i] : x[2 * i + 1];
+            x[2 * i] = pairs ? y[i] : y[2 * i];
+            x[2 * i + 1] = pairs ? y[8 + i] : y[2 * i + 1];
         }
-        if (!pairs)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = y[e];
     }
 };
 
@@ -207,8 +238,8 @@ template <int ROW, typename F>
 __device__ __forceinline__ float over_rows(float x, F f) {
     auto g = [&](uint32_t a, uint32_t b) { return __float_as_uint(f(__uint_as_float(a), __uint_as_float(b))); };
     uint32_t y = __float_as_uint(x);
-    if constexpr (ROW == 4) y = g(y, dpp<0x124>(y));  // rotated by four, then by eight
-    y = g(y, dpp<0x128>(y));
+    if constexpr (ROW <= 4) y = g(y, dpp<0x124>(y));  // rotated by four, then by eight
+    if constexpr (ROW <= 8) y = g(y, dpp<0x128>(y));
     return __uint_as_float(over_halves(y, g));
 }
 
@@ -218,9 +249,10 @@ struct WriteGrid {
     unsigned blocks, tokens;   // workgroups that take blocks, those behind them take queries; B T
 };
 
-template <int D>
+// NP pieces of eight channels to a lane.
+template <int D, int NP>
 struct Lanes {
-    static constexpr int kRow = D / 16;            // lanes to a row
+    static constexpr int kRow = D / 8 / NP;        // lanes to a row
     static constexpr int kStep = kThreads / kRow;  // rows per step
 };
 
@@ -228,73 +260,82 @@ struct Lanes {
 template <typename T, int D>
 __device__ __forceinline__ void turn_queries(const RowView& view, char* out, const WriteGrid& g, unsigned x,
                                              const BlockRotation& rot) {
-    using Ln = Lanes<D>;
+    using Ln = Lanes<D, 2>;
     const unsigned sets = (unsigned)(g.heads + kBlocksQueryHeads - 1) / kBlocksQueryHeads;
     const unsigned y = x / sets, h0 = (x - y * sets) * kBlocksQueryHeads;
     const unsigned groups = (g.tokens + Ln::kStep - 1) / Ln::kStep, l = y / groups;
     const unsigned token = (y - l * groups) * Ln::kStep + threadIdx.x / Ln::kRow;
     if (token >= g.tokens) return;
     const int part = threadIdx.x % Ln::kRow;
-    const Pieces at = pieces_of<D>(part, rot, true);
+    const Pieces at = pieces_of<D>(part, rot);
     const unsigned b = token / (unsigned)g.T, t = token - b * g.T;
     const char* row = view.base + (size_t)l * view.s_layer + (size_t)b * view.s_batch + (size_t)t * view.s_token;
     const int pos = rot.position[token];
     Sixteen<T> raw[kBlocksQueryHeads];
 #pragma unroll
     for (int h = 0; h < kBlocksQueryHeads; ++h)
-        raw[h].template load<false>(row + (size_t)min((int)h0 + h, g.heads - 1) * view.s_head, at);
+        raw[h].load(row + (size_t)min((int)h0 + h, g.heads - 1) * view.s_head, at);
     Angles angles;
     angles.load(part, pos, rot, at.turned);
 #pragma unroll
     for (int h = 0; h < kBlocksQueryHeads; ++h) {
         if ((int)h0 + h >= g.heads) break;
         float z[16];
-        raw[h].turn(angles, rot.pairs, at.turned, [](double v) { return sizeof(T) == 2 ? to_odd(v) : (float)v; }, z);
+        raw[h].template turn<sizeof(T) == 2 ? Turned::Half : Turned::Float>(angles, rot.pairs, at.turned, z);
         char* o = out + ((((size_t)l * g.B + b) * g.heads + h0 + h) * g.T + t) * (D * sizeof(T));
         Eight<T>::store(o, at.a, *reinterpret_cast<const float(*)[8]>(z));
         Eight<T>::store(o, at.b, *reinterpret_cast<const float(*)[8]>(z + 8));
     }
 }
 
-// A workgroup takes the keys or the values of one block of a segment (layer, sample,
-// KV head), both and the heads of a page side by side: ITEMS rows per lane group.  A
-// decode step's call is a chain of memory latencies (slot, place, page, the block's
-// scale), so everything is loaded as soon as its address is known: the new rows and
-// their angles beside the look-up of the block.
-template <typename T, int D, int ITEMS, bool Gather>
-__global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv, RowView qv, char* __restrict__ q_out,
-                                                         WriteGrid g, const int32_t* __restrict__ idx,
-                                                         const int32_t* __restrict__ count,
-                                                         const int32_t* __restrict__ start,
-                                                         const int32_t* __restrict__ seq, BlockRotation rot,
-                                                         PagePool p) {
-    using Ln = Lanes<D>;
-    if constexpr (!Gather) {
-        if (blockIdx.x >= g.blocks) return turn_queries<T, D>(qv, q_out, g, blockIdx.x - g.blocks, rot);
+// A channel packed under a scale, and into the bounds of its kind.  Careful: there may
+// be infinities, NaN or magnitudes that no scale holds.
+template <bool Careful>
+struct Packer {
+    float scale, most;
+    __device__ __forceinline__ float take(float x) const { return Careful ? bounded(x, most) : x; }
+    __device__ __forceinline__ static float low(float a, float b) { return Careful ? lower(a, b) : fminf(a, b); }
+    __device__ __forceinline__ static float high(float a, float b) { return Careful ? higher(a, b) : fmaxf(a, b); }
+    // eight channels, with their bounds where Ends
+    template <bool Ends>
+    __device__ __forceinline__ u32x2 pack(float (&x)[8], float (&lo)[8], float (&hi)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = take(x[e]);
+            if constexpr (Ends) {
+                lo[e] = low(lo[e], x[e]);
+                hi[e] = high(hi[e], x[e]);
+            }
+        }
+        return u32x2{codes4(x[0], x[1], x[2], x[3], scale), codes4(x[4], x[5], x[6], x[7], scale)};
     }
-    __shared__ uint32_t s_top[kWaves];
-    __shared__ float s_ends[2][kWaves][D];
+};
+
+// The keys or the values (Ends: keys) of one block: NP pieces to a lane, ITEMS rows to
+// a lane group.  A decode step's call is a chain of memory latencies (slot, place,
+// page, the block's scale), so everything is loaded as soon as its address is known:
+// the new rows and their angles beside the look-up of the block.
+template <typename T, int D, int PAGE, int NP, bool Gather, bool Ends>
+__device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWaves][D], const RowView& view, int role,
+                                            const WriteGrid& g, int l, int b, int j, int i, size_t seg,
+                                            const int32_t* idx, int slot, int s0, int n, const BlockRotation& rot,
+                                            const PagePool& p) {
+    using Ln = Lanes<D, NP>;
+    constexpr int ITEMS = (PAGE + Ln::kStep - 1) / Ln::kStep, kShift = PAGE == 32 ? 5 : PAGE == 64 ? 6 : 7;
     const int part = threadIdx.x % Ln::kRow, in = threadIdx.x / Ln::kRow;
-    const unsigned role = blockIdx.x & 1, x2 = blockIdx.x >> 1;
-    const unsigned x1 = x2 / (unsigned)p.Hkv, lb = x1 / (unsigned)g.nblk;
-    const int j = (int)(x2 - x1 * p.Hkv), i = (int)(x1 - lb * g.nblk);
-    const int l = (int)(lb / (unsigned)g.B), b = (int)(lb - (unsigned)l * g.B);
-    const size_t seg = (size_t)lb * p.Hkv + j;
-    const int slot = slot_of(seq, b, p.S), s0 = start[b];
-    const int n = Gather ? min(count[seg], g.T) : count != nullptr ? min(count[b], g.T) : g.T;
-    if (slot < 0 || s0 < 0 || n <= 0) return;
-    const int at = min((s0 >> p.shift) + i, p.M);   // block of the sequence
+    const int at = min((s0 >> kShift) + i, p.M);   // block of the sequence
     const int page = p.table[(size_t)slot * p.M + min(at, p.M - 1)], held = held_of(p, slot);
-    const long long pos0 = (long long)at << p.shift;
-    const int r0 = (int)max(0LL, s0 - pos0), r1 = (int)min((long long)1 << p.shift, s0 + (long long)n - pos0);
+    const long long pos0 = (long long)at << kShift;
+    const int r0 = (int)max(0LL, s0 - pos0), r1 = (int)min((long long)PAGE, s0 + (long long)n - pos0);
     if (r1 <= r0) return;
 
-    const bool turn = !Gather && role == 0 && rot.cos != nullptr;
-    const Pieces pc = pieces_of<D>(part, rot, turn);
-    const RowView& view = role == 0 ? kv : vv;
+    Pieces pc{part, 0, false};
+    if constexpr (NP == 2) pc = pieces_of<D>(part, rot);
     const char* base = view.base + (size_t)l * view.s_layer + (size_t)b * view.s_batch + (size_t)j * view.s_head;
-    Sixteen<T> raw[ITEMS];
-    int from[ITEMS];  // Gather: the source row; else the row's position for its angles
+    Sixteen<T> two[NP == 2 ? ITEMS : 1];
+    Eight<T> one[NP == 1 ? ITEMS : 1];
+    Angles angles[NP == 2 ? ITEMS : 1];
+    int from[ITEMS];  // the source row, then its position
 #pragma unroll
     for (int it = 0; it < ITEMS; ++it) {
         const int row = it * Ln::kStep + in;
@@ -303,14 +344,18 @@ __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv,
     }
 #pragma unroll
     for (int it = 0; it < ITEMS; ++it) {
-        const bool there = it * Ln::kStep + in >= r0 && it * Ln::kStep + in < r1;
-        if (there && (!Gather || (from[it] >= 0 && from[it] < g.N)))
-            raw[it].template load<Gather>(base + (size_t)from[it] * view.s_token, pc);
-        else
-            raw[it] = Sixteen<T>{};
+        const int row = it * Ln::kStep + in;
+        const bool there = row >= r0 && row < r1 && (!Gather || (from[it] >= 0 && from[it] < g.N));
+        const char* at_row = base + (size_t)from[it] * view.s_token;
+        if constexpr (NP == 2) {
+            two[it] = Sixteen<T>{};
+            if (there) two[it].load(at_row, pc);
+        } else {
+            one[it] = Eight<T>{};
+            if (there) one[it].template load<Gather>(at_row, pc.a);
+        }
     }
-    Angles angles[ITEMS];
-    if (turn) {
+    if constexpr (NP == 2) {
 #pragma unroll
         for (int it = 0; it < ITEMS; ++it) from[it] = rot.position[(size_t)b * g.T + from[it]];
 #pragma unroll
@@ -318,111 +363,171 @@ __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv,
     }
     if (at >= held || page < 0 || page >= p.n_pages) return;
     char* block = block_at<D>(p, l, page, j);
-    char* tail = block + tail_at<D>(p.shift);
-    char* codes = block + ((size_t)(role * D) << p.shift);
+    char* tail = block + tail_at<D>(kShift);
+    char* codes = block + role * D * PAGE;
     const int old = r0 > 0 ? scale_of((uint8_t)tail[role]) : 0;
+    // four channels of one bound to a thread
+    uint32_t* ends = reinterpret_cast<uint32_t*>(tail + kBlockScales) + threadIdx.x % (2 * D / 4);
+    const uint32_t old_ends = Ends && r0 > 0 ? *ends : 0u;
 
-    // the rows' largest magnitude
-    float x[ITEMS][16];
+    // the rows' largest magnitude; rows that there are not are zeros
+    float x[ITEMS][NP][8];
     uint32_t top = 0;
 #pragma unroll
     for (int it = 0; it < ITEMS; ++it) {
-        if (it * Ln::kStep + in < r0 || it * Ln::kStep + in >= r1) continue;
-        if (turn)
-            raw[it].turn(angles[it], rot.pairs, pc.turned, to_odd, x[it]);
-        else
-            raw[it].floats(x[it]);
+        if constexpr (NP == 2) {
+            const int row = it * Ln::kStep + in;
+            if (row >= r0 && row < r1) {
+                float y[16];
+                two[it].template turn<Turned::Odd>(angles[it], rot.pairs, pc.turned, y);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const uint32_t bits = __float_as_uint(x[it][e]) & 0x7fffffffu;
-            top = max(top, bits < 0x7f800000u ? bits : 0u);
+                for (int e = 0; e < 16; ++e) x[it][e / 8][e % 8] = y[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[it][e / 8][e % 8] = 0.0f;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[it][0][e] = one[it].get(e);
         }
+#pragma unroll
+        for (int e = 0; e < 8 * NP; ++e) top = max(top, __float_as_uint(x[it][e / 8][e % 8]) & 0x7fffffffu);
     }
     const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
-    top = wave_max(top);
-    if (lane == 0) s_top[wv] = top;
-    __syncthreads();
+    auto over_all = [&](uint32_t y) {
+        y = wave_max(y);
+        if (lane == 0) s_top[wv] = y;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = max(top, s_top[w]);
+        for (int w = 0; w < kWaves; ++w) y = max(y, s_top[w]);
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)y);
+    };
+    top = over_all(top);
+    bool careful = top >= 0x7f800000u;
+    if (careful) {  // once more, of the finite ones
+        uint32_t finite = 0;
+#pragma unroll
+        for (int it = 0; it < ITEMS; ++it)
+#pragma unroll
+            for (int e = 0; e < 8 * NP; ++e) {
+                const uint32_t bits = __float_as_uint(x[it][e / 8][e % 8]) & 0x7fffffffu;
+                finite = max(finite, bits < 0x7f800000u ? bits : 0u);
+            }
+        __syncthreads();  // s_top is read
+        top = over_all(finite);
+    }
     const int s = max(scale_byte8(top), old);
-    const float scale = scale_float(s), most = 448.0f * scale;
+    careful |= s == kBlockScaleMax;
+    const float scale = scale_float(s);
     // rows under another scale: 2^-60 of it is zero like any smaller share
     const float factor = scale_float(127 - min(s - old, 60));
 
-    float lo[16], hi[16];
+    float lo[NP][8], hi[NP][8];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        lo[e] = INFINITY;
-        hi[e] = -INFINITY;
+    for (int e = 0; e < 8 * NP; ++e) {
+        lo[e / 8][e % 8] = INFINITY;
+        hi[e / 8][e % 8] = -INFINITY;
     }
+    auto pack = [&](auto packer) {
 #pragma unroll
-    for (int it = 0; it < ITEMS; ++it) {
-        const int row = it * Ln::kStep + in;
-        if (row >= r1) continue;
-        char* here = codes + (size_t)row * D;
-        if (row < r0) {
-            if (s == old) continue;
-            u32x4* sixteen = reinterpret_cast<u32x4*>(here) + part;
-            u32x4 w = *sixteen;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = rescale4(w[e], factor);
-            *sixteen = w;
-            continue;
+        for (int it = 0; it < ITEMS; ++it) {
+            const int row = it * Ln::kStep + in;
+            if (row < r0 || row >= r1) continue;
+            u32x2* here = reinterpret_cast<u32x2*>(codes + row * D);
+            here[pc.a] = packer.template pack<Ends>(x[it][0], lo[0], hi[0]);
+            if constexpr (NP == 2) here[pc.b] = packer.template pack<Ends>(x[it][1], lo[1], hi[1]);
         }
+    };
+    if (careful)
+        pack(Packer<true>{scale, 448.0f * scale});
+    else
+        pack(Packer<false>{scale, 0.0f});
+    if (s != old && r0 > 0) {  // what was there, 16 bytes at a time
+        for (int e = threadIdx.x; e < r0 * (D / 16); e += kThreads) {
+            u32x4* here = reinterpret_cast<u32x4*>(codes) + e;
+            u32x4 w = *here;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            x[it][e] = bounded(x[it][e], most);
-            lo[e] = lower(lo[e], x[it][e]);
-            hi[e] = higher(hi[e], x[it][e]);
+            for (int k = 0; k < 4; ++k) w[k] = rescale4(w[k], factor);
+            *here = w;
         }
-        u32x2 w[2];
-#pragma unroll
-        for (int h = 0; h < 4; ++h)
-            w[h / 2][h % 2] = codes4(x[it][4 * h], x[it][4 * h + 1], x[it][4 * h + 2], x[it][4 * h + 3], scale);
-        reinterpret_cast<u32x2*>(here)[pc.a] = w[0];
-        reinterpret_cast<u32x2*>(here)[pc.b] = w[1];
     }
     if (threadIdx.x == 0) tail[role] = (char)s;
-    if (role != 0) return;
-    // bounds: rounding keeps the order, so the bounds of the codes are the codes of the bounds
-    if (r1 - r0 > 1) {
+    if constexpr (Ends) {
+        // bounds: rounding keeps the order, so the bounds of the codes are the codes of the bounds
+        const bool single = r1 - r0 == 1;
+        if (!single) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            lo[e] = over_rows<Ln::kRow>(lo[e], lower);
-            hi[e] = over_rows<Ln::kRow>(hi[e], higher);
+            for (int e = 0; e < 8 * NP; ++e) {
+                float &a = lo[e / 8][e % 8], &c = hi[e / 8][e % 8];
+                a = careful ? over_rows<Ln::kRow>(a, lower) : over_rows<Ln::kRow>(a, fminf);
+                c = careful ? over_rows<Ln::kRow>(c, higher) : over_rows<Ln::kRow>(c, fmaxf);
+            }
+        }
+        // a wave's, or a single row's
+        if (single ? in == r0 % Ln::kStep : lane < Ln::kRow) {
+            const int w = single ? 0 : wv;
+#pragma unroll
+            for (int e = 0; e < 8 * NP; ++e) {
+                const int ch = 8 * (e < 8 ? pc.a : pc.b) + e % 8;
+                s_ends[0][w][ch] = lo[e / 8][e % 8];
+                s_ends[1][w][ch] = hi[e / 8][e % 8];
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x >= 2 * D / 4) return;
+        const int ch = threadIdx.x * 4 % D;
+        const bool upper = threadIdx.x * 4 >= D;
+        float was[4];
+        if (r0 > 0) floats4(rescale4(old_ends, factor), 1.0f, was);
+        float y[4];
+        const int waves = single ? 1 : kWaves;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            y[e] = s_ends[upper][0][ch + e];
+            for (int w = 1; w < waves; ++w) {
+                const float z = s_ends[upper][w][ch + e];
+                y[e] = upper ? higher(y[e], z) : lower(y[e], z);
+            }
+            // in units of the scale: old bounds are codes already
+            if (r0 > 0) y[e] = upper ? higher(y[e], was[e] * scale) : lower(y[e], was[e] * scale);
+        }
+        *ends = codes4(y[0], y[1], y[2], y[3], scale);
+    }
+}
+
+// A workgroup takes the keys or the values of one block of a segment (layer, sample,
+// KV head), both and the heads of a page side by side.
+template <typename T, int D, int PAGE, bool Gather>
+__global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv, RowView qv, char* __restrict__ q_out,
+                                                         WriteGrid g, const int32_t* __restrict__ idx,
+                                                         const int32_t* __restrict__ count,
+                                                         const int32_t* __restrict__ start,
+                                                         const int32_t* __restrict__ seq, BlockRotation rot,
+                                                         PagePool p) {
+    if constexpr (!Gather) {
+        if (blockIdx.x >= g.blocks) return turn_queries<T, D>(qv, q_out, g, blockIdx.x - g.blocks, rot);
+    }
+    __shared__ uint32_t s_top[kWaves];
+    __shared__ float s_ends[2][kWaves][D];
+    const unsigned role = blockIdx.x & 1, x2 = blockIdx.x >> 1;
+    const unsigned x1 = x2 / (unsigned)p.Hkv, lb = x1 / (unsigned)g.nblk;
+    const int j = (int)(x2 - x1 * p.Hkv), i = (int)(x1 - lb * g.nblk);
+    const int l = (int)(lb / (unsigned)g.B), b = (int)(lb - (unsigned)l * g.B);
+    const size_t seg = (size_t)lb * p.Hkv + j;
+    const int slot = slot_of(seq, b, p.S), s0 = start[b];
+    const int n = Gather ? min(count[seg], g.T) : count != nullptr ? min(count[b], g.T) : g.T;
+    if (slot < 0 || s0 < 0 || n <= 0) return;
+    if (role != 0) {
+        write_block<T, D, PAGE, 1, Gather, false>(s_top, s_ends, vv, 1, g, l, b, j, i, seg, idx, slot, s0, n, rot, p);
+        return;
+    }
+    if constexpr (!Gather) {
+        if (rot.cos != nullptr) {
+            write_block<T, D, PAGE, 2, false, true>(s_top, s_ends, kv, 0, g, l, b, j, i, seg, idx, slot, s0, n, rot, p);
+            return;
         }
     }
-    // a wave's, or a single row's
-    if (r1 - r0 > 1 ? lane < Ln::kRow : in == r0 % Ln::kStep) {
-        const int w = r1 - r0 > 1 ? wv : 0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int ch = 8 * (e < 8 ? pc.a : pc.b) + e % 8;
-            s_ends[0][w][ch] = lo[e];
-            s_ends[1][w][ch] = hi[e];
-        }
-    }
-    __syncthreads();
-    // four channels of one bound to a thread
-    if (threadIdx.x >= 2 * D / 4) return;
-    const int ch = threadIdx.x * 4 % D;
-    const bool upper = threadIdx.x * 4 >= D;
-    uint32_t* out = reinterpret_cast<uint32_t*>(tail + kBlockScales) + threadIdx.x;
-    float was[4];
-    if (r0 > 0) floats4(rescale4(*out, factor), 1.0f, was);
-    float y[4];
-    const int waves = r1 - r0 > 1 ? kWaves : 1;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        y[e] = s_ends[upper][0][ch + e];
-        for (int w = 1; w < waves; ++w) {
-            const float z = s_ends[upper][w][ch + e];
-            y[e] = upper ? higher(y[e], z) : lower(y[e], z);
-        }
-        // in units of the scale: old bounds are codes already
-        if (r0 > 0) y[e] = upper ? higher(y[e], was[e] * scale) : lower(y[e], was[e] * scale);
-    }
-    *out = codes4(y[0], y[1], y[2], y[3], scale);
+    write_block<T, D, PAGE, 1, Gather, true>(s_top, s_ends, kv, 0, g, l, b, j, i, seg, idx, slot, s0, n, rot, p);
 }
 
 // ---------------------------------------------------------------------------
@@ -493,29 +598,28 @@ __global__ __launch_bounds__(kThreads) void read_blocks(PagePool p, ReadGrid g, 
     }
 }
 
-template <typename T, int D, int ITEMS>
-void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, const WriteGrid& g,
-               unsigned groups, const int32_t* idx, const int32_t* count, const int32_t* start, const int32_t* seq,
+template <typename T, int D, int PAGE>
+void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, const WriteGrid& g, unsigned groups,
+               const int32_t* idx, const int32_t* count, const int32_t* start, const int32_t* seq,
                const BlockRotation& rot, const PagePool& p, hipStream_t st) {
     if (idx != nullptr)
-        hipLaunchKernelGGL((write_blocks<T, D, ITEMS, true>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out,
-                           g, idx, count, start, seq, rot, p);
+        hipLaunchKernelGGL((write_blocks<T, D, PAGE, true>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out, g, idx,
+                           count, start, seq, rot, p);
     else
-        hipLaunchKernelGGL((write_blocks<T, D, ITEMS, false>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out,
-                           g, idx, count, start, seq, rot, p);
+        hipLaunchKernelGGL((write_blocks<T, D, PAGE, false>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out, g,
+                           idx, count, start, seq, rot, p);
 }
 
 template <typename T, int D>
-void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, const WriteGrid& g,
-               unsigned groups, const int32_t* idx, const int32_t* count, const int32_t* start, const int32_t* seq,
+void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out, const WriteGrid& g, unsigned groups,
+               const int32_t* idx, const int32_t* count, const int32_t* start, const int32_t* seq,
                const BlockRotation& rot, const PagePool& p, hipStream_t st) {
-    constexpr int kStep = Lanes<D>::kStep;
     if (p.shift == 5)
-        run_write<T, D, (32 + kStep - 1) / kStep>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
+        run_write<T, D, 32>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
     else if (p.shift == 6)
-        run_write<T, D, 64 / kStep>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
+        run_write<T, D, 64>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
     else
-        run_write<T, D, 128 / kStep>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
+        run_write<T, D, 128>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
 }
 
 template <typename T, int D, bool Bounds>
@@ -548,7 +652,7 @@ hipError_t launch_blocks_write(const RowView& k, const RowView& v, const RowView
     if (cap == 0) return hipSuccess;
     WriteGrid g{B, cap, N, (int)blocks_touched(cap, 1 << p.shift), Hq, 0, (unsigned)B * cap};
     g.blocks = 2u * p.L * B * p.Hkv * g.nblk;
-    const unsigned step = d == 128 ? Lanes<128>::kStep : Lanes<64>::kStep;
+    const unsigned step = d == 128 ? Lanes<128, 2>::kStep : Lanes<64, 2>::kStep;
     const unsigned groups =
         g.blocks + (q_out == nullptr ? 0u : (unsigned)p.L * ((g.tokens + step - 1) / step) *
                                                 ((unsigned)(Hq + kBlocksQueryHeads - 1) / kBlocksQueryHeads));

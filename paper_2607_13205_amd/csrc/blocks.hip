@@ -67,10 +67,9 @@ struct Eight {
 __device__ __forceinline__ float to_odd(double y) {
     const float f = (float)y;
     const double back = (double)f;
-    if (back == y || !(fabs(y) < INFINITY)) return f;
-    uint32_t bits = __float_as_uint(f);
-    bits -= fabs(back) > fabs(y) ? 1u : 0u;
-    return __uint_as_float(bits | 1u);
+    const uint32_t bits = __float_as_uint(f);
+    const bool kept = back == y | !(fabs(y) < INFINITY);
+    return __uint_as_float(kept ? bits : (bits - (uint32_t)(fabs(back) > fabs(y))) | 1u);
 }
 
 // A lane of a turned row takes two pieces of eight channels, `a` and `b`, which hold
@@ -116,11 +115,11 @@ struct Sixteen {
         a.template load<false>(row, at.a);
         b.template load<false>(row, at.b);
     }
-    // Pair i of a row's pieces: channels i of the two, or neighbours of one.
-    __device__ __forceinline__ static void pair(const float (&x)[16], bool pairs, int i, float& u, float& w) {
-        u = pairs ? x[2 * i] : x[i];
-        w = pairs ? x[2 * i + 1] : x[8 + i];
-    }
+    // Pair i of a row's pieces: neighbours of one (Pairs), or channels i of the two.
+    template <bool Pairs>
+    static constexpr int first(int i) { return Pairs ? 2 * i : i; }
+    template <bool Pairs>
+    static constexpr int second(int i) { return Pairs ? 2 * i + 1 : 8 + i; }
     // Turned in 32 bits with the products' errors: y is off by less than three steps of
     // float32 (u c - p is rounded once, and the sum with the exact error of p once, each by
     // half a step, where the error is not what is left of it).  That decides every later
@@ -128,14 +127,13 @@ struct Sixteen {
     // zero bits, those of bfloat16 in a one and 15 zeros.  Returns whether all are decided;
     // 64 bits otherwise (a chunk of 1003 tokens, 32 and 8 heads: 25.6 us with 64 bits
     // throughout).
-    template <Turned How>
-    __device__ __forceinline__ static bool fast(const float (&x)[16], const Angles& g, bool pairs, float (&y)[16]) {
+    template <Turned How, bool Pairs>
+    __device__ __forceinline__ static bool fast(const float (&x)[16], const Angles& g, float (&y)[16]) {
         uint32_t border = 0xffffu;
         float clear = INFINITY, most = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float u, w;
-            pair(x, pairs, i, u, w);
+            const float u = x[first<Pairs>(i)], w = x[second<Pairs>(i)];
             const float c = g.cos[i / 4][i % 4], s = g.sin[i / 4][i % 4];
             const float p = w * s, q = u * s, ep = fmaf(w, s, -p), eq = fmaf(u, s, -q);
             const float lo = fmaf(u, c, -p) - ep, hi = fmaf(w, c, q) + eq;
@@ -143,10 +141,26 @@ struct Sixteen {
             border = min(border, min((__float_as_uint(lo) + kAt) & 0xffffu, (__float_as_uint(hi) + kAt) & 0xffffu));
             clear = fminf(clear, fminf(fmaf(-4.0f, fabsf(ep), fabsf(lo)), fmaf(-4.0f, fabsf(eq), fabsf(hi))));
             most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
-            y[i] = lo;
-            y[8 + i] = hi;
+            y[first<Pairs>(i)] = lo;
+            y[second<Pairs>(i)] = hi;
         }
         return border > 6 && clear > 0x1p-90f && most < 0x1p120f;
+    }
+    template <Turned How, bool Pairs>
+    __device__ __forceinline__ static void turn(const Angles& g, float (&x)[16]) {
+        float y[16];
+        if (How == Turned::Float || !fast<How, Pairs>(x, g, y)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double u = x[first<Pairs>(i)], w = x[second<Pairs>(i)];
+                const double c = g.cos[i / 4][i % 4], s = g.sin[i / 4][i % 4];
+                const double lo = fma(u, c, -(w * s)), hi = fma(w, c, u * s);
+                y[first<Pairs>(i)] = How == Turned::Float ? (float)lo : to_odd(lo);
+                y[second<Pairs>(i)] = How == Turned::Float ? (float)hi : to_odd(hi);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = y[e];
     }
     template <Turned How>
     __device__ __forceinline__ void turn(const Angles& g, bool pairs, bool turned, float (&x)[16]) const {
@@ -158,25 +172,11 @@ struct Sixteen {
         if (!g.there) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(0x7fc00000u);
-            return;
-        }
-        if (!turned) return;
-        float y[16];
-        if (How == Turned::Float || !fast<How>(x, g, pairs, y)) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float u, w;
-                pair(x, pairs, i, u, w);
-                const double c = g.cos[i / 4][i % 4], s = g.sin[i / 4][i % 4];
-                const double lo = fma((double)u, c, -((double)w * s)), hi = fma((double)w, c, (double)u * s);
-                y[i] = How == Turned::Float ? (float)lo : to_odd(lo);
-                y[8 + i] = How == Turned::Float ? (float)hi : to_odd(hi);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[2 * i] = pairs ? y[i] : y[2 * i];
-            x[2 * i + 1] = pairs ? y[8 + i] : y[2 * i + 1];
+        } else if (turned) {
+            if (pairs)
+                turn<How, true>(g, x);
+            else
+                turn<How, false>(g, x);
         }
     }
 };
@@ -210,15 +210,6 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float factor) {
     return codes4(x[0], x[1], x[2], x[3], 1.0f);
 }
 
-// x of lane ^ 16, or ^ 32, beside x: the two results of a swap with itself hold both.
-template <typename F>
-__device__ __forceinline__ uint32_t over_halves(uint32_t x, F f) {
-    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = f(a[0], a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return f(b[0], b[1]);
-}
-
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
@@ -230,17 +221,41 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
     x = max(x, dpp<0x4e>(x));   // lanes 2 3 0 1
     x = max(x, dpp<0x141>(x));  // mirrored within eight
     x = max(x, dpp<0x140>(x));  // within sixteen
-    return over_halves(x, [](uint32_t a, uint32_t b) { return max(a, b); });
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);  // lane ^ 16 and the lane itself
+    x = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
 }
 
-// f over the lanes of a wave that hold the same pieces of its rows, ROW lanes to a row.
-template <int ROW, typename F>
-__device__ __forceinline__ float over_rows(float x, F f) {
-    auto g = [&](uint32_t a, uint32_t b) { return __float_as_uint(f(__uint_as_float(a), __uint_as_float(b))); };
-    uint32_t y = __float_as_uint(x);
-    if constexpr (ROW <= 4) y = g(y, dpp<0x124>(y));  // rotated by four, then by eight
-    if constexpr (ROW <= 8) y = g(y, dpp<0x128>(y));
-    return __uint_as_float(over_halves(y, g));
+// f over the four rows of sixteen lanes of a wave, of N values of each lane: a swap of
+// halves leaves either half of the lanes with half of the values, each beside that of
+// the other half.  Lane l is left with values N / 4 ((l >> 4 & 1) + 2 (l >> 5)) .. + N / 4,
+// in x[0 .. N / 4).
+template <int N, typename F>
+__device__ __forceinline__ void over_quarters(float (&x)[N], F f) {
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[e]), __float_as_uint(x[e + N / 2]), false, false);
+        x[e] = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+#pragma unroll
+    for (int e = 0; e < N / 4; ++e) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(x[e + N / 4]), false, false);
+        x[e] = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+}
+
+// The smallest and largest of three, a quiet NaN passed over (fminf spends an
+// instruction on what could be a signalling one).
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
 }
 
 // What a call writes.
@@ -248,6 +263,10 @@ struct WriteGrid {
     int B, T, N, nblk, heads;  // nblk: blocks per segment; heads: of the queries
     unsigned blocks, tokens;   // workgroups that take blocks, those behind them take queries; B T
 };
+
+// Partial bounds that a wave leaves: its rows are D / 16 lanes wide at least.
+template <int D>
+constexpr int kParts = 256 / D;
 
 // NP pieces of eight channels to a lane.
 template <int D, int NP>
@@ -288,35 +307,12 @@ __device__ __forceinline__ void turn_queries(const RowView& view, char* out, con
     }
 }
 
-// A channel packed under a scale, and into the bounds of its kind.  Careful: there may
-// be infinities, NaN or magnitudes that no scale holds.
-template <bool Careful>
-struct Packer {
-    float scale, most;
-    __device__ __forceinline__ float take(float x) const { return Careful ? bounded(x, most) : x; }
-    __device__ __forceinline__ static float low(float a, float b) { return Careful ? lower(a, b) : fminf(a, b); }
-    __device__ __forceinline__ static float high(float a, float b) { return Careful ? higher(a, b) : fmaxf(a, b); }
-    // eight channels, with their bounds where Ends
-    template <bool Ends>
-    __device__ __forceinline__ u32x2 pack(float (&x)[8], float (&lo)[8], float (&hi)[8]) const {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = take(x[e]);
-            if constexpr (Ends) {
-                lo[e] = low(lo[e], x[e]);
-                hi[e] = high(hi[e], x[e]);
-            }
-        }
-        return u32x2{codes4(x[0], x[1], x[2], x[3], scale), codes4(x[4], x[5], x[6], x[7], scale)};
-    }
-};
-
 // The keys or the values (Ends: keys) of one block: NP pieces to a lane, ITEMS rows to
 // a lane group.  A decode step's call is a chain of memory latencies (slot, place,
 // page, the block's scale), so everything is loaded as soon as its address is known:
 // the new rows and their angles beside the look-up of the block.
 template <typename T, int D, int PAGE, int NP, bool Gather, bool Ends>
-__device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWaves][D], const RowView& view, int role,
+__device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWaves * kParts<D>][D], const RowView& view, int role,
                                             const WriteGrid& g, int l, int b, int j, int i, size_t seg,
                                             const int32_t* idx, int slot, int s0, int n, const BlockRotation& rot,
                                             const PagePool& p) {
@@ -366,9 +362,9 @@ __device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWa
     char* tail = block + tail_at<D>(kShift);
     char* codes = block + role * D * PAGE;
     const int old = r0 > 0 ? scale_of((uint8_t)tail[role]) : 0;
-    // four channels of one bound to a thread
-    uint32_t* ends = reinterpret_cast<uint32_t*>(tail + kBlockScales) + threadIdx.x % (2 * D / 4);
-    const uint32_t old_ends = Ends && r0 > 0 ? *ends : 0u;
+    // a channel of one bound to a thread
+    char* end = tail + kBlockScales + threadIdx.x % (2 * D);
+    const uint32_t old_end = Ends && r0 > 0 ? (uint8_t)*end : 0u;
 
     // the rows' largest magnitude; rows that there are not are zeros
     float x[ITEMS][NP][8];
@@ -422,26 +418,34 @@ __device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWa
     // rows under another scale: 2^-60 of it is zero like any smaller share
     const float factor = scale_float(127 - min(s - old, 60));
 
-    float lo[NP][8], hi[NP][8];
+    const bool single = r1 - r0 == 1;
+    const bool whole = r0 == 0 && r1 == PAGE && PAGE % Ln::kStep == 0;
+    float lo[8 * NP], hi[8 * NP];
+    if (careful) {
 #pragma unroll
-    for (int e = 0; e < 8 * NP; ++e) {
-        lo[e / 8][e % 8] = INFINITY;
-        hi[e / 8][e % 8] = -INFINITY;
+        for (int it = 0; it < ITEMS; ++it)
+#pragma unroll
+            for (int e = 0; e < 8 * NP; ++e) {
+                const int row = it * Ln::kStep + in;
+                float& y = x[it][e / 8][e % 8];
+                y = bounded(y, 448.0f * scale);
+                const bool there = row >= r0 && row < r1;
+                lo[e] = lower(it == 0 ? INFINITY : lo[e], there ? y : INFINITY);
+                hi[e] = higher(it == 0 ? -INFINITY : hi[e], there ? y : -INFINITY);
+            }
     }
-    auto pack = [&](auto packer) {
 #pragma unroll
-        for (int it = 0; it < ITEMS; ++it) {
-            const int row = it * Ln::kStep + in;
-            if (row < r0 || row >= r1) continue;
-            u32x2* here = reinterpret_cast<u32x2*>(codes + row * D);
-            here[pc.a] = packer.template pack<Ends>(x[it][0], lo[0], hi[0]);
-            if constexpr (NP == 2) here[pc.b] = packer.template pack<Ends>(x[it][1], lo[1], hi[1]);
+    for (int it = 0; it < ITEMS; ++it) {
+        const int row = it * Ln::kStep + in;
+        if (row < r0 || row >= r1) continue;
+        u32x2* here = reinterpret_cast<u32x2*>(codes + row * D);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            const float(&y)[8] = x[it][k];
+            here[k == 0 ? pc.a : pc.b] =
+                u32x2{codes4(y[0], y[1], y[2], y[3], scale), codes4(y[4], y[5], y[6], y[7], scale)};
         }
-    };
-    if (careful)
-        pack(Packer<true>{scale, 448.0f * scale});
-    else
-        pack(Packer<false>{scale, 0.0f});
+    }
     if (s != old && r0 > 0) {  // what was there, 16 bytes at a time
         for (int e = threadIdx.x; e < r0 * (D / 16); e += kThreads) {
             u32x4* here = reinterpret_cast<u32x4*>(codes) + e;
@@ -453,45 +457,80 @@ __device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWa
     }
     if (threadIdx.x == 0) tail[role] = (char)s;
     if constexpr (Ends) {
-        // bounds: rounding keeps the order, so the bounds of the codes are the codes of the bounds
-        const bool single = r1 - r0 == 1;
-        if (!single) {
+        // bounds: rounding keeps the order, so the bounds of the codes are the codes of the
+        // bounds.  Where all is finite, NaN stand for rows that there are not.
+        constexpr int kLeft = 2 * NP;  // of a lane's channels, once the wave's quarters are together
+        if (!careful) {
+            if (!whole)
+#pragma unroll
+                for (int it = 0; it < ITEMS; ++it) {
+                    const int row = it * Ln::kStep + in;
+                    const bool there = row >= r0 && row < r1;
+#pragma unroll
+                    for (int e = 0; e < 8 * NP; ++e) {
+                        float& y = x[it][e / 8][e % 8];
+                        y = there ? y : __uint_as_float(0x7fc00000u);
+                    }
+                }
 #pragma unroll
             for (int e = 0; e < 8 * NP; ++e) {
-                float &a = lo[e / 8][e % 8], &c = hi[e / 8][e % 8];
-                a = careful ? over_rows<Ln::kRow>(a, lower) : over_rows<Ln::kRow>(a, fminf);
-                c = careful ? over_rows<Ln::kRow>(c, higher) : over_rows<Ln::kRow>(c, fmaxf);
+                lo[e] = hi[e] = x[0][e / 8][e % 8];
+#pragma unroll
+                for (int it = 1; it < ITEMS; it += 2) {
+                    const float a = x[it][e / 8][e % 8], c = x[it + 1 < ITEMS ? it + 1 : it][e / 8][e % 8];
+                    lo[e] = min3(lo[e], a, c);
+                    hi[e] = max3(hi[e], a, c);
+                }
             }
         }
-        // a wave's, or a single row's
-        if (single ? in == r0 % Ln::kStep : lane < Ln::kRow) {
-            const int w = single ? 0 : wv;
+        const int quarter = ((lane >> 4) & 1) + 2 * (lane >> 5);
+        if (!single) {
+            if (careful) {
+                over_quarters(lo, lower);
+                over_quarters(hi, higher);
+            } else {
+                over_quarters(lo, [](float a, float c) { return min3(a, c, c); });
+                over_quarters(hi, [](float a, float c) { return max3(a, c, c); });
+            }
+            const int w = wv * kParts<D> + (lane & 15) / Ln::kRow;
+#pragma unroll
+            for (int e = 0; e < kLeft; ++e) {
+                const int at_e = quarter * kLeft + e;
+                const int ch = 8 * (at_e < 8 ? pc.a : pc.b) + at_e % 8;
+                s_ends[0][w][ch] = lo[e];
+                s_ends[1][w][ch] = hi[e];
+            }
+        } else if (in == r0 % Ln::kStep) {
 #pragma unroll
             for (int e = 0; e < 8 * NP; ++e) {
                 const int ch = 8 * (e < 8 ? pc.a : pc.b) + e % 8;
-                s_ends[0][w][ch] = lo[e / 8][e % 8];
-                s_ends[1][w][ch] = hi[e / 8][e % 8];
+                s_ends[0][0][ch] = lo[e];
+                s_ends[1][0][ch] = hi[e];
             }
         }
         __syncthreads();
-        if (threadIdx.x >= 2 * D / 4) return;
-        const int ch = threadIdx.x * 4 % D;
-        const bool upper = threadIdx.x * 4 >= D;
-        float was[4];
-        if (r0 > 0) floats4(rescale4(old_ends, factor), 1.0f, was);
-        float y[4];
-        const int waves = single ? 1 : kWaves;
+        if (threadIdx.x >= 2 * D) return;
+        const int ch = threadIdx.x % D;
+        const bool upper = threadIdx.x >= D;
+        constexpr int kOf = Ln::kRow >= 16 ? 1 : 16 / Ln::kRow;  // of a wave's partial bounds, those written
+        float y = s_ends[upper][0][ch];
+        if (!single)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            y[e] = s_ends[upper][0][ch + e];
-            for (int w = 1; w < waves; ++w) {
-                const float z = s_ends[upper][w][ch + e];
-                y[e] = upper ? higher(y[e], z) : lower(y[e], z);
-            }
-            // in units of the scale: old bounds are codes already
-            if (r0 > 0) y[e] = upper ? higher(y[e], was[e] * scale) : lower(y[e], was[e] * scale);
+            for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+                for (int k = 0; k < kOf; ++k) {
+                    const float z = s_ends[upper][w * kParts<D> + k][ch];
+                    if (careful)
+                        y = upper ? higher(y, z) : lower(y, z);
+                    else
+                        y = upper ? max3(y, z, z) : min3(y, z, z);
+                }
+        if (r0 > 0) {  // the old bound in the new scale is a code's value
+            float was[4];
+            floats4(rescale4(old_end, factor), scale, was);
+            y = upper ? higher(y, was[0]) : lower(y, was[0]);
         }
-        *ends = codes4(y[0], y[1], y[2], y[3], scale);
+        *end = (char)codes4(y, y, y, y, scale);
     }
 }
 
@@ -508,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv,
         if (blockIdx.x >= g.blocks) return turn_queries<T, D>(qv, q_out, g, blockIdx.x - g.blocks, rot);
     }
     __shared__ uint32_t s_top[kWaves];
-    __shared__ float s_ends[2][kWaves][D];
+    __shared__ float s_ends[2][kWaves * kParts<D>][D];
     const unsigned role = blockIdx.x & 1, x2 = blockIdx.x >> 1;
     const unsigned x1 = x2 / (unsigned)p.Hkv, lb = x1 / (unsigned)g.nblk;
     const int j = (int)(x2 - x1 * p.Hkv), i = (int)(x1 - lb * g.nblk);

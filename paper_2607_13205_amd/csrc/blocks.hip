@@ -569,6 +569,147 @@ __global__ __launch_bounds__(kThreads) void write_blocks(RowView kv, RowView vv,
     write_block<T, D, PAGE, 1, Gather, true>(s_top, s_ends, kv, 0, g, l, b, j, i, seg, idx, slot, s0, n, rot, p);
 }
 
+// Eight channels of a row, one piece to a lane: the other channels of its pairs are
+// loaded beside it.  Turned as Sixteen turns them.
+template <typename T, int D, bool Pairs>
+__device__ __forceinline__ void turn_eight(const Eight<T>& own, const Eight<T>& other, const Angles& g, bool low,
+                                           float (&x)[8]) {
+    uint32_t border = 0xffffu;
+    float clear = INFINITY, most = 0.0f;
+    float u[8], w[8], c[8], s[8];  // x[e] = u c + w s
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        u[e] = own.get(e);
+        w[e] = Pairs ? own.get(e ^ 1) : other.get(e);
+        const int i = Pairs ? e / 2 : e;
+        c[e] = g.cos[i / 4][i % 4];
+        s[e] = g.sin[i / 4][i % 4];
+        s[e] = (Pairs ? e % 2 == 0 : low) ? -s[e] : s[e];
+        const float p = w[e] * s[e], ep = fmaf(w[e], s[e], -p);
+        x[e] = fmaf(u[e], c[e], p) + ep;
+        border = min(border, (__float_as_uint(x[e]) + 3u) & 0xffffu);
+        clear = fminf(clear, fmaf(-4.0f, fabsf(ep), fabsf(x[e])));
+        most = fmaxf(most, fabsf(x[e]));
+    }
+    if (border > 6 && clear > 0x1p-90f && most < 0x1p120f) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = to_odd(fma((double)u[e], (double)c[e], (double)w[e] * s[e]));
+}
+
+// Codes of eight channels after another rounding, and NaN told.
+__device__ __forceinline__ void floats8(u32x2 w, float scale, float (&x)[8]) {
+    floats4(w[0], scale, *reinterpret_cast<float(*)[4]>(x));
+    floats4(w[1], scale, *reinterpret_cast<float(*)[4]>(x + 4));
+}
+
+// One row of each sample, a decode step's: D / 8 lanes take a segment's key, as many its
+// value, without LDS or barriers.  A workgroup to each block has one row in 64 places of
+// threads to work on: 256 samples, 8 KV heads 14.7 us so, rotated 17.6.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void write_rows(RowView kv, RowView vv, RowView qv, char* __restrict__ q_out,
+                                                       WriteGrid g, const int32_t* __restrict__ count,
+                                                       const int32_t* __restrict__ start,
+                                                       const int32_t* __restrict__ seq, BlockRotation rot, PagePool p) {
+    constexpr int kRow = D / 8, kSegs = kThreads / (2 * kRow);
+    if (blockIdx.x >= g.blocks) return turn_queries<T, D>(qv, q_out, g, blockIdx.x - g.blocks, rot);
+    const int part = threadIdx.x % kRow, role = threadIdx.x / kRow % 2;
+    const unsigned seg = blockIdx.x * kSegs + threadIdx.x / (2 * kRow);
+    const unsigned lb = seg / (unsigned)p.Hkv;
+    const int j = (int)(seg - lb * p.Hkv), l = (int)(lb / (unsigned)g.B), b = (int)(lb - (unsigned)l * g.B);
+    if (l >= p.L) return;
+    const int slot = slot_of(seq, b, p.S), s0 = start[b];
+    if (slot < 0 || s0 < 0 || (count != nullptr && count[b] <= 0)) return;
+    const int at = s0 >> p.shift, r0 = s0 & ((1 << p.shift) - 1);
+    const int page = p.table[(size_t)slot * p.M + min(at, p.M - 1)], held = held_of(p, slot);
+    const RowView& view = role == 0 ? kv : vv;
+    const char* row = view.base + (size_t)l * view.s_layer + (size_t)b * view.s_batch + (size_t)j * view.s_head;
+    const int half = rot.r / 16;  // pieces of half the turned channels
+    const bool turn = role == 0 && rot.cos != nullptr, turned = turn && part < 2 * half, low = part < half;
+    Eight<T> own, other;
+    own.template load<false>(row, part);
+    other = own;
+    Angles angles;
+    angles.there = true;
+    if (turn) {
+        const int pos = rot.position[b];
+        if (turned && !rot.pairs) other.template load<false>(row, low ? part + half : part - half);
+        angles.there = pos >= 0 && pos < rot.P;
+        if (angles.there && turned) {
+            const size_t first = (size_t)pos * (rot.r / 2) + (rot.pairs ? 4 * part : 8 * (low ? part : part - half));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                // neighbouring pairs: four angles to a piece
+                const size_t four = first + (rot.pairs ? 0 : 4 * i);
+                angles.cos[i] = *reinterpret_cast<const f32x4*>(rot.cos + four);
+                angles.sin[i] = *reinterpret_cast<const f32x4*>(rot.sin + four);
+            }
+        }
+    }
+    if (at >= held || page < 0 || page >= p.n_pages) return;
+    char* block = block_at<D>(p, l, page, j);
+    char* tail = block + tail_at<D>(p.shift);
+    u32x2* codes = reinterpret_cast<u32x2*>(block + ((size_t)(role * D) << p.shift)) + part;  // of row 0
+    u32x2* ends = reinterpret_cast<u32x2*>(tail + kBlockScales) + part;                       // minima, then maxima
+    int old = 0;
+    u32x2 was[2] = {};
+    if (r0 > 0) {
+        old = scale_of((uint8_t)tail[role]);
+        if (role == 0) {
+            was[0] = ends[0];
+            was[1] = ends[kRow];
+        }
+    }
+    float x[8];
+    if (turned && angles.there) {
+        if (rot.pairs)
+            turn_eight<T, D, true>(own, other, angles, low, x);
+        else
+            turn_eight<T, D, false>(own, other, angles, low, x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = angles.there ? own.get(e) : __uint_as_float(0x7fc00000u);
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = __float_as_uint(x[e]) & 0x7fffffffu;
+        top = max(top, bits < 0x7f800000u ? bits : 0u);
+    }
+    top = max(top, dpp<0xb1>(top));
+    top = max(top, dpp<0x4e>(top));
+    top = max(top, dpp<0x141>(top));
+    if constexpr (kRow == 16) top = max(top, dpp<0x140>(top));
+    const int s = max(scale_byte8(top), old);
+    const float scale = scale_float(s), factor = scale_float(127 - min(s - old, 60));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = bounded(x[e], 448.0f * scale);
+    codes[r0 * kRow] = u32x2{codes4(x[0], x[1], x[2], x[3], scale), codes4(x[4], x[5], x[6], x[7], scale)};
+    if (r0 > 0 && s != old)
+        for (int e0 = 0; e0 < r0; e0 += 16) {  // what was there, sixteen rows in flight
+            u32x2 w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = codes[min(e0 + e, r0 - 1) * kRow];
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (e0 + e < r0) codes[(e0 + e) * kRow] = u32x2{rescale4(w[e][0], factor), rescale4(w[e][1], factor)};
+        }
+    if (part == 0) tail[role] = (char)s;
+    if (role != 0) return;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        float y[8];
+        if (r0 > 0) {
+            floats8(u32x2{rescale4(was[k][0], factor), rescale4(was[k][1], factor)}, scale, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = k == 0 ? lower(x[e], y[e]) : higher(x[e], y[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = x[e];
+        }
+        ends[k * kRow] = u32x2{codes4(y[0], y[1], y[2], y[3], scale), codes4(y[4], y[5], y[6], y[7], scale)};
+    }
+}
+
 // ---------------------------------------------------------------------------
 // rows and bounds out of blocks
 // ---------------------------------------------------------------------------
@@ -690,12 +831,20 @@ hipError_t launch_blocks_write(const RowView& k, const RowView& v, const RowView
                                hipStream_t st) {
     if (cap == 0) return hipSuccess;
     WriteGrid g{B, cap, N, (int)blocks_touched(cap, 1 << p.shift), Hq, 0, (unsigned)B * cap};
-    g.blocks = 2u * p.L * B * p.Hkv * g.nblk;
+    const bool single = cap == 1 && idx == nullptr;
+    const unsigned segs = (unsigned)p.L * B * p.Hkv, per = kThreads / (d / 4);  // write_rows' segments per workgroup
+    g.blocks = single ? (segs + per - 1) / per : 2u * segs * g.nblk;
     const unsigned step = d == 128 ? Lanes<128, 2>::kStep : Lanes<64, 2>::kStep;
     const unsigned groups =
         g.blocks + (q_out == nullptr ? 0u : (unsigned)p.L * ((g.tokens + step - 1) / step) *
                                                 ((unsigned)(Hq + kBlocksQueryHeads - 1) / kBlocksQueryHeads));
     char* o = static_cast<char*>(q_out);
+    auto rows = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(groups), dim3(kThreads), 0, st, k, v, q, o, g, count, start, seq, rot, p);
+        return hipGetLastError();
+    };
+    if (single && dtype == 0) return d == 128 ? rows(write_rows<__bf16, 128>) : rows(write_rows<__bf16, 64>);
+    if (single) return d == 128 ? rows(write_rows<float, 128>) : rows(write_rows<float, 64>);
     if (dtype == 0 && d == 128) run_write<__bf16, 128>(k, v, q, o, g, groups, idx, count, start, seq, rot, p, st);
     if (dtype == 0 && d == 64) run_write<__bf16, 64>(k, v, q, o, g, groups, idx, count, start, seq, rot, p, st);
     if (dtype == 1 && d == 128) run_write<float, 128>(k, v, q, o, g, groups, idx, count, start, seq, rot, p, st);

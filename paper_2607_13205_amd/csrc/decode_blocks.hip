@@ -155,7 +155,8 @@ struct Sums {
 
     // The tokens' share of the sums.  left: tokens that count for the lane's column;
     // most: for any column; even: for all columns alike, and tile the query token of
-    // the column where not.  tiles: query tokens of the entry.
+    // the column where not (Several).  tiles: query tokens of the entry.
+    template <bool Several>
     __device__ __forceinline__ void add(const char* slot, float scale, f32x4 (&acc)[2], int left, int most, bool even,
                                         int tile, int tiles, float sl2) {
         const int lane = threadIdx.x & (kWave - 1);
@@ -172,7 +173,7 @@ struct Sums {
                 v[0][i] = *reinterpret_cast<const uint32_t*>(rows + 4 * i * D);
             }
         }
-        if (most < kBlk || !even) {
+        if (most < kBlk || (Several && !even)) {
             __builtin_amdgcn_sched_barrier(0);  // a branch, not selects in every step
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -204,7 +205,7 @@ struct Sums {
         const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int a = NW - 1; a >= 0; --a) den = mma(__builtin_bit_cast(bf16x8, ones), part[a], den);
-        if (even) {
+        if (!Several || even) {
             values<false>(v, scale, part, true);
             return;
         }
@@ -299,14 +300,16 @@ __device__ __forceinline__ size_t row_at(const Entries& n, int l, int b, int j, 
 }
 
 // One workgroup per split of an entry and (layer, KV head); its waves take 32
-// tokens in turn.
-template <typename T, int D, int NH, int NWV>
-__global__ __launch_bounds__(NWV * kWave, 2) void blocks_split(const T* __restrict__ q, PagePool p, Entries n,
+// tokens in turn.  Several: entries of more than one query token.  The code is kept
+// short (a loop over the steps that is not unrolled over the slots, no masks by query
+// token where there is one): short calls wait for it as for their data.
+template <typename T, int D, int NH, bool Several>
+__global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict__ q, PagePool p, Entries n,
                                                                int share, int groups, int R, int whole, float sl2,
                                                                float* __restrict__ ws_o, float2* __restrict__ ws_ml,
                                                                SplitRange* __restrict__ ranges,
                                                                float* __restrict__ out) {
-    constexpr int NC = D / 16;
+    constexpr int NC = D / 16, NWV = kWaves;
     using S = Slot<D>;
     // the waves' rings, and behind their last use the waves' sums
     constexpr int kRing = S::kSlots * S::kBytes, kSums = NH * D * (int)sizeof(float);
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(NWV * kWave, 2) void blocks_split(const T* __restri
     const int places = chosen != nullptr ? n.k : p.M;
     const char* ring = s_ring + wv * kRing;
     int ids = 0, blks = 0, ids0 = -kWave;
-    int first[S::kSlots];  // position of a slot's first token, or seen_most: passed over
+    // loads 32 tokens into slot i; their first position, or seen_most: to be passed over
     auto issue = [&](int t, int i) -> int {
         const int at = t >> p.shift;
         if (at >= ids0 + kWave || ids0 < 0) {
@@ -386,36 +389,33 @@ __global__ __launch_bounds__(NWV * kWave, 2) void blocks_split(const T* __restri
         return ok ? (blk << p.shift) + tok : seen_most;
     };
     constexpr int kStride = NWV * kBlk;
-    int at0 = k0 + wv * kBlk;
+    static_assert(S::kSlots == 2, "a step's position and the next one's");
+    int at0 = k0 + wv * kBlk, pos = 0, next = 0;
     sums.settle_queries();
     settle(seen);
-#pragma unroll
-    for (int i = 0; i < S::kSlots; ++i)
-        if (at0 + i * kStride < k1) first[i] = issue(at0 + i * kStride, i);
-    while (at0 < k1) {
-#pragma unroll
-        for (int i = 0; i < S::kSlots; ++i) {
-            if (at0 >= k1) break;
-            // the slot's loads are the oldest: those of the slots behind it may be in flight
-            if (at0 + (S::kSlots - 1) * kStride < k1)
-                wait_vmcnt<(S::kSlots - 1) * S::kLoads>();
-            else
-                wait_vmcnt<0>();
-            asm volatile("" ::: "memory");
-            const int most = seen_most - first[i];
-            if (most > 0) {
-                const char* slot_at = ring + i * S::kBytes;
-                const uint32_t scales = *reinterpret_cast<const uint16_t*>(slot_at + 2 * S::kCodes);
-                f32x4 acc[2];
-                sums.logits(slot_at, scale_float(scale_of((uint8_t)scales)), acc);
-                sums.add(slot_at, scale_float(scale_of((uint8_t)(scales >> 8))), acc, seen - first[i], most,
-                         seen_least == seen_most || seen_least - first[i] >= kBlk, tile, here, sl2);
-            }
-            if (at0 + S::kSlots * kStride < k1) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
-                first[i] = issue(at0 + S::kSlots * kStride, i);
-            }
-            at0 += kStride;
+    if (at0 < k1) pos = issue(at0, 0);
+    if (at0 + kStride < k1) next = issue(at0 + kStride, 1);
+#pragma unroll 1
+    for (int i = 0; at0 < k1; at0 += kStride, i ^= 1) {
+        // the slot's loads are the oldest: those of the other slot may be in flight
+        if (at0 + kStride < k1)
+            wait_vmcnt<S::kLoads>();
+        else
+            wait_vmcnt<0>();
+        asm volatile("" ::: "memory");
+        const int most = seen_most - pos;
+        if (most > 0) {
+            const char* slot_at = ring + i * S::kBytes;
+            const uint32_t scales = *reinterpret_cast<const uint16_t*>(slot_at + 2 * S::kCodes);
+            f32x4 acc[2];
+            sums.logits(slot_at, scale_float(scale_of((uint8_t)scales)), acc);
+            sums.template add<Several>(slot_at, scale_float(scale_of((uint8_t)(scales >> 8))), acc, seen - pos, most,
+                                       seen_least == seen_most || seen_least - pos >= kBlk, tile, here, sl2);
+        }
+        pos = next;
+        if (at0 + 2 * kStride < k1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
+            next = issue(at0 + 2 * kStride, i);
         }
     }
     sums.finish();
@@ -481,13 +481,19 @@ __global__ __launch_bounds__(kThreads) void blocks_merge(int Hkv, Entries n, int
 template <typename T, int D, int NH>
 hipError_t run_columns(const void* q, const PagePool& p, const Entries& n, const BlocksPlan& plan, float scale,
                        float* out, void* ws, hipStream_t st) {
-    const int share = max(1, kDecodeUnits * kBlocksPerUnit / plan.pairs);  // one round of workgroups
+    const int share = max(1, kDecodeUnits / plan.pairs);  // a workgroup to each compute unit
     float* wo = static_cast<float*>(ws);
     float2* wml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.off_ml);
     SplitRange* ranges = reinterpret_cast<SplitRange*>(static_cast<char*>(ws) + plan.off_ranges);
-    hipLaunchKernelGGL((blocks_split<T, D, NH, kWaves>), dim3((unsigned)plan.pairs * plan.groups),
-                       dim3(kWaves * kWave), 0, st, static_cast<const T*>(q), p, n, share, plan.groups, plan.R,
-                       (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads), 0, st,
+                           static_cast<const T*>(q), p, n, share, plan.groups, plan.R, (int)plan.whole, scale * kLog2e,
+                           wo, wml, ranges, out);
+    };
+    if (plan.per > 1)
+        launch(blocks_split<T, D, NH, true>);
+    else
+        launch(blocks_split<T, D, NH, false>);
     const int rows = plan.pairs * plan.entries * plan.R;
     if (!plan.whole && share > 16)
         hipLaunchKernelGGL((blocks_merge<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, p.Hkv, n, plan.R,

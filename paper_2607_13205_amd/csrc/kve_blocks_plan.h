@@ -42,9 +42,6 @@ struct BlocksPlan {
     size_t off_ml, off_ranges, total;
 };
 
-// Workgroups that share a compute unit, by their LDS.
-constexpr int kBlocksPerUnit = 2;
-
 inline size_t decode_blocks_bytes(size_t parts, long long entries, int d, BlocksPlan* p) {
     p->off_ml = align_up(parts * d * sizeof(float));
     p->off_ranges = p->off_ml + align_up(parts * 2 * sizeof(float));
@@ -64,7 +61,7 @@ inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long 
     const long long quanta = (tokens + kDecodeQuantum - 1) / kDecodeQuantum;
     const long long segs = (long long)p.pairs * p.entries;
     p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > kPagesWhole ? segs / 8 : kPagesWhole);
-    const int share = p.pairs < kBlocksPerUnit * kDecodeUnits ? kBlocksPerUnit * kDecodeUnits / p.pairs : 1;
+    const int share = p.pairs < kDecodeUnits ? kDecodeUnits / p.pairs : 1;
     long long groups = (long long)share + p.entries;
     if (groups > p.entries * quanta) groups = p.entries * quanta;
     if (p.whole) groups = p.entries;
@@ -80,7 +77,7 @@ inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long 
 inline size_t decode_blocks_size(int L, int B, int Hq, int Hkv, int T, int d) {
     const long long pairs = (long long)L * Hkv, G = Hq / Hkv;
     const long long most = G * T < kPagesMaxGroup ? G * T : kPagesMaxGroup;
-    const long long round = pairs > kBlocksPerUnit * kDecodeUnits ? pairs : kBlocksPerUnit * kDecodeUnits;
+    const long long round = pairs > kDecodeUnits ? pairs : kDecodeUnits;
     BlocksPlan p{};
     return decode_blocks_bytes((size_t)(round * most + pairs * B * G * T * (T > 1 ? 2 : 1)), (long long)B * T, d, &p);
 }

@@ -5,6 +5,7 @@
 // block's score is <up, hi> + <down, lo>: two products of d channels whatever the
 // number of heads.  They are summed in 64 bits, so that the order of the sum does not
 // decide which of two blocks is chosen.
+#include <algorithm>
 #include <type_traits>
 
 #include "kve_blocks_device.h"
@@ -15,7 +16,9 @@ namespace kve {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kScored = 64;              // blocks per workgroup of top_scores
+constexpr int kScored = 64;              // blocks per workgroup of top_scores,
+constexpr int kTokens = 4;               // and query tokens that share its read of their bounds
+constexpr int kScoreGroups = 1024, kMostTiles = 8;  // workgroups from which each takes more blocks, up to eight times as many
 
 template <int N>
 using Int = std::integral_constant<int, N>;
@@ -84,66 +87,123 @@ __device__ __forceinline__ double add4(const double (&up)[8], const double (&dow
     return fma(up[4 * W + 3], tiny<3>(hi), fma(down[4 * W + 3], tiny<3>(lo), sum));
 }
 
-// Keys of kScored blocks of a segment.  D / 8 lanes to a block, eight channels of
-// both bounds each, and all of a lane's blocks looked up and loaded together.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, PagePool p, TopGrid g, int chunks,
-                                                       uint32_t* __restrict__ keys) {
-    constexpr int kRow = D / 8, kStep = kThreads / kRow, kItems = kScored / kStep;
-    __shared__ __attribute__((aligned(16))) double s_up[2][D];
-    const unsigned seg = blockIdx.x / (unsigned)chunks;
-    const int chunk = (int)(blockIdx.x - seg * chunks);
-    const Segment x = segment_of(p, g, seg);
-    if (x.blocks <= g.k || chunk * kScored >= x.blocks) return;  // all are taken, or none here
-    const int part = threadIdx.x % kRow, in = threadIdx.x / kRow;
-    int page[kItems];
+// What a lane holds of kItems blocks: eight channels of both bounds.
+template <int D>
+struct Bounds {
+    static constexpr int kRow = D / 8, kStep = kThreads / kRow, kItems = kScored / kStep;
+    u32x2 lo[kItems], hi[kItems];
+    uint8_t unit[kItems];
+    __device__ __forceinline__ static void pages(const PagePool& p, const Segment& x, int first, int (&page)[kItems]) {
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int at = chunk * kScored + i * kStep + in;
-        page[i] = at < x.blocks ? p.table[(size_t)x.slot * p.M + at] : -1;
+        for (int i = 0; i < kItems; ++i) {
+            const int at = first + i * kStep + (int)threadIdx.x / kRow;
+            page[i] = at < x.blocks ? p.table[(size_t)x.slot * p.M + at] : -1;
+        }
     }
+    __device__ __forceinline__ void load(const PagePool& p, const Segment& x, const int (&page)[kItems]) {
+        const int part = threadIdx.x % kRow;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            // a block without a page: any page's bounds, and not their score
+            const int pg = page[i] >= 0 && page[i] < p.n_pages ? page[i] : 0;
+            const char* tail = block_at<D>(p, x.l, pg, x.j) + tail_at<D>(p.shift);
+            lo[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales)[part];
+            hi[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales + D)[part];
+            unit[i] = (uint8_t)tail[0];
+        }
+    }
+    // the keys of a query token
+    __device__ __forceinline__ void score(const PagePool& p, const Segment& x, int first, const int (&page)[kItems],
+                                          const double (&up)[8], const double (&down)[8], uint32_t* keys) const {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            double sum = add4<1>(up, down, lo[i][1], hi[i][1], add4<0>(up, down, lo[i][0], hi[i][0], 0.0));
+            if ((nan_codes(lo[i][0]) | nan_codes(lo[i][1]) | nan_codes(hi[i][0]) | nan_codes(hi[i][1])) != 0)
+                sum = __builtin_nan("");
+            sum = row_sum<kRow>(sum);
+            const int at = first + i * kStep + (int)threadIdx.x / kRow;
+            if (threadIdx.x % kRow == 0 && at < x.blocks) {
+                const bool ok = page[i] >= 0 && page[i] < p.n_pages;
+                const double score = sum * kDown * (double)scale_float(scale_of(unit[i]));
+                keys[at] = ok ? score_key((float)score) : 0u;
+            }
+        }
+    }
+};
+
+// Keys of `tiles` times kScored blocks of a (layer, sample, KV head) for up to TOKENS
+// query tokens.  The next tile's bounds, and the page numbers of the one after it, are
+// on their way while a tile is scored.
+template <typename T, int D, int TOKENS>
+__global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, PagePool p, TopGrid g, int chunks,
+                                                       int tiles, int groups, uint32_t* __restrict__ keys) {
+    using B = Bounds<D>;
+    // channels 2 e, 2 e + 1 of every eight, side by side
+    __shared__ __attribute__((aligned(16))) double s_up[TOKENS][2][4][B::kRow][2];
+    const unsigned y = blockIdx.x / (unsigned)chunks, lbj = y / (unsigned)groups;
+    const int first = (int)(blockIdx.x - y * chunks) * tiles * kScored, t0 = (int)(y - lbj * groups) * TOKENS;
+    const int tokens = min(TOKENS, g.view.T - t0);
+    const Segment x = segment_of(p, g, lbj * (unsigned)g.view.T + (t0 + tokens - 1));  // the token that sees most
+    if (x.blocks <= g.k || first >= x.blocks) return;  // all are taken, or none here
+    const int end = min(x.blocks, first + tiles * kScored);
+    int now[B::kItems], next[B::kItems], then[B::kItems];
+    B::pages(p, x, first, now);
+    B::pages(p, x, first + kScored, next);
     // the heads' sums: a thread to each channel of either
     if (threadIdx.x < 2 * D) {
         const int c = threadIdx.x % D;
         const bool lower = threadIdx.x >= D;
-        const T* row = q + ((((size_t)x.l * g.view.B + x.b) * g.Hq + (size_t)x.j * g.G) * g.view.T + x.t) * D + c;
-        double sum = 0.0;
-#pragma unroll 4
-        for (int h = 0; h < g.G; ++h) {
-            const float y = (float)row[(size_t)h * g.view.T * D];
-            sum += (lower ? y > 0.0f : y < 0.0f) ? 0.0 : (double)y;
+        const T* row = q + ((((size_t)x.l * g.view.B + x.b) * g.Hq + (size_t)x.j * g.G) * g.view.T + t0) * D + c;
+#pragma unroll 1
+        for (int t = 0; t < tokens; ++t, row += D) {
+            double sum = 0.0;
+#pragma unroll 8
+            for (int h = 0; h < g.G; ++h) {
+                const float z = (float)row[(size_t)h * g.view.T * D];
+                sum += (lower ? z > 0.0f : z < 0.0f) ? 0.0 : (double)z;
+            }
+            s_up[t][lower][c % 8 / 2][c / 8][c % 2] = sum * kUp;
         }
-        s_up[lower][c] = sum * kUp;
     }
-    u32x2 lo[kItems], hi[kItems];
-    uint8_t unit[kItems];
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        // a block without a page: any page's bounds, and not their score
-        const int pg = page[i] >= 0 && page[i] < p.n_pages ? page[i] : 0;
-        const char* tail = block_at<D>(p, x.l, pg, x.j) + tail_at<D>(p.shift);
-        lo[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales)[part];
-        hi[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales + D)[part];
-        unit[i] = (uint8_t)tail[0];
-    }
+    B mine;
+    mine.load(p, x, now);
     __syncthreads();
+    const int part = threadIdx.x % B::kRow;
     double up[8], down[8];
+    auto token = [&](int t) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        up[e] = s_up[0][8 * part + e];
-        down[e] = s_up[1][8 * part + e];
-    }
+        for (int e = 0; e < 8; ++e) {
+            up[e] = s_up[t][0][e / 2][part][e % 2];
+            down[e] = s_up[t][1][e / 2][part][e % 2];
+        }
+    };
+    if constexpr (TOKENS == 1) token(0);
+#pragma unroll 1
+    for (int at = first; at < end; at += kScored) {
+        B ahead;
+        ahead.load(p, x, next);
+        B::pages(p, x, at + 2 * kScored, then);
+        if constexpr (TOKENS == 1) {
+            mine.score(p, x, at, now, up, down, keys + (size_t)(lbj * (unsigned)g.view.T + t0) * g.pitch);
+        } else {
+#pragma unroll 1
+            for (int t = 0; t < tokens; ++t) {
+                token(t);
+                // the codes as doubles are made again for each token: held, they would leave two
+                // waves to a compute unit's quarter
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        double sum = add4<1>(up, down, lo[i][1], hi[i][1], add4<0>(up, down, lo[i][0], hi[i][0], 0.0));
-        if ((nan_codes(lo[i][0]) | nan_codes(lo[i][1]) | nan_codes(hi[i][0]) | nan_codes(hi[i][1])) != 0)
-            sum = __builtin_nan("");
-        sum = row_sum<kRow>(sum);
-        const int at = chunk * kScored + i * kStep + in;
-        if (part == 0 && at < x.blocks) {
-            const bool ok = page[i] >= 0 && page[i] < p.n_pages;
-            const double score = sum * kDown * (double)scale_float(scale_of(unit[i]));
-            keys[(size_t)seg * g.pitch + at] = ok ? score_key((float)score) : 0u;
+                for (int i = 0; i < B::kItems; ++i) {
+                    asm volatile("" : "+v"(mine.lo[i]));
+                    asm volatile("" : "+v"(mine.hi[i]));
+                }
+                mine.score(p, x, at, now, up, down, keys + (size_t)(lbj * (unsigned)g.view.T + t0 + t) * g.pitch);
+            }
+        }
+        mine = ahead;
+#pragma unroll
+        for (int i = 0; i < B::kItems; ++i) {
+            now[i] = next[i];
+            next[i] = then[i];
         }
     }
 }
@@ -303,20 +363,26 @@ hipError_t launch_blocks_top(const void* q, int dtype, const PagePool& p, int d,
     const unsigned segs = (unsigned)p.L * view.B * p.Hkv * view.T;
     uint32_t* keys = static_cast<uint32_t*>(ws);
     if (most > k) {
-        const int chunks = (most + kScored - 1) / kScored;
-        const dim3 grid(segs * (unsigned)chunks), block(kThreads);
-        if (dtype == 0 && d == 128)
-            hipLaunchKernelGGL((top_scores<__bf16, 128>), grid, block, 0, st, static_cast<const __bf16*>(q), p, g,
-                               chunks, keys);
-        if (dtype == 0 && d == 64)
-            hipLaunchKernelGGL((top_scores<__bf16, 64>), grid, block, 0, st, static_cast<const __bf16*>(q), p, g,
-                               chunks, keys);
-        if (dtype == 1 && d == 128)
-            hipLaunchKernelGGL((top_scores<float, 128>), grid, block, 0, st, static_cast<const float*>(q), p, g,
-                               chunks, keys);
-        if (dtype == 1 && d == 64)
-            hipLaunchKernelGGL((top_scores<float, 64>), grid, block, 0, st, static_cast<const float*>(q), p, g,
-                               chunks, keys);
+        const int tokens = view.T == 1 ? 1 : kTokens, groups = (view.T + tokens - 1) / tokens;
+        const int all = (most + kScored - 1) / kScored;
+        const long long pairs = (long long)p.L * view.B * p.Hkv * groups;
+        const int tiles = (int)std::min(std::max(pairs * all / kScoreGroups, 1LL), (long long)kMostTiles);
+        const int chunks = (all + tiles - 1) / tiles;
+        auto launch = [&](auto kernel, auto rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * chunks)), dim3(kThreads), 0, st, rows, p, g, chunks, tiles,
+                               groups, keys);
+        };
+        auto by_size = [&](auto rows) {
+            using T = std::remove_const_t<std::remove_pointer_t<decltype(rows)>>;
+            if (tokens == 1)
+                launch(d == 128 ? top_scores<T, 128, 1> : top_scores<T, 64, 1>, rows);
+            else
+                launch(d == 128 ? top_scores<T, 128, kTokens> : top_scores<T, 64, kTokens>, rows);
+        };
+        if (dtype == 0)
+            by_size(static_cast<const __bf16*>(q));
+        else
+            by_size(static_cast<const float*>(q));
     }
     hipLaunchKernelGGL(top_select, dim3(segs), dim3(kSelect), 0, st, p, g, keys, top);
     return hipGetLastError();

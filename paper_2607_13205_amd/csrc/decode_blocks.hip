@@ -305,7 +305,7 @@ __device__ __forceinline__ size_t row_at(const Entries& n, int l, int b, int j, 
 // token where there is one): short calls wait for it as for their data.
 template <typename T, int D, int NH, bool Several>
 __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict__ q, PagePool p, Entries n,
-                                                               int share, int groups, int R, int whole, float sl2,
+                                                               int share, int level, int groups, int R, int whole, float sl2,
                                                                float* __restrict__ ws_o, float2* __restrict__ ws_ml,
                                                                SplitRange* __restrict__ ranges,
                                                                float* __restrict__ out) {
@@ -340,7 +340,8 @@ __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict_
             __syncthreads();
         }
         // the first workgroup's first wave leaves the ranges for the merge
-        work = find_work(of, n.count, share, x, staged, blockIdx.x == 0 && wv == 0 ? ranges : nullptr);
+        work = find_work(of, n.count, share, x, staged, blockIdx.x == 0 && wv == 0 ? ranges : nullptr,
+                         level);
         if (staged != nullptr) __syncthreads();  // the rings take the lengths' place
         if (work.b < 0) return;
     }
@@ -481,13 +482,12 @@ __global__ __launch_bounds__(kThreads) void blocks_merge(int Hkv, Entries n, int
 template <typename T, int D, int NH>
 hipError_t run_columns(const void* q, const PagePool& p, const Entries& n, const BlocksPlan& plan, float scale,
                        float* out, void* ws, hipStream_t st) {
-    const int share = max(1, kDecodeUnits / plan.pairs);  // a workgroup to each compute unit
     float* wo = static_cast<float*>(ws);
     float2* wml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.off_ml);
     SplitRange* ranges = reinterpret_cast<SplitRange*>(static_cast<char*>(ws) + plan.off_ranges);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads), 0, st,
-                           static_cast<const T*>(q), p, n, share, plan.groups, plan.R, (int)plan.whole, scale * kLog2e,
+                           static_cast<const T*>(q), p, n, plan.share, plan.level, plan.groups, plan.R, (int)plan.whole, scale * kLog2e,
                            wo, wml, ranges, out);
     };
     if (plan.per > 1)
@@ -495,7 +495,7 @@ hipError_t run_columns(const void* q, const PagePool& p, const Entries& n, const
     else
         launch(blocks_split<T, D, NH, false>);
     const int rows = plan.pairs * plan.entries * plan.R;
-    if (!plan.whole && share > 16)
+    if (!plan.whole && plan.level > 16)
         hipLaunchKernelGGL((blocks_merge<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, p.Hkv, n, plan.R,
                            plan.groups, wo, wml, ranges, rows, out);
     else if (!plan.whole)

@@ -32,11 +32,21 @@ struct BlockView {
     int B, T, max_tokens;
 };
 
+// Workgroups per compute unit that a decode is cut for.  One reads as fast as two that
+// a unit holds, and leaves the fewest partial results (8 sequences of 32768 tokens, 8 KV
+// heads: 102.6 us with one, 103.6, 109 and 104 with two, three and four; 16 tokens' pairs
+// of 100 blocks of 32 41, 46 and 53).  Sequences whose lengths differ leave units without
+// work at the end, the fewer the shorter the splits are (64 of up to 32768: 251 us with
+// one, 231, 216 and 211; 8 57, 54, 53 and 52; but 4 33, 33, 36 and 35, 2 20, 21, 25 and
+// 27): from kBlocksSeveral entries on those are cut for four.
+constexpr int kBlocksLevel = 1, kBlocksRagged = 4, kBlocksSeveral = 8;
+
 // Plan of a decode over blocks.  Query tokens of a sample are taken `per` at a time,
 // an entry each: as many as the sixteen columns of a product hold heads for, or one
 // where each has its own blocks.  The entries' tokens are cut as PagesPlan's.
 struct BlocksPlan {
     int pairs, G, per, tiles, entries, R;  // R: query rows of an entry, per * G
+    int share, level;                      // splits of all entries together, and where their lengths are level
     int groups;                            // workgroups per (layer, KV head)
     bool whole;                            // one split per entry: nothing to merge
     size_t off_ml, off_ranges, total;
@@ -61,8 +71,11 @@ inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long 
     const long long quanta = (tokens + kDecodeQuantum - 1) / kDecodeQuantum;
     const long long segs = (long long)p.pairs * p.entries;
     p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > kPagesWhole ? segs / 8 : kPagesWhole);
-    const int share = p.pairs < kDecodeUnits ? kDecodeUnits / p.pairs : 1;
-    long long groups = (long long)share + p.entries;
+    auto splits = [&](int per_unit) { return p.pairs < per_unit * kDecodeUnits ? per_unit * kDecodeUnits / p.pairs : 1; };
+    p.level = splits(kBlocksLevel);
+    // chosen blocks are equally many
+    p.share = sparse || p.entries < kBlocksSeveral ? p.level : splits(kBlocksRagged);
+    long long groups = (long long)p.share + p.entries;
     if (groups > p.entries * quanta) groups = p.entries * quanta;
     if (p.whole) groups = p.entries;
     p.groups = (int)groups;
@@ -77,7 +90,7 @@ inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long 
 inline size_t decode_blocks_size(int L, int B, int Hq, int Hkv, int T, int d) {
     const long long pairs = (long long)L * Hkv, G = Hq / Hkv;
     const long long most = G * T < kPagesMaxGroup ? G * T : kPagesMaxGroup;
-    const long long round = pairs > kDecodeUnits ? pairs : kDecodeUnits;
+    const long long round = pairs > kBlocksRagged * kDecodeUnits ? pairs : kBlocksRagged * kDecodeUnits;
     BlocksPlan p{};
     return decode_blocks_bytes((size_t)(round * most + pairs * B * G * T * (T > 1 ? 2 : 1)), (long long)B * T, d, &p);
 }

@@ -138,8 +138,11 @@ struct Work {
 // itself, 64 sequences at a time.  of(b): sequence b, none from B on.  staged: the
 // lengths of all sequences (null: they are loaded; up to 64 once, and more several
 // times).  ranges: where not null, every sequence's range is written there.
+// level: where not 0, the share for sequences of which none is much longer than the
+// mean.
 template <typename Of>
-__device__ __forceinline__ Work find_work(Of of, int B, int share, int x, const int* staged, SplitRange* ranges) {
+__device__ __forceinline__ Work find_work(Of of, int B, int share, int x, const int* staged, SplitRange* ranges,
+                                          int level = 0) {
     const int lane = threadIdx.x & (kWave - 1);
     Sequence mine{-1, 0};
     if (staged == nullptr) mine = of(lane);
@@ -149,7 +152,13 @@ __device__ __forceinline__ Work find_work(Of of, int B, int share, int x, const 
     };
     // sums over the lanes' shares: up to 2^23 quanta each, any number of sequences
     long long total = 0;
-    for (int b0 = 0; b0 < B; b0 += kWave) total += wave_sum(quanta_of(tokens_at(b0)));
+    int longest = 0;
+    for (int b0 = 0; b0 < B; b0 += kWave) {
+        const int quanta = quanta_of(tokens_at(b0));
+        total += wave_sum(quanta);
+        if (level != 0) longest = max(longest, quanta);
+    }
+    if (level != 0 && __builtin_amdgcn_ballot_w64((long long)longest * B > total + total / 8) == 0) share = level;
     // no sequence has more than kMostQuanta
     int per = total < kMostQuanta ? max(1, splits_of((int)total, share))
                                   : (int)min((total + share - 1) / share, (long long)kMostQuanta);

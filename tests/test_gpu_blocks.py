@@ -177,9 +177,56 @@ def test_rows_written_piece_by_piece(K, dtype, d, page):
             m.same(b, at[b])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(64, 32), (128, 64), (64, 128), (128, 128)])
+def test_single_rows_hold_the_nearest(K, dtype, d, page):
+    """A decode step's one row of many sequences: every border of the format, behind any number of rows."""
+    x = hard_rows(dtype, d, page)[::max(1, page // 16)]
+    B, r = len(x), np.random.default_rng(page)
+    cache = make(K, 1, 2, d, page, 3 * B, B, 3)
+    have = r.integers(0, 2 * page, B)
+    have[:4] = 0, page, page - 1, 1
+    start, _ = K.pages_extend(cache, dev(have))
+    old = (normal((1, B, 2, 2 * page, d), dtype, 3) * 2.0 ** torch.from_numpy(r.integers(-20, 20, (1, B, 2, 1, 1)))).to(TORCH[dtype])
+    old = old.cuda()
+    K.blocks_append(old, old.flip(2), cache, start, n_new=dev(have))
+    start, _ = K.pages_extend(cache, dev([1] * B))
+    k = torch.stack([x, x.flip(0)], 1)[None, :, :, None].cuda()
+    K.blocks_append(k, k.flip(2), cache, start)
+    m = Model(cache)
+    for b in range(B):
+        n = int(have[b])
+        with np.errstate(over="ignore"):
+            m.write(b, 0, host(old)[:, b, :, :n], host(old.flip(2))[:, b, :, :n])
+            m.write(b, n, host(k)[:, b], host(k.flip(2))[:, b])
+        m.same(b, n + 1)
+
+
+def test_append_of_many_samples(K):
+    """More rows than a workgroup takes, an odd number of heads, samples without a row among them."""
+    L, B, Hkv, d, page = 2, 37, 3, 64, 32
+    cache = make(K, L, Hkv, d, page, B * 2, B, 2)
+    m, at = Model(cache), np.zeros(B, dtype=np.int64)
+    r = np.random.default_rng(0)
+    for step in range(5):
+        new = r.integers(0, 2, B)
+        start, _ = K.pages_extend(cache, dev(new))
+        k, v = normal((L, B, Hkv, 1, d), "bf16", step, 2.0 ** step).cuda(), normal((L, B, Hkv, 1, d), "bf16", 50 + step).cuda()
+        K.blocks_append(k, v, cache, start, n_new=dev(new))
+        for b in range(B):
+            if new[b]:
+                m.write(b, int(at[b]), host(k)[:, b], host(v)[:, b])
+        at += new
+    for b in range(B):
+        m.same(b, int(at[b]))
+
+
 @pytest.mark.parametrize("dtype,d,r,pairs,T,Hq,Hkv,P", [
     ("bf16", 128, 128, False, 1, 8, 2, 5000),
     ("bf16", 128, 128, True, 1, 3, 3, 17),
+    ("f32", 64, 48, False, 1, 3, 1, 60000),
+    ("f32", 128, 32, True, 1, 4, 2, 900),
+    ("bf16", 64, 16, False, 1, 9, 2, 900),
     ("bf16", 128, 48, False, 70, 4, 1, 1000),
     ("f32", 64, 16, True, 33, 2, 2, 300),
     ("f32", 64, 64, False, 5, 5, 1, 40),
@@ -641,6 +688,20 @@ def test_top(K, Hkv, G, d, page, lengths, T, k, first, last, most, dtype):
     q = normal((L, B, Hq, T, d), dtype, 31).cuda()
     top = K.blocks_top(q, cache, k, first=first, last=last, max_tokens=most, seq=dev(order))
     same_top(top, want_top(cache, host(q), lengths, order, k, first, last, most))
+
+
+@pytest.mark.parametrize("T,Hkv,page,M", [(1, 8, 32, 2600), (6, 4, 64, 1500)])
+def test_top_of_many_long_sequences(K, T, Hkv, page, M):
+    """Enough blocks that a workgroup scores several tiles of them; sequences that share pages, of different lengths."""
+    L, B, G, d, n_pages, k = 2, 8, 2, 64, 400, 33
+    r = np.random.default_rng(M)
+    cache, _, _ = filled(K, L, Hkv, d, page, [page * n_pages])
+    lengths = [M * page] + [int(r.integers(1, M * page)) for _ in range(B - 1)]
+    table = dev(r.integers(0, n_pages, (B, M)))
+    shared = K.Blocks(cache.pool, cache.refs, table, dev([M] * B), dev(lengths), page, d)
+    q = normal((L, B, Hkv * G, T, d), "bf16", 6).cuda()
+    top = K.blocks_top(q, shared, k)
+    same_top(top, want_top(shared, host(q), lengths, range(B), k, 1, 1))
 
 
 def test_top_ties_nan_and_missing_pages(K):

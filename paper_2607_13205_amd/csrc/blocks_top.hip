@@ -55,13 +55,12 @@ __device__ __forceinline__ double row_move(double x) {
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-// Sum over the LANES lanes (8 or 16) of a block, in every lane.
+// Sum over the LANES lanes (4 or 8) of a block, in every lane.
 template <int LANES>
 __device__ __forceinline__ double row_sum(double x) {
-    x += row_move<0xb1>(x);   // lanes 1 0 3 2
-    x += row_move<0x4e>(x);   // lanes 2 3 0 1
-    x += row_move<0x141>(x);  // mirrored within eight
-    if constexpr (LANES == 16) x += row_move<0x140>(x);  // within sixteen
+    x += row_move<0xb1>(x);  // lanes 1 0 3 2
+    x += row_move<0x4e>(x);  // lanes 2 3 0 1
+    if constexpr (LANES == 8) x += row_move<0x141>(x);  // mirrored within eight
     return x;
 }
 
@@ -79,7 +78,7 @@ constexpr double kUp = 0x1p800, kDown = 0x1p216;  // what brings products of suc
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
 template <int W>
-__device__ __forceinline__ double add4(const double (&up)[8], const double (&down)[8], uint32_t lo, uint32_t hi,
+__device__ __forceinline__ double add4(const double (&up)[16], const double (&down)[16], uint32_t lo, uint32_t hi,
                                        double sum) {
     sum = fma(up[4 * W], tiny<0>(hi), fma(down[4 * W], tiny<0>(lo), sum));
     sum = fma(up[4 * W + 1], tiny<1>(hi), fma(down[4 * W + 1], tiny<1>(lo), sum));
@@ -87,11 +86,11 @@ __device__ __forceinline__ double add4(const double (&up)[8], const double (&dow
     return fma(up[4 * W + 3], tiny<3>(hi), fma(down[4 * W + 3], tiny<3>(lo), sum));
 }
 
-// What a lane holds of kItems blocks: eight channels of both bounds.
+// What a lane holds of kItems blocks: sixteen channels of both bounds.
 template <int D>
 struct Bounds {
-    static constexpr int kRow = D / 8, kStep = kThreads / kRow, kItems = kScored / kStep;
-    u32x2 lo[kItems], hi[kItems];
+    static constexpr int kRow = D / 16, kStep = kThreads / kRow, kItems = kScored / kStep;
+    u32x4 lo[kItems], hi[kItems];
     uint8_t unit[kItems];
     __device__ __forceinline__ static void pages(const PagePool& p, const Segment& x, int first, int (&page)[kItems]) {
 #pragma unroll
@@ -107,19 +106,23 @@ struct Bounds {
             // a block without a page: any page's bounds, and not their score
             const int pg = page[i] >= 0 && page[i] < p.n_pages ? page[i] : 0;
             const char* tail = block_at<D>(p, x.l, pg, x.j) + tail_at<D>(p.shift);
-            lo[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales)[part];
-            hi[i] = reinterpret_cast<const u32x2*>(tail + kBlockScales + D)[part];
+            lo[i] = ld16(tail + kBlockScales + 16 * part);
+            hi[i] = ld16(tail + kBlockScales + D + 16 * part);
             unit[i] = (uint8_t)tail[0];
         }
     }
     // the keys of a query token
     __device__ __forceinline__ void score(const PagePool& p, const Segment& x, int first, const int (&page)[kItems],
-                                          const double (&up)[8], const double (&down)[8], uint32_t* keys) const {
+                                          const double (&up)[16], const double (&down)[16], uint32_t* keys) const {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            double sum = add4<1>(up, down, lo[i][1], hi[i][1], add4<0>(up, down, lo[i][0], hi[i][0], 0.0));
-            if ((nan_codes(lo[i][0]) | nan_codes(lo[i][1]) | nan_codes(hi[i][0]) | nan_codes(hi[i][1])) != 0)
-                sum = __builtin_nan("");
+            // two chains, which hide each other's latency
+            double sum = add4<1>(up, down, lo[i][1], hi[i][1], add4<0>(up, down, lo[i][0], hi[i][0], 0.0)) +
+                         add4<3>(up, down, lo[i][3], hi[i][3], add4<2>(up, down, lo[i][2], hi[i][2], 0.0));
+            uint32_t bad = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) bad |= nan_codes(lo[i][w]) | nan_codes(hi[i][w]);
+            if (bad != 0) sum = __builtin_nan("");
             sum = row_sum<kRow>(sum);
             const int at = first + i * kStep + (int)threadIdx.x / kRow;
             if (threadIdx.x % kRow == 0 && at < x.blocks) {
@@ -138,8 +141,8 @@ template <typename T, int D, int TOKENS>
 __global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, PagePool p, TopGrid g, int chunks,
                                                        int tiles, int groups, uint32_t* __restrict__ keys) {
     using B = Bounds<D>;
-    // channels 2 e, 2 e + 1 of every eight, side by side
-    __shared__ __attribute__((aligned(16))) double s_up[TOKENS][2][4][B::kRow][2];
+    // channels 2 e, 2 e + 1 of every sixteen, side by side
+    __shared__ __attribute__((aligned(16))) double s_up[TOKENS][2][8][B::kRow][2];
     const unsigned y = blockIdx.x / (unsigned)chunks, lbj = y / (unsigned)groups;
     const int first = (int)(blockIdx.x - y * chunks) * tiles * kScored, t0 = (int)(y - lbj * groups) * TOKENS;
     const int tokens = min(TOKENS, g.view.T - t0);
@@ -162,17 +165,17 @@ __global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, 
                 const float z = (float)row[(size_t)h * g.view.T * D];
                 sum += (lower ? z > 0.0f : z < 0.0f) ? 0.0 : (double)z;
             }
-            s_up[t][lower][c % 8 / 2][c / 8][c % 2] = sum * kUp;
+            s_up[t][lower][c % 16 / 2][c / 16][c % 2] = sum * kUp;
         }
     }
     B mine;
     mine.load(p, x, now);
     __syncthreads();
     const int part = threadIdx.x % B::kRow;
-    double up[8], down[8];
+    double up[16], down[16];
     auto token = [&](int t) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 16; ++e) {
             up[e] = s_up[t][0][e / 2][part][e % 2];
             down[e] = s_up[t][1][e / 2][part][e % 2];
         }

@@ -12,6 +12,7 @@ module) can be imported before the library is built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -160,7 +161,9 @@ class _Lib:
     def __getattr__(self, name):
         if _Lib._cdll is None:
             _Lib._cdll = _load()
-        return getattr(_Lib._cdll, name)
+        fn = getattr(_Lib._cdll, name)
+        setattr(self, name, fn)      # found as an attribute the next time
+        return fn
 
 
 LIB = _Lib()
@@ -184,6 +187,7 @@ def _check(status: int):
 # torch plumbing
 # ---------------------------------------------------------------------------
 
+@functools.lru_cache(maxsize=None)
 def _torch():
     import torch
     return torch

@@ -246,6 +246,7 @@ def _queries(q, blocks, max_tokens):
     return shape[0], shape[1], shape[2], T, blocks.c.M * blocks.page if max_tokens is None else int(max_tokens)
 
 
+@functools.lru_cache(maxsize=1024)
 def blocks_top_workspace_size(L, B, Hkv, T, max_tokens, page) -> int:
     return int(LIB.kve_blocks_top_workspace_size(L, B, Hkv, T, max_tokens, page))
 
@@ -272,6 +273,7 @@ def blocks_top(q, blocks: Blocks, k: int, first: int = 1, last: int = 1, max_tok
     return out
 
 
+@functools.lru_cache(maxsize=1024)
 def decode_blocks_workspace_size(L, B, Hq, Hkv, T, d) -> int:
     return int(LIB.kve_decode_blocks_workspace_size(L, B, Hq, Hkv, T, d))
 

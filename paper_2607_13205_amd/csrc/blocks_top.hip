@@ -18,7 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kScored = 64;              // blocks per workgroup of top_scores,
 constexpr int kTokens = 4;               // and query tokens that share its read of their bounds
-constexpr int kScoreGroups = 1024, kMostTiles = 8;  // workgroups from which each takes more blocks, up to eight times as many
+constexpr int kScoreGroups = 2048, kMostTiles = 8;  // workgroups from which each takes more blocks, up to eight times as many
 
 template <int N>
 using Int = std::integral_constant<int, N>;

@@ -101,7 +101,7 @@ def _four_bit(pages):
 def _on(pages: Pages, stream):
     """The stream to launch on; the cache's device must be the current one."""
     torch = kb._torch()
-    if pages.index != torch.cuda.current_device():
+    if pages.index != torch._C._cuda_getDevice():
         raise ValueError(f"the cache is on {pages.pool.device}, the current device is {torch.cuda.current_device()}")
     return torch._C._cuda_getCurrentRawStream(pages.index) if stream is None else stream.cuda_stream
 

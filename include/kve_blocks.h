@@ -33,8 +33,9 @@
  * as a NaN.  Where the scale rises, the rows and bounds that the block held are
  * rounded once more in the same way: multiplying by a power of two changes only
  * those that become smaller than 2^-6 of the new scale.  The bounds are those of
- * the codes; a channel with a NaN has NaN bounds.  Every value is exact in
- * bfloat16 and float32.
+ * the codes that calls have left in the block since a row was written at its first
+ * position; a channel with a NaN has NaN bounds.  Every value is exact in bfloat16
+ * and float32.
  *
  * The cache is a kve_pages_t whose pool is [L, n_pages, Hkv, block bytes] and
  * whose page is 32, 64 or 128.  The bookkeeping is that of kve_pages.h, and
@@ -84,7 +85,8 @@ typedef struct kve_rotation {
  * start[b] + i of the sequence in slot seq[b], the keys rotated.  Rows whose
  * position has no page are dropped, as are all rows of a sequence whose start is
  * negative (a refused kve_pages_extend).  A block that holds positions below
- * start[b] keeps them (see above); what it held at start[b] and beyond is gone.
+ * start[b] keeps them (see above); what it held at start[b] and beyond is gone, but
+ * its scale and bounds may stay as wide as that made them.
  * With q, also writes the queries, rotated in the same way and rounded to their
  * type, to q_out: all of them, whatever start and n_new are.
  *

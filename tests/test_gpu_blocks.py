@@ -932,3 +932,138 @@ def test_blocks_beyond_four_gigabytes(K, d, page):
     top = K.blocks_top(q, cache, 2)
     same_top(top, want_top(cache, host(q), lengths, [0, 1], 2, 1, 1))
     check_decode(cache, kk, vv, host(q), host(K.decode_blocks(q, cache, top=top)), lengths, [0, 1], top=top.cpu().numpy())
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_drawn_calls(K, seed):
+    """Shapes, lengths, starts, bounds and lists drawn over the contract: append in pieces, choice, attention over all
+    and over the chosen blocks."""
+    r = np.random.default_rng(100 + seed)
+    d, page = int(r.choice([64, 128])), int(r.choice([32, 64, 128]))
+    Hkv, G = int(r.choice([1, 2, 3, 5])), int(r.choice([1, 2, 3, 4, 7, 8, 13, 16]))
+    L, B, T = int(r.choice([1, 2])), int(r.integers(1, 6)), int(r.choice([1, 1, 2, 3, 5, 9, 17]))
+    dtype = str(r.choice(["bf16", "f32"]))
+    S, longest = B + int(r.integers(0, 3)), int(r.choice([1, 40, 200, 900]))
+    M = -(-longest // page) + int(r.integers(0, 2))
+    cache = make(K, L, Hkv, d, page, S * M + 1, S, M, seed)
+    slots = r.permutation(S)[:B]
+    seq, m, at = dev(slots), Model(cache), np.zeros(B, dtype=np.int64)
+    want = r.integers(0, longest + 1, B)
+    want[0] = longest
+    while (at < want).any():
+        T_new = int(r.choice([1, 3, 70, 300]))
+        new = np.minimum(r.integers(0, T_new + 1, B), want - at)
+        start, missing = K.pages_extend(cache, dev(new), seq=seq)
+        assert missing.item() == 0
+        k, v = (normal((L, B, T_new, Hkv, d), dtype, int(r.integers(1 << 30)), float(2.0 ** r.integers(-3, 4))).cuda()
+                .permute(0, 1, 3, 2, 4) for _ in (0, 1))
+        K.blocks_append(k, v, cache, start, n_new=dev(new), seq=seq)
+        for b in range(B):
+            m.write(int(slots[b]), int(at[b]), host(k)[:, b, :, :new[b]], host(v)[:, b, :, :new[b]])
+        at += new
+    for b in range(B):
+        m.same(int(slots[b]), int(at[b]))
+    lengths = [0] * S
+    for b in range(B):
+        lengths[slots[b]] = int(at[b])
+    kk, vv = (host(x) for x in K.blocks_read(cache, longest, dtype=torch.float32))
+    order = np.concatenate([slots, r.integers(-1, S + 1, 2)])
+    n = len(order)
+    start = None if r.random() < 0.5 else r.integers(-2, longest + 3, n)
+    most = None if r.random() < 0.5 else int(r.integers(1, M * page + 1))
+    q = normal((L, n, Hkv * G, T, d), dtype, seed, float(r.choice([0.1, 1.0, 4.0]))).cuda()
+    kw = dict(max_tokens=most, seq=dev(order), start=None if start is None else dev(start))
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    K.decode_blocks(q, cache, out=out, **kw)
+    check_decode(cache, kk, vv, host(q), host(out), lengths, order, most=most, start=start)
+    first, last = int(r.integers(0, 3)), int(r.integers(0, 3))
+    k = max(1, first + last) + int(r.integers(0, 6))
+    top = K.blocks_top(q, cache, k, first=first, last=last, **kw)
+    same_top(top, want_top(cache, host(q), lengths, order, k, first, last, most=most, start=start))
+    out.fill_(float("nan"))
+    K.decode_blocks(q, cache, top=top, out=out, **kw)
+    check_decode(cache, kk, vv, host(q), host(out), lengths, order, most=most, start=start, top=top.cpu().numpy())
+
+
+@pytest.mark.parametrize("page,M,G,dtype", [(32, 1 << 18, 3, "bf16"), (64, 1 << 14, 8, "f32")])
+def test_millions_of_tokens(K, page, M, G, dtype):
+    """A long table over few pages: every page many times, so that scores tie by the thousand and a page's weight is
+    that of its copies."""
+    d, n_pages, k = 64, 37, 300
+    cache, _, _ = filled(K, 1, 1, d, page, [page * n_pages], spare=0)
+    ids = np.random.default_rng(1).integers(0, n_pages, M)
+    n = M * page - 11
+    long = K.Blocks(cache.pool, cache.refs, dev(ids[None]), dev([M]), dev([n]), page, d)
+    q = normal((1, 1, G, 1, d), dtype, 2, 0.5).cuda()
+    whole = K.Blocks(cache.pool, cache.refs, dev(np.arange(n_pages)[None]), dev([n_pages]), dev([n_pages * page]), page, d)
+    kk, vv = (host(x)[0, 0, 0].reshape(n_pages, page, d) for x in K.blocks_read(whole, n_pages * page, dtype=torch.float32))
+    count = np.bincount(ids[:-1], minlength=n_pages)[:, None] * np.ones((1, page))
+    count[ids[-1], :page - 11] += 1                                   # the last block is not full
+    x = np.einsum("gd,ptd->gpt", host(q)[0, 0, :, 0], kk) / np.sqrt(d)
+    w = count * np.exp(x - x.max())
+    want = np.einsum("gpt,ptd->gd", w, vv) / w.sum((1, 2))[:, None]
+    mag = np.einsum("gpt,ptd->gd", w, np.abs(vv)) / w.sum((1, 2))[:, None]
+    biggest = float((np.abs(host(q)[0, 0, :, 0]) @ np.abs(kk.reshape(-1, d)).T).max() / np.sqrt(d))
+    check(host(K.decode_blocks(q, long))[0, 0, :, 0], want, mag, biggest, n, d)
+    top = K.blocks_top(q, long, k, first=1, last=2)
+    lo, hi = (host(t)[0, 0, 0] for t in K.blocks_bounds(whole, n_pages, dtype=torch.float32))
+    score = O.block_scores(host(q)[0, 0, :, 0], lo, hi)[ids]
+    same_top(top[0, 0], np.array(O.top_blocks(score, k, 1, 2))[None, None])
+    chosen = top[0, 0, 0, 0].cpu().numpy()
+    rows = [(kk[ids[b]], vv[ids[b]]) for b in chosen[:-1]] + [(kk[ids[-1]][:page - 11], vv[ids[-1]][:page - 11])]
+    ks, vs = (np.concatenate([t[i] for t in rows]) for i in (0, 1))
+    want, mag, biggest = O.attend(host(q)[0, 0, :, 0], ks, vs, 1 / np.sqrt(d))
+    check(host(K.decode_blocks(q, long, top=top))[0, 0, :, 0], want, mag, biggest, len(ks), d)
+
+
+def test_calls_that_read_may_overlap(K):
+    """Choice and attention of two streams at once, each with workspaces of its own, over one cache."""
+    lengths = [3000, 700, 2500, 64]
+    cache, _, _ = filled(K, 1, 4, 128, 32, lengths)
+    qs = [normal((1, 4, 16, T, 128), "bf16", T).cuda() for T in (1, 3)]
+    want = []
+    for q in qs:
+        top = K.blocks_top(q, cache, 9)
+        want.append((top, K.decode_blocks(q, cache), K.decode_blocks(q, cache, top=top)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = [[], []]
+    for _ in range(10):
+        for i, (q, s) in enumerate(zip(qs, streams)):
+            top = K.blocks_top(q, cache, 9, stream=s)
+            got[i].append((top, K.decode_blocks(q, cache, stream=s), K.decode_blocks(q, cache, top=top, stream=s)))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_captured_calls_share_a_workspace(K, T):
+    """Two graphs over one workspace, replayed in turn with eager calls between them."""
+    cache, _, _ = filled(K, 1, 2, 64, 64, [5000, 40, 1300])
+    qs = [normal((1, 3, 8, T, 64), "bf16", 5 + i).cuda() for i in (0, 1)]
+    wd = torch.empty(K.decode_blocks_workspace_size(1, 3, 8, 2, T, 64), dtype=torch.uint8, device="cuda")
+    wt = torch.empty(K.blocks_top_workspace_size(1, 3, 2, T, cache.c.M * 64, 64), dtype=torch.uint8, device="cuda")
+    want = [(K.blocks_top(q, cache, 6), K.decode_blocks(q, cache)) for q in qs]
+    outs = [(torch.zeros_like(a), torch.zeros_like(b)) for a, b in want]
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    for q, (a, b) in zip(qs, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            K.blocks_top(q, cache, 6, out=a, workspace=wt)
+            K.decode_blocks(q, cache, out=b, workspace=wd)
+        graphs.append(g)
+    for i in range(6):
+        for a, b in outs:
+            a.fill_(-7)
+            b.fill_(float("nan"))
+        wd.fill_(255)
+        wt.fill_(i)
+        for g in graphs:
+            g.replay()
+        eager = K.decode_blocks(qs[0], cache, workspace=wd)
+        assert torch.equal(eager, want[0][1])
+        for (a, b), (wa, wb) in zip(outs, want):
+            assert torch.equal(a, wa) and torch.equal(b, wb), i

@@ -39,7 +39,11 @@ struct BlockView {
 // work at the end, the fewer the shorter the splits are (64 of up to 32768: 251 us with
 // one, 231, 216 and 211; 8 57, 54, 53 and 52; but 4 33, 33, 36 and 35, 2 20, 21, 25 and
 // 27): from kBlocksSeveral entries on those are cut for four.
-constexpr int kBlocksLevel = 1, kBlocksRagged = 4, kBlocksSeveral = 8;
+// Rows of 64 channels are half as many bytes to a step, too few in flight in one workgroup
+// to read at full rate: level ones are cut for two where there are kBlocksLong quanta to
+// a unit (8 sequences of 122844, 2 KV heads 47.7 us for 53.6, 4 of 20000, 4 heads 14.5 for
+// 15.4, but 2 heads, five quanta to a unit, 12.5 for 11.9).
+constexpr int kBlocksLevel = 1, kBlocksRagged = 4, kBlocksSeveral = 8, kBlocksLong = 8;
 
 // Plan of a decode over blocks.  Query tokens of a sample are taken `per` at a time,
 // an entry each: as many as the sixteen columns of a product hold heads for, or one
@@ -72,7 +76,7 @@ inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long 
     const long long segs = (long long)p.pairs * p.entries;
     p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > kPagesWhole ? segs / 8 : kPagesWhole);
     auto splits = [&](int per_unit) { return p.pairs < per_unit * kDecodeUnits ? per_unit * kDecodeUnits / p.pairs : 1; };
-    p.level = splits(kBlocksLevel);
+    p.level = splits(d == 64 && segs * quanta >= kBlocksLong * kDecodeUnits ? 2 * kBlocksLevel : kBlocksLevel);
     // chosen blocks are equally many
     p.share = sparse || p.entries < kBlocksSeveral ? p.level : splits(kBlocksRagged);
     long long groups = (long long)p.share + p.entries;

@@ -43,21 +43,27 @@ struct Eight {
             return __uint_as_float(v[e / 4][e % 4]);
         }
     }
+    // Once: non-temporal, for what is not read soon.
+    template <bool Once>
     __device__ __forceinline__ static void store(char* row, int part, const float (&x)[8]) {
+        u32x4 o[kRegs];
         if constexpr (kRegs == 1) {
-            u32x4 o;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bf16x2 two = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
-                o[i] = __builtin_bit_cast(uint32_t, two);
+                o[0][i] = __builtin_bit_cast(uint32_t, two);
             }
-            __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>(row) + part);
         } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const f32x4 o = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-                __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(row) + 2 * part + i);
-            }
+            for (int i = 0; i < 8; ++i) o[i / 4][i % 4] = __float_as_uint(x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kRegs; ++i) {
+            u32x4* at = reinterpret_cast<u32x4*>(row) + part * kRegs + i;
+            if constexpr (Once)
+                __builtin_nontemporal_store(o[i], at);
+            else
+                *at = o[i];
         }
     }
 };
@@ -275,9 +281,12 @@ struct Lanes {
     static constexpr int kStep = kThreads / kRow;  // rows per step
 };
 
-// kHeads heads of the queries of Lanes::kStep tokens, whose angles are loaded once.
-template <typename T, int D>
-__device__ __forceinline__ void turn_queries(const RowView& view, char* out, const WriteGrid& g, unsigned x,
+// kBlocksQueryHeads heads of the queries of Lanes::kStep tokens, whose angles are loaded
+// once.  Lines: a wave's store covers whole lines.  Those go past the caches (4 samples of
+// 4000 tokens, 32 heads 73 us, 80 through them); others meet their other halves there (32
+// of 2173 tokens, 16 heads, 16 turned channels 137 us, 187 past them).
+template <typename T, int D, bool Lines>
+__device__ __forceinline__ void queries_turned(const RowView& view, char* out, const WriteGrid& g, unsigned x,
                                              const BlockRotation& rot) {
     using Ln = Lanes<D, 2>;
     const unsigned sets = (unsigned)(g.heads + kBlocksQueryHeads - 1) / kBlocksQueryHeads;
@@ -300,11 +309,20 @@ __device__ __forceinline__ void turn_queries(const RowView& view, char* out, con
     for (int h = 0; h < kBlocksQueryHeads; ++h) {
         if ((int)h0 + h >= g.heads) break;
         float z[16];
-        raw[h].template turn<sizeof(T) == 2 ? Turned::Half : Turned::Float>(angles, rot.pairs, at.turned, z);
+        raw[h].template turn<sizeof(T) == 2 ? Turned::Half : Turned::Float>(angles, !Lines && rot.pairs, at.turned, z);
         char* o = out + ((((size_t)l * g.B + b) * g.heads + h0 + h) * g.T + t) * (D * sizeof(T));
-        Eight<T>::store(o, at.a, *reinterpret_cast<const float(*)[8]>(z));
-        Eight<T>::store(o, at.b, *reinterpret_cast<const float(*)[8]>(z + 8));
+        Eight<T>::template store<Lines>(o, at.a, *reinterpret_cast<const float(*)[8]>(z));
+        Eight<T>::template store<Lines>(o, at.b, *reinterpret_cast<const float(*)[8]>(z + 8));
     }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void turn_queries(const RowView& view, char* out, const WriteGrid& g, unsigned x,
+                                             const BlockRotation& rot) {
+    if (sizeof(T) == 2 && rot.r == D && !rot.pairs)
+        queries_turned<T, D, sizeof(T) == 2>(view, out, g, x, rot);
+    else
+        queries_turned<T, D, false>(view, out, g, x, rot);
 }
 
 // The keys or the values (Ends: keys) of one block: NP pieces to a lane, ITEMS rows to
@@ -775,7 +793,7 @@ __global__ __launch_bounds__(kThreads) void read_blocks(PagePool p, ReadGrid g, 
         const float unit = scale_float(scale_of((uint8_t)s));
         floats4(w[0], unit, *reinterpret_cast<float(*)[4]>(x));
         floats4(w[1], unit, *reinterpret_cast<float(*)[4]>(x + 4));
-        Eight<T>::store(o, part, x);
+        Eight<T>::template store<true>(o, part, x);
     };
 #pragma unroll
     for (int it = 0; it < kReadItems; ++it) {

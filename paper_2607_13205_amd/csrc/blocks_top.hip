@@ -19,8 +19,10 @@ constexpr int kThreads = 256;
 constexpr int kScored = 64;              // blocks per workgroup of top_scores,
 constexpr int kTokens = 4;               // and query tokens that share its read of their bounds
 // Workgroups from which each takes more blocks, up to eight times as many: 16 sequences
-// of 4096 blocks 47, 50 and 55 us for 1024, 2048 and 4096; of up to that many, two query
-// tokens, 41, 33 and 38.
+// of 4096 blocks 46, 50 and 49 us for 1024, 2048 and 4096; of up to that many 36, 29 and
+// 30, with two query tokens of 3125 47, 37 and 43.  The first blocks of all sequences come
+// first, so that workgroups without blocks are the last ones (sequence after sequence:
+// the first two 50 and 35 for 2048, the third 33).
 constexpr int kScoreGroups = 2048, kMostTiles = 8;
 
 template <int N>
@@ -144,13 +146,13 @@ struct Bounds {
 // (two query tokens for one, 3125 blocks: 60 us and 46, the choice included).  Small calls
 // are latency: 5 us for one sequence of 1024 blocks.
 template <typename T, int D, int TOKENS>
-__global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, PagePool p, TopGrid g, int chunks,
+__global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, PagePool p, TopGrid g, int sets,
                                                        int tiles, int groups, uint32_t* __restrict__ keys) {
     using B = Bounds<D>;
     // channels 2 e, 2 e + 1 of every sixteen, side by side
     __shared__ __attribute__((aligned(16))) double s_up[TOKENS][2][8][B::kRow][2];
-    const unsigned y = blockIdx.x / (unsigned)chunks, lbj = y / (unsigned)groups;
-    const int first = (int)(blockIdx.x - y * chunks) * tiles * kScored, t0 = (int)(y - lbj * groups) * TOKENS;
+    const unsigned chunk = blockIdx.x / (unsigned)sets, y = blockIdx.x - chunk * sets, lbj = y / (unsigned)groups;
+    const int first = (int)chunk * tiles * kScored, t0 = (int)(y - lbj * groups) * TOKENS;
     const int tokens = min(TOKENS, g.view.T - t0);
     const Segment x = segment_of(p, g, lbj * (unsigned)g.view.T + (t0 + tokens - 1));  // the token that sees most
     if (x.blocks <= g.k || first >= x.blocks) return;  // all are taken, or none here
@@ -379,7 +381,7 @@ hipError_t launch_blocks_top(const void* q, int dtype, const PagePool& p, int d,
         const int tiles = (int)std::min(std::max(pairs * all / kScoreGroups, 1LL), (long long)kMostTiles);
         const int chunks = (all + tiles - 1) / tiles;
         auto launch = [&](auto kernel, auto rows) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * chunks)), dim3(kThreads), 0, st, rows, p, g, chunks, tiles,
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * chunks)), dim3(kThreads), 0, st, rows, p, g, (int)pairs, tiles,
                                groups, keys);
         };
         auto by_size = [&](auto rows) {

@@ -22,7 +22,8 @@ from .pages import _CPages, _ints, _new, _on, _rows, _workspace
 
 class _CRotation(ctypes.Structure):
     """kve_rotation_t"""
-    _fields_ = [(n, ctypes.c_void_p) for n in ("cos", "sin", "position")] + [(n, ctypes.c_int) for n in ("P", "r", "pairs")]
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cos", "sin", "position")] + \
+        [(n, ctypes.c_int) for n in ("P", "r", "pairs")]
 
 
 @functools.lru_cache(maxsize=None)
@@ -137,7 +138,8 @@ def blocks_append(k, v, blocks: Blocks, start, n_new=None, seq=None, rotation: R
             raise ValueError("queries are turned: they need a rotation")
         if q.dim() != 5 or q.shape[0] != blocks.c.L or q.shape[1] != B or q.shape[3:] != (T, blocks.d) or \
                 q.dtype is not k.dtype or q.get_device() != blocks.index:
-            raise ValueError(f"q must be [L={blocks.L}, B={B}, Hq, T={T}, d={blocks.d}] of k's type on the cache's device")
+            raise ValueError(f"q must be [L={blocks.L}, B={B}, Hq, T={T}, d={blocks.d}] of k's type "
+                             "on the cache's device")
         Hq = q.shape[2]
         if q.is_contiguous():
             qp = q.data_ptr()

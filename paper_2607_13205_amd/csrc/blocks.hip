@@ -241,12 +241,14 @@ template <int N, typename F>
 __device__ __forceinline__ void over_quarters(float (&x)[N], F f) {
 #pragma unroll
     for (int e = 0; e < N / 2; ++e) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[e]), __float_as_uint(x[e + N / 2]), false, false);
+        const auto r =
+            __builtin_amdgcn_permlane32_swap(__float_as_uint(x[e]), __float_as_uint(x[e + N / 2]), false, false);
         x[e] = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
     }
 #pragma unroll
     for (int e = 0; e < N / 4; ++e) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(x[e + N / 4]), false, false);
+        const auto r =
+            __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(x[e + N / 4]), false, false);
         x[e] = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
     }
 }
@@ -287,7 +289,7 @@ struct Lanes {
 // of 2173 tokens, 16 heads, 16 turned channels 137 us, 187 past them).
 template <typename T, int D, bool Lines>
 __device__ __forceinline__ void queries_turned(const RowView& view, char* out, const WriteGrid& g, unsigned x,
-                                             const BlockRotation& rot) {
+                                               const BlockRotation& rot) {
     using Ln = Lanes<D, 2>;
     const unsigned sets = (unsigned)(g.heads + kBlocksQueryHeads - 1) / kBlocksQueryHeads;
     const unsigned y = x / sets, h0 = (x - y * sets) * kBlocksQueryHeads;
@@ -330,10 +332,10 @@ __device__ __forceinline__ void turn_queries(const RowView& view, char* out, con
 // page, the block's scale), so everything is loaded as soon as its address is known:
 // the new rows and their angles beside the look-up of the block.
 template <typename T, int D, int PAGE, int NP, bool Gather, bool Ends>
-__device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWaves * kParts<D>][D], const RowView& view, int role,
-                                            const WriteGrid& g, int l, int b, int j, int i, size_t seg,
-                                            const int32_t* idx, int slot, int s0, int n, const BlockRotation& rot,
-                                            const PagePool& p) {
+__device__ __forceinline__ void write_block(uint32_t* s_top, float (*s_ends)[kWaves * kParts<D>][D],
+                                            const RowView& view, int role, const WriteGrid& g, int l, int b, int j,
+                                            int i, size_t seg, const int32_t* idx, int slot, int s0, int n,
+                                            const BlockRotation& rot, const PagePool& p) {
     using Ln = Lanes<D, NP>;
     constexpr int ITEMS = (PAGE + Ln::kStep - 1) / Ln::kStep, kShift = PAGE == 32 ? 5 : PAGE == 64 ? 6 : 7;
     const int part = threadIdx.x % Ln::kRow, in = threadIdx.x / Ln::kRow;
@@ -782,8 +784,9 @@ __global__ __launch_bounds__(kThreads) void read_blocks(PagePool p, ReadGrid g, 
     for (int it = 0; it < kReadItems; ++it) {
         if (block[it] == nullptr) continue;
         const char* tail = block[it] + tail_at<D>(p.shift);
-        const char* rows[2] = {Bounds ? tail + kBlockScales : block[it] + (size_t)tok[it] * D,
-                               Bounds ? tail + kBlockScales + D : block[it] + ((size_t)D << p.shift) + (size_t)tok[it] * D};
+        const char* row = block[it] + (size_t)tok[it] * D;
+        const char* rows[2] = {Bounds ? tail + kBlockScales : row,
+                               Bounds ? tail + kBlockScales + D : row + ((size_t)D << p.shift)};
         a[it] = reinterpret_cast<const u32x2*>(rows[0])[part];
         c[it] = reinterpret_cast<const u32x2*>(rows[1])[part];
         scales[it] = *reinterpret_cast<const uint16_t*>(tail);
@@ -809,8 +812,8 @@ void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out
                const int32_t* idx, const int32_t* count, const int32_t* start, const int32_t* seq,
                const BlockRotation& rot, const PagePool& p, hipStream_t st) {
     if (idx != nullptr)
-        hipLaunchKernelGGL((write_blocks<T, D, PAGE, true>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out, g, idx,
-                           count, start, seq, rot, p);
+        hipLaunchKernelGGL((write_blocks<T, D, PAGE, true>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out, g,
+                           idx, count, start, seq, rot, p);
     else
         hipLaunchKernelGGL((write_blocks<T, D, PAGE, false>), dim3(groups), dim3(kThreads), 0, st, k, v, q, q_out, g,
                            idx, count, start, seq, rot, p);

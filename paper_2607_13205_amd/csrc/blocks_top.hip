@@ -241,8 +241,8 @@ __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* s, uint32_t& tota
     __syncthreads();
     const uint32_t sums = wave(lane < kSelectWaves ? s[lane] : 0u);
     total = (uint32_t)__builtin_amdgcn_readlane((int)sums, kSelectWaves - 1);
-    const uint32_t before = w > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, __builtin_amdgcn_readfirstlane(w) - 1)
-                                  : 0u;
+    const int last = __builtin_amdgcn_readfirstlane(w) - 1;  // the wave before
+    const uint32_t before = last >= 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, last) : 0u;
     return before + inc - x;
 }
 
@@ -381,8 +381,8 @@ hipError_t launch_blocks_top(const void* q, int dtype, const PagePool& p, int d,
         const int tiles = (int)std::min(std::max(pairs * all / kScoreGroups, 1LL), (long long)kMostTiles);
         const int chunks = (all + tiles - 1) / tiles;
         auto launch = [&](auto kernel, auto rows) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * chunks)), dim3(kThreads), 0, st, rows, p, g, (int)pairs, tiles,
-                               groups, keys);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(pairs * chunks)), dim3(kThreads), 0, st, rows, p, g, (int)pairs,
+                               tiles, groups, keys);
         };
         auto by_size = [&](auto rows) {
             using T = std::remove_const_t<std::remove_pointer_t<decltype(rows)>>;

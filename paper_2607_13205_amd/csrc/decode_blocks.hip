@@ -285,12 +285,18 @@ struct Entries {
     int k, Hq, G, per, tiles, count;
 };
 
-__device__ __forceinline__ Sequence entry_of(const PagePool& p, const Entries& n, int e) {
-    if (e >= n.count) return Sequence{-1, 0};
+// An entry as a lane holds it: the rows to go through, and those that its last query
+// token sees.
+struct Entry : Sequence {
+    int seen;
+};
+
+__device__ __forceinline__ Entry entry_of(const PagePool& p, const Entries& n, int e) {
+    if (e >= n.count) return Entry{{-1, 0}, 0};
     const int b = e / n.tiles, t0 = (e - b * n.tiles) * n.per;
     const int slot = slot_of(n.view.seq, b, p.S);
     const int seen = seen_by(p, n.view, slot, b, min(t0 + n.per, n.view.T) - 1);
-    return Sequence{slot, n.top == nullptr ? seen : seen > 0 ? n.k << p.shift : 0};
+    return Entry{{slot, n.top == nullptr ? seen : seen > 0 ? n.k << p.shift : 0}, seen};
 }
 
 // Output row of row r (query token r / G of the entry, head r % G of the group).
@@ -308,11 +314,10 @@ __device__ __forceinline__ size_t row_at(const Entries& n, int l, int b, int j, 
 // query token where there is one: three and four slots, unrolled, lose up to a quarter
 // (one sequence of 32768: 19 us with two, 24 with either).
 template <typename T, int D, int NH, bool Several>
-__global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict__ q, PagePool p, Entries n,
-                                                               int share, int level, int groups, int R, int whole, float sl2,
-                                                               float* __restrict__ ws_o, float2* __restrict__ ws_ml,
-                                                               SplitRange* __restrict__ ranges,
-                                                               float* __restrict__ out) {
+__global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict__ q, PagePool p, Entries n, int share,
+                                                            int level, int groups, int R, int whole, float sl2,
+                                                            float* __restrict__ ws_o, float2* __restrict__ ws_ml,
+                                                            SplitRange* __restrict__ ranges, float* __restrict__ out) {
     constexpr int NC = D / 16, NWV = kWaves;
     using S = Slot<D>;
     // the waves' rings, and behind their last use the waves' sums
@@ -329,13 +334,19 @@ __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict_
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int c = lane & 15, quarter = lane >> 4;
 
-    auto of = [&](int e) { return entry_of(p, n, e); };
     Work work{x, -1, 0, 0, {x, 1}};
+    int seen_most;
     if (whole) {
-        const Sequence s = of(x);
+        const Entry s = entry_of(p, n, x);
         work.slot = __builtin_amdgcn_readfirstlane(s.slot);
         work.k1 = __builtin_amdgcn_readfirstlane(s.tokens);
+        seen_most = __builtin_amdgcn_readfirstlane(s.seen);
     } else {
+        // up to 64 entries: looked up once, by the lane of their number
+        const bool few = n.count <= kWave;
+        Entry mine{{-1, 0}, 0};
+        if (few) mine = entry_of(p, n, lane);
+        auto of = [&](int e) -> Sequence { return few ? mine : entry_of(p, n, e); };
         int* staged = nullptr;
         if (n.count > kWave && n.count <= kStaged) {
             static_assert(kStaged * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
@@ -348,6 +359,8 @@ __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict_
                          level);
         if (staged != nullptr) __syncthreads();  // the rings take the lengths' place
         if (work.b < 0) return;
+        seen_most = few ? __builtin_amdgcn_readlane(mine.seen, work.b)
+                        : __builtin_amdgcn_readfirstlane(entry_of(p, n, work.b).seen);
     }
     const int slot = work.slot, k0 = work.k0, k1 = work.k1;
     const int b = work.b / n.tiles, t0 = (work.b - b * n.tiles) * n.per;
@@ -359,9 +372,11 @@ __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict_
     const int col = c & (NH - 1);
     const bool used = col < rows && c < (NH == 4 ? 12 : 16);
     const int tile = used ? col / n.G : -1;
-    int seen = used ? seen_by(p, n.view, slot, b, t0 + tile) : 0;
-    const int seen_most = __builtin_amdgcn_readfirstlane(seen_by(p, n.view, slot, b, t0 + here - 1));
-    const int seen_least = __builtin_amdgcn_readfirstlane(seen_by(p, n.view, slot, b, t0));
+    int seen = used ? seen_most : 0, seen_least = seen_most;
+    if constexpr (Several) {
+        if (used) seen = seen_by(p, n.view, slot, b, t0 + tile);
+        seen_least = __builtin_amdgcn_readfirstlane(seen_by(p, n.view, slot, b, t0));
+    }
 
     Sums<T, D, NH> sums;
     sums.start(used ? q + row_at(n, l, b, j, t0, col) * D : nullptr);
@@ -491,8 +506,8 @@ hipError_t run_columns(const void* q, const PagePool& p, const Entries& n, const
     SplitRange* ranges = reinterpret_cast<SplitRange*>(static_cast<char*>(ws) + plan.off_ranges);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads), 0, st,
-                           static_cast<const T*>(q), p, n, plan.share, plan.level, plan.groups, plan.R, (int)plan.whole, scale * kLog2e,
-                           wo, wml, ranges, out);
+                           static_cast<const T*>(q), p, n, plan.share, plan.level, plan.groups, plan.R,
+                           (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
     };
     if (plan.per > 1)
         launch(blocks_split<T, D, NH, true>);

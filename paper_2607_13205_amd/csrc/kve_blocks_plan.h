@@ -75,7 +75,9 @@ inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long 
     const long long quanta = (tokens + kDecodeQuantum - 1) / kDecodeQuantum;
     const long long segs = (long long)p.pairs * p.entries;
     p.whole = quanta <= kDecodeLongest && quanta <= (segs / 8 > kPagesWhole ? segs / 8 : kPagesWhole);
-    auto splits = [&](int per_unit) { return p.pairs < per_unit * kDecodeUnits ? per_unit * kDecodeUnits / p.pairs : 1; };
+    auto splits = [&](int per_unit) {
+        return p.pairs < per_unit * kDecodeUnits ? per_unit * kDecodeUnits / p.pairs : 1;
+    };
     p.level = splits(d == 64 && segs * quanta >= kBlocksLong * kDecodeUnits ? 2 * kBlocksLevel : kBlocksLevel);
     // chosen blocks are equally many
     p.share = sparse || p.entries < kBlocksSeveral ? p.level : splits(kBlocksRagged);

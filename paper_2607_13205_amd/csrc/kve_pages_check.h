@@ -48,7 +48,8 @@ inline kve_status_t check_entries(const char* fn, const kve_pages_t* c, const in
 }
 
 // B samples of `cap` rows each in a call on the cache's rows.
-inline kve_status_t check_rows(const char* fn, const kve_pages_t* c, int B, int cap, const int32_t* seq, bool need_seq) {
+inline kve_status_t check_rows(const char* fn, const kve_pages_t* c, int B, int cap, const int32_t* seq,
+                               bool need_seq) {
     if (B <= 0 || cap < 0) return fail(KVE_ERR_INVALID_ARG, "%s: invalid sizes (B=%d rows=%d)", fn, B, cap);
     if (need_seq && seq == nullptr) return fail(KVE_ERR_INVALID_ARG, "%s: null slots", fn);
     if (seq == nullptr && B > c->S)

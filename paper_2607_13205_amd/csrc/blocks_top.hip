@@ -219,9 +219,9 @@ __global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, 
     }
 }
 
-// Exclusive sum over the threads of a workgroup of kSelect, and over all in `total`.
-// s: kSelectWaves words of LDS, free again behind the next barrier.
-constexpr int kSelect = 1024, kSelectWaves = kSelect / kWave;
+// Exclusive sum over the threads of a workgroup of WAVES waves, and over all in `total`.
+// s: WAVES words of LDS, free again behind the next barrier.
+template <int WAVES>
 __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* s, uint32_t& total) {
     const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
     auto step = [](uint32_t v, auto ctrl, auto rows) {
@@ -239,29 +239,30 @@ __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* s, uint32_t& tota
     const uint32_t inc = wave(x);
     if (lane == kWave - 1) s[w] = inc;
     __syncthreads();
-    const uint32_t sums = wave(lane < kSelectWaves ? s[lane] : 0u);
-    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, kSelectWaves - 1);
+    const uint32_t sums = wave(lane < WAVES ? s[lane] : 0u);
+    total = (uint32_t)__builtin_amdgcn_readlane((int)sums, WAVES - 1);
     const int last = __builtin_amdgcn_readfirstlane(w) - 1;  // the wave before
     const uint32_t before = last >= 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, last) : 0u;
     return before + inc - x;
 }
 
 // One workgroup per segment.  The blocks that are not forced compete for the places
-// that the forced ones leave: the lowest key that gets one is found in digits of 11
+// that the forced ones leave: the lowest key that gets one is found in digits of BITS
 // bits, from the highest bit in which the keys differ on (keys of one sign and a few
 // binades, as scores are, spread over the digits of the first pass, and the counts in
 // LDS do not collide), until all that share its digits get one.  4096 blocks: 6 us; with
 // digits of 8 bits from the top one, 256 threads and the keys loaded again for each, 25.
-__global__ __launch_bounds__(kSelect) void top_select(PagePool p, TopGrid g, const uint32_t* __restrict__ keys,
+template <int THREADS, int BITS>
+__global__ __launch_bounds__(THREADS) void top_select(PagePool p, TopGrid g, const uint32_t* __restrict__ keys,
                                                       int32_t* __restrict__ top) {
-    constexpr int kBits = 11, kBins = 1 << kBits, kTile = 4 * kSelect;
-    __shared__ uint32_t s_hist[kBins], s_scan[2][kSelectWaves], s_ends[2][kSelectWaves], s_pick[3];
+    constexpr int kWaves = THREADS / kWave, kBins = 1 << BITS, kOwn = kBins / THREADS, kTile = 4 * THREADS;
+    __shared__ uint32_t s_hist[kBins], s_scan[2][kWaves], s_ends[2][kWaves], s_pick[3];
     const unsigned seg = blockIdx.x;
     const Segment x = segment_of(p, g, seg);
     int32_t* out = top + (size_t)seg * g.k;
     const int n = x.blocks, tid = threadIdx.x;
     if (n <= g.k) {
-        for (int i = tid; i < g.k; i += kSelect) out[i] = i < n ? i : -1;
+        for (int i = tid; i < g.k; i += THREADS) out[i] = i < n ? i : -1;
         return;
     }
     const uint32_t* key = keys + (size_t)seg * g.pitch;
@@ -283,7 +284,7 @@ __global__ __launch_bounds__(kSelect) void top_select(PagePool p, TopGrid g, con
             }
         }
     };
-    for (int i = tid; i < kBins; i += kSelect) s_hist[i] = 0;
+    for (int i = tid; i < kBins; i += THREADS) s_hist[i] = 0;
     uint32_t least = 0xffffffffu, most = 0;
     each([&](uint32_t y) {
         least = min(least, y);
@@ -301,7 +302,7 @@ __global__ __launch_bounds__(kSelect) void top_select(PagePool p, TopGrid g, con
     }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
         least = min(least, s_ends[0][w]);
         most = max(most, s_ends[1][w]);
     }
@@ -310,24 +311,30 @@ __global__ __launch_bounds__(kSelect) void top_select(PagePool p, TopGrid g, con
     uint32_t prefix = shift < 32 ? most >> shift : 0u;
     bool done = want == 0 || shift == 0;
     while (!done) {
-        const int low = max(0, shift - kBits), bits = shift - low;
+        const int low = max(0, shift - BITS), bits = shift - low;
         each([&](uint32_t y) {
             if (shift == 32 || y >> shift == prefix) atomicAdd(&s_hist[(y >> low) & ((1u << bits) - 1)], 1u);
         });
         __syncthreads();
-        // thread e: digits kBins - 1 - 2 e and the one below it
-        const uint32_t a = s_hist[kBins - 1 - 2 * tid], b = s_hist[kBins - 2 - 2 * tid];
-        uint32_t total;
-        const uint32_t above = scan(a + b, s_scan[0], total);
-        if (above < want && above + a + b >= want) {
-            const bool first = above + a >= want;
-            s_pick[0] = (uint32_t)(kBins - 1 - 2 * tid - !first);
-            s_pick[1] = want - (first ? above : above + a);
-            s_pick[2] = first ? a : b;
+        // thread e: kOwn digits, from kBins - 1 - kOwn e downwards
+        uint32_t* own = s_hist + kBins - kOwn * (tid + 1);
+        uint32_t counts[kOwn], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            counts[i] = own[kOwn - 1 - i];
+            sum += counts[i];
         }
-        // the next pass counts from zero
-        s_hist[kBins - 1 - 2 * tid] = 0;
-        s_hist[kBins - 2 - 2 * tid] = 0;
+        uint32_t total, above = scan<kWaves>(sum, s_scan[0], total);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            if (above < want && above + counts[i] >= want) {
+                s_pick[0] = (uint32_t)(kBins - 1 - kOwn * tid - i);
+                s_pick[1] = want - above;
+                s_pick[2] = counts[i];
+            }
+            above += counts[i];
+            own[i] = 0;  // the next pass counts from zero
+        }
         __syncthreads();
         prefix = prefix << bits | s_pick[0];
         want = s_pick[1];
@@ -352,7 +359,7 @@ __global__ __launch_bounds__(kSelect) void top_select(PagePool p, TopGrid g, con
             own += (take[e] ? 1u : 0u) + (same[e] ? 0x10000u : 0u);
         }
         uint32_t total;
-        const uint32_t before = scan(own, s_scan[turn], total);
+        const uint32_t before = scan<kWaves>(own, s_scan[turn], total);
         uint32_t at = placed + (before & 0xffffu), ties = equal + (before >> 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -396,7 +403,21 @@ hipError_t launch_blocks_top(const void* q, int dtype, const PagePool& p, int d,
         else
             by_size(static_cast<const float*>(q));
     }
-    hipLaunchKernelGGL(top_select, dim3(segs), dim3(kSelect), 0, st, p, g, keys, top);
+    // as few threads as hold a segment with four keys each: one sequence of 1024 blocks, 8
+    // segments, 8.6 us with 256 threads, 9.9 with 1024, scores included, 64 of 128 blocks
+    // 13.0 and 16.2; 16 of 2048 blocks 29.5 with 512, 30.2 with 1024; in two tiles they lose
+    // (4 of 4096 blocks, 2 KV heads: 13.2 with 512, 12.7 with 1024)
+    auto select = [&](auto threads, auto bits) {
+        constexpr int kThreadsOf = decltype(threads)::value;
+        hipLaunchKernelGGL((top_select<kThreadsOf, decltype(bits)::value>), dim3(segs), dim3(kThreadsOf), 0, st, p, g,
+                           keys, top);
+    };
+    if (g.pitch <= 4 * 256)
+        select(Int<256>{}, Int<10>{});
+    else if (g.pitch <= 4 * 512)
+        select(Int<512>{}, Int<11>{});
+    else
+        select(Int<1024>{}, Int<11>{});
     return hipGetLastError();
 }
 

@@ -704,6 +704,21 @@ def test_top_of_many_long_sequences(K, T, Hkv, page, M):
     same_top(top, want_top(shared, host(q), lengths, range(B), k, 1, 1))
 
 
+@pytest.mark.parametrize("M", [1023, 1024, 1025, 1029, 2047, 2048, 2049, 4096, 4097, 8200])
+@pytest.mark.parametrize("k,first,last", [(1, 0, 0), (64, 1, 1), (1000, 0, 3)])
+def test_top_where_the_choice_changes_its_form(K, M, k, first, last):
+    """Numbers of blocks around those that 256, 512 and 1024 threads hold at once; pages taken many times tie."""
+    L, B, Hkv, G, d, page, n_pages = 1, 3, 2, 2, 64, 32, 100
+    r = np.random.default_rng(M + k)
+    cache, _, _ = filled(K, L, Hkv, d, page, [page * n_pages])
+    lengths = [M * page, M * page - page, max(1, M * page // 2 - 5)]
+    table = dev(r.integers(0, n_pages, (B, M)))
+    shared = K.Blocks(cache.pool, cache.refs, table, dev([M] * B), dev(lengths), page, d)
+    q = normal((L, B, Hkv * G, 1, d), "bf16", M).cuda()
+    top = K.blocks_top(q, shared, k, first=first, last=last)
+    same_top(top, want_top(shared, host(q), lengths, range(B), k, first, last))
+
+
 def test_top_ties_nan_and_missing_pages(K):
     """Equal scores go to the lower block, NaN and missing ones come last, forced ones first."""
     d, page, n = 64, 32, 32 * 300

@@ -79,9 +79,6 @@ __device__ __forceinline__ double tiny(uint32_t w) {
 }
 constexpr double kUp = 0x1p800, kDown = 0x1p216;  // what brings products of such doubles back to scale, in two steps
 
-// Not 0 if one of four codes is NaN.
-__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-
 template <int W>
 __device__ __forceinline__ double add4(const double (&up)[16], const double (&down)[16], uint32_t lo, uint32_t hi,
                                        double sum) {

@@ -209,19 +209,29 @@ struct Sums {
             values<false>(v, scale, part, true);
             return;
         }
-        // a product takes no weight times a NaN for a NaN: query token by query token, the
-        // rows behind what it sees as zeros, and only its columns' sums kept
+        // a product takes no weight times a NaN for a NaN: without one, all query tokens at
+        // once, the rows that a column does not see with no weight
+        uint32_t bad = 0;
+#pragma unroll
+        for (int e = 0; e < NC / 4; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) bad |= nan_codes(v[e][i]);
+        const int turns = __builtin_amdgcn_ballot_w64(bad != 0) == 0 ? 1 : tiles;
+        // with one, query token by query token: the rows behind what it sees as zeros, and only
+        // its columns' sums kept.  One loop for both: with a third call of values() for the
+        // first, ROCm 7.2's compiler left den undefined behind it.
 #pragma unroll 1
-        for (int t = 0; t < tiles; ++t) {
-            const uint64_t mine = __builtin_amdgcn_ballot_w64(tile == t);
+        for (int t = 0; t < turns; ++t) {
+            const bool all = turns == 1;
+            const uint64_t mine = __builtin_amdgcn_ballot_w64(all || tile == t);
             if (mine == 0) continue;
-            const int seen = __builtin_amdgcn_readlane(left, __builtin_ctzll(mine));
+            const int seen = all ? kBlk : __builtin_amdgcn_readlane(left, __builtin_ctzll(mine));
             uint32_t vt[NC / 4][8];
 #pragma unroll
             for (int e = 0; e < NC / 4; ++e)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) vt[e][i] = 4 * i + quarter < seen ? v[e][i] : 0u;
-            values<true>(vt, scale, part, tile == t);
+            values<true>(vt, scale, part, all || tile == t);
         }
     }
 

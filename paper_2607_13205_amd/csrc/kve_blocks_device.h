@@ -36,6 +36,9 @@ __device__ __forceinline__ void floats4(uint32_t w, float scale, float (&x)[4]) 
     x[3] = b[1];
 }
 
+// Not 0 if one of four codes is NaN.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 // Rows that query token t of sample b sees in the sequence of `slot`.
 __device__ __forceinline__ int seen_by(const PagePool& p, const BlockView& v, int slot, int b, int t) {
     if (slot < 0) return 0;

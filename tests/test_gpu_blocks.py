@@ -592,6 +592,28 @@ def test_masked_rows_of_any_content_do_not_matter(K, G, T, most, dtype):
     assert np.isnan(out[..., T - 3:, :]).all() and np.array_equal(out[..., :T - 3, :], clean[..., :T - 3, :])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,T", [(1, 2), (1, 4), (2, 2), (3, 2), (2, 4), (5, 3), (4, 4), (8, 2), (16, 2), (1, 17)])
+def test_drafts_where_the_last_step_of_a_wave_differs_by_token(K, G, T, d, dtype):
+    """Sequences that end in the first, a middle or the last row of a wave's step of 32: each form of the kernel, over
+    finite values, and over a NaN that only the last token sees."""
+    page, lengths = 32, [T, 31, 32, 33, 39, 40, 63, 64, 65, 66, 129, 160, 161, 300]
+    cache, k, v = filled(K, 1, 2, d, page, lengths, seed=G + T)
+    q = normal((1, len(lengths), 2 * G, T, d), dtype, 9).cuda()
+    for most in (None, 300):
+        out = host(K.decode_blocks(q, cache, max_tokens=most))
+        check_decode(cache, k, v, host(q), out, lengths, range(len(lengths)), most=most)
+        bad = cache.pool.clone()
+        for s, n in enumerate(lengths):
+            bad[0, int(cache.table[s, (n - 1) // page]), 1, page * d + (n - 1) % page * d + 5] = 0x7F
+        nan = K.Blocks(bad, cache.refs, cache.table, cache.held, cache.length, page, d)
+        got = host(K.decode_blocks(q, nan, max_tokens=most))
+        assert np.isnan(got[:, :, G:, T - 1, 5]).all()
+        got[:, :, G:, T - 1, 5] = out[:, :, G:, T - 1, 5]
+        assert np.array_equal(got, out)
+
+
 @pytest.mark.parametrize("L,B,Hkv,G,page,longest,most,T", [
     (1, 150, 1, 2, 32, 700, None, 1),     # more sequences than a wave has lanes, several splits each
     (1, 64, 2, 4, 64, 200, 200, 1),

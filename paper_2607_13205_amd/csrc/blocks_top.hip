@@ -140,8 +140,8 @@ struct Bounds {
 // query tokens.  The next tile's bounds, and the page numbers of the one after it, are
 // on their way while a tile is scored.  16 sequences of 4096 blocks, 8 KV heads: 42 us for
 // three lines of 128 bytes to a block, 4.8 TB/s; the sums take half of that beside it
-// (two query tokens for one, 3125 blocks: 60 us and 46, the choice included).  Small calls
-// are latency: 5 us for one sequence of 1024 blocks.
+// (two query tokens for one, 3125 blocks: 54 us and 41, the choice included).  Small calls
+// are latency: 4.8 us for one sequence of 1024 blocks.
 template <typename T, int D, int TOKENS>
 __global__ __launch_bounds__(kThreads) void top_scores(const T* __restrict__ q, PagePool p, TopGrid g, int sets,
                                                        int tiles, int groups, uint32_t* __restrict__ keys) {

@@ -319,7 +319,7 @@ __device__ __forceinline__ size_t row_at(const Entries& n, int l, int b, int j, 
 // tokens in turn.  Several: entries of more than one query token.  Bound by the loads:
 // 8 sequences of 131072 tokens, 8 KV heads (2.1 GB) 323 us, 6.6 TB/s; without the
 // non-temporal hint 387.  A short call is a chain of latencies: 4 sequences of 32 tokens
-// 5.7 us, of 1639 11.2 with the merge, 30 to 40 KB to a compute unit.  For these the code
+// 5.4 us, of 1639 11.0 with the merge, 30 to 40 KB to a compute unit.  For these the code
 // is kept short, a loop over the steps that is not unrolled over the slots and no masks by
 // query token where there is one: three and four slots, unrolled, lose up to a quarter
 // (one sequence of 32768: 19 us with two, 24 with either).

@@ -745,23 +745,24 @@ struct ReadGrid {
     uint32_t rows;  // of all segments
 };
 
-// D / 8 lanes to a row, kReadItems rows to a lane, those of all segments one after the
+// D / 8 lanes to a row, Items rows to a lane, those of all segments one after the
 // other.  Bounds: row m is block first + m's bound, else the row at position first + m.
-// Bound by memory: 1.7 M rows 300 us, 1.29 GB read and written at 4.3 TB/s (sixteen
-// channels to a lane, whose 16-byte stores then lie apart: 385).
-constexpr int kReadItems = 2;
-template <typename T, int D, bool Bounds>
+// Past: loads past the caches, for more codes than the last one holds.  Bound by memory:
+// 1.7 M rows just written, 1.29 GB read and written, 255 us, 5.1 TB/s (through the caches
+// 280, and 300 with two rows to a lane; sixteen channels to a lane, whose 16-byte stores
+// then lie apart: 385).
+template <typename T, int D, bool Bounds, int Items, bool Past>
 __global__ __launch_bounds__(kThreads) void read_blocks(PagePool p, ReadGrid g, const int32_t* __restrict__ seq,
                                                         const int32_t* __restrict__ first,
                                                         const int32_t* __restrict__ count, char* __restrict__ a_out,
                                                         char* __restrict__ b_out) {
     constexpr int kRow = D / 8, kStep = kThreads / kRow;
     const int part = threadIdx.x % kRow;
-    const uint32_t at0 = blockIdx.x * (uint32_t)(kStep * kReadItems) + threadIdx.x / kRow;
-    const char* block[kReadItems];
-    int tok[kReadItems];
+    const uint32_t at0 = blockIdx.x * (uint32_t)(kStep * Items) + threadIdx.x / kRow;
+    const char* block[Items];
+    int tok[Items];
 #pragma unroll
-    for (int it = 0; it < kReadItems; ++it) {
+    for (int it = 0; it < Items; ++it) {
         const uint32_t at = at0 + it * kStep;
         block[it] = nullptr;
         if (at >= g.rows) continue;
@@ -778,17 +779,19 @@ __global__ __launch_bounds__(kThreads) void read_blocks(PagePool p, ReadGrid g, 
         tok[it] = pos & ((1 << p.shift) - 1);
         if (pg >= 0 && pg < p.n_pages) block[it] = block_at<D>(p, l, pg, j);
     }
-    u32x2 a[kReadItems], c[kReadItems];
-    uint32_t scales[kReadItems];
+    u32x2 a[Items], c[Items];
+    uint32_t scales[Items];
 #pragma unroll
-    for (int it = 0; it < kReadItems; ++it) {
+    for (int it = 0; it < Items; ++it) {
         if (block[it] == nullptr) continue;
         const char* tail = block[it] + tail_at<D>(p.shift);
         const char* row = block[it] + (size_t)tok[it] * D;
         const char* rows[2] = {Bounds ? tail + kBlockScales : row,
                                Bounds ? tail + kBlockScales + D : row + ((size_t)D << p.shift)};
-        a[it] = reinterpret_cast<const u32x2*>(rows[0])[part];
-        c[it] = reinterpret_cast<const u32x2*>(rows[1])[part];
+        const u32x2 *from = reinterpret_cast<const u32x2*>(rows[0]) + part,
+                    *other = reinterpret_cast<const u32x2*>(rows[1]) + part;
+        a[it] = Past ? __builtin_nontemporal_load(from) : *from;
+        c[it] = Past ? __builtin_nontemporal_load(other) : *other;
         scales[it] = *reinterpret_cast<const uint16_t*>(tail);
     }
     auto give = [&](char* o, u32x2 w, uint32_t s) {
@@ -799,7 +802,7 @@ __global__ __launch_bounds__(kThreads) void read_blocks(PagePool p, ReadGrid g, 
         Eight<T>::template store<true>(o, part, x);
     };
 #pragma unroll
-    for (int it = 0; it < kReadItems; ++it) {
+    for (int it = 0; it < Items; ++it) {
         if (block[it] == nullptr) continue;
         const size_t out = (size_t)(at0 + it * kStep) * (D * sizeof(T));
         if (a_out != nullptr) give(a_out + out, a[it], scales[it]);
@@ -831,14 +834,26 @@ void run_write(const RowView& k, const RowView& v, const RowView& q, char* q_out
         run_write<T, D, 128>(k, v, q, q_out, g, groups, idx, count, start, seq, rot, p, st);
 }
 
+// Codes, in bytes, from which a call reads them past the caches, two bytes an element four
+// rows to a lane: 1.7 M rows as above; a read of 1 M rows (268 MB) that the last call left
+// in the last-level cache 121 us through it, 141 past it, of 2 M 283 and 272.  Else a lane
+// takes one row: 128 rows 3.7 us, with two 4.1 and with four 5.3.  Float32 rows are best
+// one to a lane at every size: 2 M 520, two 571, four 580.
+constexpr long long kReadPast = (1LL << 28) + 1;
 template <typename T, int D, bool Bounds>
 void run_read(const PagePool& p, int B, int cap, const int32_t* seq, const int32_t* first, const int32_t* count,
               void* a, void* b, hipStream_t st) {
     const ReadGrid g{B, cap, (uint32_t)p.L * B * p.Hkv * (uint32_t)cap};
-    constexpr unsigned kRows = kThreads / (D / 8) * kReadItems;
-    const unsigned groups = (g.rows + kRows - 1) / kRows;
-    hipLaunchKernelGGL((read_blocks<T, D, Bounds>), dim3(groups), dim3(kThreads), 0, st, p, g, seq, first, count,
-                       static_cast<char*>(a), static_cast<char*>(b));
+    auto launch = [&](auto kernel, unsigned items) {
+        const unsigned rows = kThreads / (D / 8) * items;
+        hipLaunchKernelGGL(kernel, dim3((g.rows + rows - 1) / rows), dim3(kThreads), 0, st, p, g, seq, first, count,
+                           static_cast<char*>(a), static_cast<char*>(b));
+    };
+    constexpr int kMost = sizeof(T) == 2 ? 4 : 1;
+    if (!Bounds && 2LL * D * g.rows >= kReadPast)
+        launch(read_blocks<T, D, false, kMost, true>, kMost);
+    else
+        launch(read_blocks<T, D, Bounds, 1, false>, 1);
 }
 
 template <bool Bounds>

@@ -392,6 +392,32 @@ def test_read_ranges(K, dtype):
             assert np.array_equal(host(b)[:, i, :, t], rows.max(2) if there else np.full((2, 2, d), 7.0)), (i, t)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(128, 32), (64, 128)])
+def test_reads_of_more_codes_than_the_caches_hold(K, d, page, dtype):
+    """One call over a quarter of a gigabyte gives the rows that calls over parts of it give, and leaves the same ones
+    untouched: ragged sequences, ends inside a lane's rows, missing pages, a slot twice and one that is none."""
+    Hkv, B, n = 3, 5, 70001 * 128 // d
+    cache = make(K, 1, Hkv, d, page, 2000, 4, -(-n // page), 3)
+    r = np.random.default_rng(d)
+    cache.pool.random_(0, 256)
+    cache.table.copy_(dev(r.integers(-1, 2001, tuple(cache.table.shape))))
+    cache.held.fill_(cache.table.shape[1])
+    cache.length.copy_(dev([n, n - 33, n // 2, 5]))
+    seq, start, count = dev([0, 1, 2, 9, 0]), dev([0, 3, 17, 0, 1]), dev([n, n - 70, n, n, n - 1])
+    assert 2 * d * B * Hkv * n > 1 << 28
+    outs = [torch.full((1, B, Hkv, n, d), 7.0, dtype=TORCH[dtype], device="cuda") for _ in range(2)]
+    K.blocks_read(cache, n, seq=seq, start=start, count=count, k_out=outs[0], v_out=outs[1])
+    step = 20011
+    for t in range(0, n, step):
+        m = min(step, n - t)
+        parts = [torch.full((1, B, Hkv, m, d), 7.0, dtype=TORCH[dtype], device="cuda") for _ in range(2)]
+        K.blocks_read(cache, m, seq=seq, start=start + t, count=(count - t).clamp(0, m).int(), k_out=parts[0],
+                      v_out=parts[1])
+        for whole, part in zip(outs, parts):
+            assert torch.equal(whole[:, :, :, t:t + m].nan_to_num(3.0), part.nan_to_num(3.0)), t
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------

@@ -109,6 +109,9 @@ struct Angles {
     }
 };
 
+// The larger of two, NaN if one is: what float32 could not hold shows in a maximum.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // How a turned channel becomes a float: as it is rounded once more, to an E4M3 or to
 // bfloat16 (Odd and Half), or as the result itself (Float).
 enum class Turned { Odd, Half, Float };
@@ -132,7 +135,8 @@ struct Sixteen {
     // rounding unless a border of one lies within three steps: borders of E4M3 end in 16
     // zero bits, those of bfloat16 in a one and 15 zeros.  Returns whether all are decided;
     // 64 bits otherwise (a chunk of 1003 tokens, 32 and 8 heads: 25.6 us with 64 bits
-    // throughout).
+    // throughout).  Products that leave float32, and those of infinities, make infinities or
+    // NaN here where y may be neither: both are above `most`'s limit.
     template <Turned How, bool Pairs>
     __device__ __forceinline__ static bool fast(const float (&x)[16], const Angles& g, float (&y)[16]) {
         uint32_t border = 0xffffu;
@@ -146,7 +150,7 @@ struct Sixteen {
             constexpr uint32_t kAt = How == Turned::Half ? 0x8003u : 3u;
             border = min(border, min((__float_as_uint(lo) + kAt) & 0xffffu, (__float_as_uint(hi) + kAt) & 0xffffu));
             clear = fminf(clear, fminf(fmaf(-4.0f, fabsf(ep), fabsf(lo)), fmaf(-4.0f, fabsf(eq), fabsf(hi))));
-            most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
+            most = larger(most, larger(fabsf(lo), fabsf(hi)));
             y[first<Pairs>(i)] = lo;
             y[second<Pairs>(i)] = hi;
         }
@@ -613,7 +617,7 @@ __device__ __forceinline__ void turn_eight(const Eight<T>& own, const Eight<T>& 
         x[e] = fmaf(u[e], c[e], p) + ep;
         border = min(border, (__float_as_uint(x[e]) + 3u) & 0xffffu);
         clear = fminf(clear, fmaf(-4.0f, fabsf(ep), fabsf(x[e])));
-        most = fmaxf(most, fabsf(x[e]));
+        most = larger(most, fabsf(x[e]));
     }
     if (border > 6 && clear > 0x1p-90f && most < 0x1p120f) return;
 #pragma unroll

@@ -278,6 +278,54 @@ def test_rotation(K, dtype, d, r, pairs, T, Hq, Hkv, P, major):
     assert torch.equal(again.pool, cache.pool)
 
 
+def nearest(y, dtype):
+    """Numbers rounded once to the type; infinities where that takes them out of it."""
+    y = O.round_to(y, 8 if dtype == "bf16" else 24)
+    return np.where(np.abs(y) >= 2.0 ** 128, np.copysign(np.inf, y), y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,r,pairs,B,T", [(128, 128, False, 2, 70), (128, 128, True, 2, 70), (64, 48, False, 3, 33),
+                                           (64, 64, True, 1, 200), (128, 96, False, 90, 1), (64, 64, True, 90, 1)])
+def test_rotation_of_what_leaves_float32(K, dtype, d, r, pairs, B, T):
+    """One pair of every eight has infinities, NaN or numbers near the type's largest, under angles of zero, one or
+    more: what float32 makes a NaN of on the way may be a number or an infinity, and the other pairs tell nothing."""
+    rng = np.random.default_rng(d + r + B)
+    Hq, Hkv, page, P = 19, 2, 64, B * T
+    big = float(torch.finfo(TORCH[dtype]).max)
+    hard = np.array([np.inf, -np.inf, np.nan, big, -big, 3.3e38, -3.3e38, 2.0 ** 127, 1e38, 1.0, -3.0, 0.5])
+    few = np.array([0.0, 1.0, -1.0, 1.2, -1.2, 0.001, 1.999, -0.75, 2.0 ** -20])
+    angle = rng.uniform(0.3, 1.2, (P, r // 2))
+    cos, sin = np.cos(angle), np.sin(angle)
+    which = 8 * np.arange(r // 16) + rng.integers(0, 8, (P, r // 16))          # a pair of every eight
+    for table in (cos, sin):
+        np.put_along_axis(table, which, rng.choice(few, which.shape), 1)
+    cos, sin = torch.from_numpy(cos).float(), torch.from_numpy(sin).float()
+
+    def rows(H):
+        x = rng.uniform(1.0, 2.0, (B, H, T, d)) * rng.choice([-1.0, 1.0], (B, H, T, d))
+        a = which.reshape(B, 1, T, -1)
+        for c in (2 * a, 2 * a + 1) if pairs else (a, a + r // 2):
+            c = np.broadcast_to(c, (B, H, T, c.shape[-1]))
+            np.put_along_axis(x, c, rng.choice(hard, c.shape), 3)
+        return torch.from_numpy(x[None]).to(TORCH[dtype]).cuda()
+    q, k, v = rows(Hq), rows(Hkv), normal((1, B, Hkv, T, d), dtype, 3).cuda()
+    pos = np.arange(P).reshape(B, T)
+    cache = make(K, 1, Hkv, d, page, B * (T // page + 1), B, T // page + 1)
+    start, _ = K.pages_extend(cache, dev([T] * B))
+    out = K.blocks_append(k, v, cache, start, rotation=K.Rotation(cos.cuda(), sin.cuda(), pairs), position=dev(pos), q=q)
+    m, cn, sn, large = Model(cache), cos.double().numpy(), sin.double().numpy(), []
+    with np.errstate(invalid="ignore", over="ignore"):
+        for b in range(B):
+            want = nearest(O.rotate(host(q)[:, b], cn, sn, pos[b], pairs), dtype)
+            assert np.array_equal(host(out)[:, b], want, equal_nan=True), b
+            large.append(np.abs(want))
+            m.write(b, 0, O.rotate(host(k)[:, b], cn, sn, pos[b], pairs), host(v)[:, b])
+            m.same(b, T)
+    large = np.stack(large)
+    assert np.isinf(large).any() and ((large > 1e38) & (large < np.inf)).any() and np.isnan(large).any()
+
+
 def test_append_drops_what_has_no_place(K):
     """Refused starts, positions without a page, page numbers outside the pool, slots outside: nothing is written there,
     and nothing but the rows' blocks anywhere."""

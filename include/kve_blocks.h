@@ -100,9 +100,10 @@ typedef struct kve_rotation {
  *   q        [L, B, Hq, T, d] (device, dtype), a view, or NULL; needs a rotation
  *   q_out    [L, B, Hq, T, d] (device, dtype), dense, 16-byte aligned, not q itself
  *
- * T = 0 is a valid size.  Errors: KVE_ERR_INVALID_ARG (null pointers, bad sizes,
- * strides or rotation, B > S without seq, q without q_out or rotation),
- * KVE_ERR_UNSUPPORTED (dtype, d, sizes), KVE_ERR_HIP.
+ * T = 0 is a valid size: nothing is launched, k, v and the rotation's tables may be
+ * NULL, and what is given is checked all the same.  Errors: KVE_ERR_INVALID_ARG
+ * (null pointers, bad sizes, strides or rotation, B > S without seq, q without q_out
+ * or rotation), KVE_ERR_UNSUPPORTED (dtype, d, sizes), KVE_ERR_HIP.
  */
 kve_status_t kve_blocks_append(const void* k, const kve_strides_t* k_strides, const void* v,
                                const kve_strides_t* v_strides, kve_dtype_t dtype, int B, int T,

@@ -49,12 +49,12 @@ kve_status_t write_common(const char* fn, const void* k, const kve_strides_t* k_
         if (misaligned16(rot.cos) || misaligned16(rot.sin))
             return fail(KVE_ERR_INVALID_ARG, "%s: cos or sin not 16-byte aligned", fn);
     }
-    if (N == 0 || (cap == 0 && (k == nullptr || v == nullptr))) return ok();
-    if (k == nullptr || v == nullptr) return fail(KVE_ERR_INVALID_ARG, "%s: null tensor pointer", fn);
+    // a call of no rows may lack its rows' tensors; what is given is checked as with rows
+    if (cap != 0 && (k == nullptr || v == nullptr)) return fail(KVE_ERR_INVALID_ARG, "%s: null tensor pointer", fn);
     const int es = dtype == KVE_DTYPE_BF16 ? 2 : 4;
-    kve::RowView kv, vv, qv{};
-    if ((st = make_view(fn, "k", k, k_st, B, blocks->Hkv, N, blocks->d, es, &kv)) != KVE_OK) return st;
-    if ((st = make_view(fn, "v", v, v_st, B, blocks->Hkv, N, blocks->d, es, &vv)) != KVE_OK) return st;
+    kve::RowView kv{}, vv{}, qv{};
+    if (k != nullptr && (st = make_view(fn, "k", k, k_st, B, blocks->Hkv, N, blocks->d, es, &kv)) != KVE_OK) return st;
+    if (v != nullptr && (st = make_view(fn, "v", v, v_st, B, blocks->Hkv, N, blocks->d, es, &vv)) != KVE_OK) return st;
     if (misaligned16(k) || misaligned16(v)) return fail(KVE_ERR_INVALID_ARG, "%s: k or v not 16-byte aligned", fn);
     const long long touched = kve::blocks_touched(cap, blocks->page);
     double groups = 2.0 * blocks->L * B * blocks->Hkv * touched;
@@ -71,7 +71,7 @@ kve_status_t write_common(const char* fn, const void* k, const kve_strides_t* k_
         groups += (double)blocks->L * ((long long)B * cap / 32 + 1) * (Hq / kve::kBlocksQueryHeads + 1);
     }
     if (groups > (double)kMaxGroups) return fail(KVE_ERR_UNSUPPORTED, "%s: shape too large", fn);
-    if (cap == 0) return ok();  // nothing to do, but what would be refused with rows has been
+    if (cap == 0) return ok();
     return from_hip(kve::launch_blocks_write(kv, vv, qv, q_out, Hq, (int)dtype, blocks->d, B, N, idx, count, cap, start,
                                              seq, rot, p, static_cast<hipStream_t>(stream)),
                     fn);

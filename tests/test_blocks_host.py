@@ -167,6 +167,29 @@ def test_empty_calls_launch_nothing(kve):
     assert calls["bounds"](n=0, lo=0, hi=0) == 0
 
 
+def test_empty_calls_are_checked(kve):
+    """A call of no rows is refused for what would refuse it with rows, but for tensors that it does not need."""
+    calls = _calls(kve, _cache(kve))
+    for name, empty in (("append", dict(T=0)), ("append", dict(T=0, k=0, v=0)), ("compact", dict(cap=0))):
+        assert calls[name](**empty) == 0
+        for kw, status in REFUSALS[name]:
+            if "T" in kw or "cap" in kw or kw in (dict(k=0), dict(v=0), dict(idx=0)):
+                continue
+            _refused(kve, status, calls[name], **dict(empty, **kw))
+    dense = dict(layer=5 * 128 * 4, batch=5 * 128 * 2, head=5 * 128, token=128)
+    for bad in (dict(token=-128), dict(head=4), dict(layer=1 << 41), dict(token=1 << 25)):
+        st = ctypes.byref(kve.Strides(**dict(dense, **bad)))
+        for which in ("ks", "vs", "qs"):
+            _refused(kve, 1, calls["append"], T=0, **{which: st})
+        _refused(kve, 1, calls["append"], T=0, k=0, v=0, qs=st)
+        _refused(kve, 1, calls["compact"], cap=0, k=0, vs=st)
+    for kw in (dict(r=0), dict(r=24), dict(r=144), dict(P=0), dict(cos=P + 8), dict(sin=P + 4)):
+        rot = _rotation(**kw)
+        _refused(kve, 1, calls["append"], T=0, rot=ctypes.byref(rot))
+    rot = _rotation(cos=0, sin=0, position=0)
+    assert calls["append"](T=0, k=0, v=0, q=0, out=0, rot=ctypes.byref(rot)) == 0
+
+
 def test_workspaces_serve_smaller_calls(kve):
     """The size never falls with L, B, Hq or T, and the call takes it: the next check is reached."""
     size = kve.decode_blocks_workspace_size

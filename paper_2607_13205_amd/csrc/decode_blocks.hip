@@ -27,7 +27,6 @@ namespace {
 constexpr int kThreads = kMergeThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBlk = 32;       // tokens per wave step
-constexpr int kStaged = 4096;  // most entries whose lengths are kept in LDS for the search
 
 // What a wave loads for 32 tokens of a block: key codes, value codes and, in every
 // lane, the two scale bytes.  16-byte pieces of a key row are permuted so that the
@@ -288,11 +287,15 @@ struct Sums {
     }
 };
 
-// The entries of a call: query tokens of a sample, `per` at a time.
+// The entries of a launch, query tokens of a sample `per` at a time: `count` of the
+// call's from number `first` on.
 struct Entries {
     BlockView view;
     const int32_t* top;  // [L, B, Hkv, T, k], null: all blocks
-    int k, Hq, G, per, tiles, count;
+    int k, Hq, G, per, tiles, first, count;
+    // sample and first query token of entry e of the launch
+    __device__ __forceinline__ int sample(int e) const { return (first + e) / tiles; }
+    __device__ __forceinline__ int token(int e) const { return (first + e) % tiles * per; }
 };
 
 // An entry as a lane holds it: the rows to go through, and those that its last query
@@ -303,7 +306,7 @@ struct Entry : Sequence {
 
 __device__ __forceinline__ Entry entry_of(const PagePool& p, const Entries& n, int e) {
     if (e >= n.count) return Entry{{-1, 0}, 0};
-    const int b = e / n.tiles, t0 = (e - b * n.tiles) * n.per;
+    const int b = n.sample(e), t0 = n.token(e);
     const int slot = slot_of(n.view.seq, b, p.S);
     const int seen = seen_by(p, n.view, slot, b, min(t0 + n.per, n.view.T) - 1);
     return Entry{{slot, n.top == nullptr ? seen : seen > 0 ? n.k << p.shift : 0}, seen};
@@ -358,8 +361,8 @@ __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict_
         if (few) mine = entry_of(p, n, lane);
         auto of = [&](int e) -> Sequence { return few ? mine : entry_of(p, n, e); };
         int* staged = nullptr;
-        if (n.count > kWave && n.count <= kStaged) {
-            static_assert(kStaged * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
+        if (!few) {
+            static_assert(kBlocksSlice * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
             staged = reinterpret_cast<int*>(s_ring);
             for (int e = threadIdx.x; e < n.count; e += NWV * kWave) staged[e] = of(e).tokens;
             __syncthreads();
@@ -373,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict_
                         : __builtin_amdgcn_readfirstlane(entry_of(p, n, work.b).seen);
     }
     const int slot = work.slot, k0 = work.k0, k1 = work.k1;
-    const int b = work.b / n.tiles, t0 = (work.b - b * n.tiles) * n.per;
+    const int b = n.sample(work.b), t0 = n.token(work.b);
     const int here = min(n.per, n.view.T - t0);  // query tokens of the entry
     const int rows = here * n.G;
     const int page = 1 << p.shift;
@@ -499,7 +502,7 @@ __global__ __launch_bounds__(kThreads) void blocks_merge(int Hkv, Entries n, int
     const int seg = row / R, r = row - seg * R;
     const int le = seg / Hkv, j = seg - le * Hkv;
     const int l = le / n.count, e = le - l * n.count;
-    const int b = e / n.tiles, t0 = (e - b * n.tiles) * n.per;
+    const int b = n.sample(e), t0 = n.token(e);
     if (r >= min(n.per, n.view.T - t0) * n.G) return;
     const SplitRange range = ranges[e];
     if (range.count == 1) return;  // written by its only split
@@ -509,27 +512,30 @@ __global__ __launch_bounds__(kThreads) void blocks_merge(int Hkv, Entries n, int
 }
 
 template <typename T, int D, int NH>
-hipError_t run_columns(const void* q, const PagePool& p, const Entries& n, const BlocksPlan& plan, float scale,
+hipError_t run_columns(const void* q, const PagePool& p, const Entries& call, const BlocksPlan& plan, float scale,
                        float* out, void* ws, hipStream_t st) {
     float* wo = static_cast<float*>(ws);
     float2* wml = reinterpret_cast<float2*>(static_cast<char*>(ws) + plan.off_ml);
     SplitRange* ranges = reinterpret_cast<SplitRange*>(static_cast<char*>(ws) + plan.off_ranges);
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads), 0, st,
-                           static_cast<const T*>(q), p, n, plan.share, plan.level, plan.groups, plan.R,
-                           (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
-    };
-    if (plan.per > 1)
-        launch(blocks_split<T, D, NH, true>);
-    else
-        launch(blocks_split<T, D, NH, false>);
-    const int rows = plan.pairs * plan.entries * plan.R;
-    if (!plan.whole && plan.level > 16)
-        hipLaunchKernelGGL((blocks_merge<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, p.Hkv, n, plan.R,
-                           plan.groups, wo, wml, ranges, rows, out);
-    else if (!plan.whole)
-        hipLaunchKernelGGL((blocks_merge<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st,
-                           p.Hkv, n, plan.R, plan.groups, wo, wml, ranges, rows, out);
+    for (Entries n = call; n.first < plan.entries; n.first += plan.slice) {
+        n.count = min(plan.slice, plan.entries - n.first);
+        auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)plan.pairs * plan.groups), dim3(kThreads), 0, st,
+                               static_cast<const T*>(q), p, n, plan.share, plan.level, plan.groups, plan.R,
+                               (int)plan.whole, scale * kLog2e, wo, wml, ranges, out);
+        };
+        if (plan.per > 1)
+            launch(blocks_split<T, D, NH, true>);
+        else
+            launch(blocks_split<T, D, NH, false>);
+        const int rows = plan.pairs * n.count * plan.R;
+        if (!plan.whole && plan.level > 16)
+            hipLaunchKernelGGL((blocks_merge<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, p.Hkv, n, plan.R,
+                               plan.groups, wo, wml, ranges, rows, out);
+        else if (!plan.whole)
+            hipLaunchKernelGGL((blocks_merge<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0,
+                               st, p.Hkv, n, plan.R, plan.groups, wo, wml, ranges, rows, out);
+    }
     return hipGetLastError();
 }
 
@@ -547,7 +553,7 @@ hipError_t launch_decode_blocks(const void* q, int dtype, const PagePool& p, int
                                 const int32_t* top, int k, float scale, float* out, void* ws, hipStream_t st) {
     const long long tokens = top != nullptr ? (long long)k << p.shift : view.max_tokens;
     const BlocksPlan plan = decode_blocks_plan(p.L, view.B, Hq, p.Hkv, view.T, tokens, top != nullptr, d);
-    const Entries n{view, top, k, Hq, plan.G, plan.per, plan.tiles, plan.entries};
+    const Entries n{view, top, k, Hq, plan.G, plan.per, plan.tiles, 0, 0};
     if (dtype == 0) {
         if (d == 128) return run<__bf16, 128>(q, p, n, plan, scale, out, ws, st);
         return run<__bf16, 64>(q, p, n, plan, scale, out, ws, st);

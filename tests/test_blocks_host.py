@@ -219,6 +219,43 @@ def test_workspaces_serve_smaller_calls(kve):
                                             top(2, 3, 4, 3, 5000, 32), top(2, 3, 4, 2, 5100, 32))
 
 
+PLAN_PROGRAM = """
+#include <cstdio>
+#include <cstdlib>
+#include "kve_blocks_plan.h"
+int main(int argc, char** argv) {
+    for (int i = 1; i + 7 < argc; i += 8) {
+        int a[8];
+        for (int j = 0; j < 8; ++j) a[j] = atoi(argv[i + j]);
+        const kve::BlocksPlan p = kve::decode_blocks_plan(a[0], a[1], a[2], a[3], a[4], a[5], a[6] != 0, a[7]);
+        printf("%d %d %d %d %d %zu %zu\\n", (int)p.whole, p.entries, p.slice, p.share, p.groups, p.total,
+               kve::decode_blocks_size(a[0], a[1], a[2], a[3], a[4], a[7]));
+    }
+}
+"""
+
+
+def test_decode_searches_few_entries_at_a_time(tmp_path):
+    """Every workgroup of a launch that is cut into splits searches all of its entries: millions of them in one launch
+    would be more work than ends in a day.  Slices hold at most 4096, cover the call, and fit the workspace."""
+    from tests.test_abi_host import _run_plan
+    cases = [(L, B, G * Hkv, Hkv, T, tokens, sparse, d) for L, Hkv in ((1, 1), (2, 8)) for G in (1, 4, 16)
+             for B in (1, 3, 4500) for T in (1, 5, 1003, 16400, 1 << 20) for tokens in (40, 2049, 1 << 20)
+             for sparse in (0, 1) for d in (64, 128) if L * B * G * Hkv * T < 1 << 24]
+    sliced = 0
+    for case, line in zip(cases, _run_plan(tmp_path, PLAN_PROGRAM, cases)):
+        L, B, Hq, Hkv, T, tokens, sparse, d = case
+        whole, entries, per, share, groups, total, size = (int(x) for x in line.split())
+        assert entries == B * -(-T // (1 if sparse else min(T, 16 * Hkv // Hq))), case
+        assert per == entries if whole else per <= 4096, case
+        slices = -(-entries // per)
+        assert slices == 1 or slices == -(-entries // 4096), case      # as few as can be, of one size
+        assert per * slices < entries + slices and groups <= (per if whole else share + per), case
+        assert total <= size, case
+        sliced += slices > 1
+    assert sliced > 50
+
+
 def test_python_checks(kve):
     """The binding's own refusals, on CPU tensors: none reaches the library."""
     import torch

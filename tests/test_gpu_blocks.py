@@ -727,6 +727,57 @@ def test_decode_of_thousands_of_samples(K):
     check_decode(cache, k, v, host(q), host(out), lengths, order, samples=some)
 
 
+@pytest.mark.parametrize("B,T,G,Hkv,lengths,sparse,dtype", [
+    (1501, 6, 8, 1, [40, 0, 2, 33, 300, 9000], 0, "bf16"),      # 4503 entries of two tokens: a slice ends within a sample
+    (8700, 1, 3, 1, [1, 0, 64, 2600, 31], 0, "f32"),            # three slices
+    (5, 900, 2, 2, [2400, 77, 0, 3000, 1000], 70, "bf16"),      # 4500 entries with lists of their own
+    (1, 16400, 4, 1, [17000], 0, "bf16"),                       # a prompt's chunk: 4100 entries of four tokens
+])
+def test_decode_of_more_entries_than_a_launch_cuts(K, B, T, G, Hkv, lengths, sparse, dtype):
+    """Slices of entries one after the other over the same workspace, rows of several splits in each, captured too."""
+    d, page = 64, 32
+    cache, k, v = filled(K, 1, Hkv, d, page, lengths)
+    r = np.random.default_rng(B)
+    order = np.arange(B) % len(lengths) if B < 10 else r.integers(-1, len(lengths) + 1, B)
+    long = int(np.argmax(lengths))
+    if B > 10:                                                  # long ones are few, and at the ends of slices
+        order[order == long] = 0
+        order[[0, B // 3 - 1, B // 3, B // 2 - 1, B // 2, B // 2 + 1, 2 * B // 3, B - 1]] = long
+    start = None if T < 900 else dev([max(0, lengths[s] - T - 40 * i) for i, s in enumerate(order)])
+    q = normal((1, B, G * Hkv, T, d), dtype, 80).cuda()
+    top = None
+    if sparse:
+        top = dev(np.sort(r.integers(-1, cache.table.shape[1] + 1, (1, B, Hkv, T, sparse)), -1))
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    ws = torch.empty(K.decode_blocks_workspace_size(1, B, G * Hkv, Hkv, T, d), dtype=torch.uint8, device="cuda")
+    ws.fill_(255)
+    K.decode_blocks(q, cache, seq=dev(order), start=start, top=top, out=out, workspace=ws)
+    assert torch.isfinite(out).all()
+    begin = None if start is None else start.cpu().numpy()
+    hq, ho, ht = host(q), host(out), None if top is None else top.cpu().numpy()
+    if T < 900:
+        at = sorted({0, 1, B // 3 - 1, B // 3, B // 2 - 1, B // 2, B // 2 + 1, 2 * B // 3, B - 1,
+                     *r.integers(0, B, 60).tolist()})
+        check_decode(cache, k, v, hq, ho, lengths, order, samples=at)
+    else:                                                       # some tokens of each sample, as samples of one
+        for b in range(B):
+            at = np.unique(np.concatenate([[0, 1, T // 2 - 1, T // 2, T // 2 + 1, T - 1], r.integers(0, T, 20)]))
+            one = (np.moveaxis(x[0, b][:, at], 1, 0)[None, :, :, None] for x in (hq, ho))
+            check_decode(cache, k, v, *one, lengths, [order[b]] * len(at), start=begin[b] + at,
+                         top=None if ht is None else np.moveaxis(ht[0, b][:, at], 1, 0)[None, :, :, None])
+    want = out.clone()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    seq = dev(order)
+    with torch.cuda.graph(graph, stream=side):
+        K.decode_blocks(q, cache, seq=seq, start=start, top=top, out=out, workspace=ws)
+    for i in range(3):
+        out.fill_(float("nan"))
+        ws.fill_(i)
+        graph.replay()
+        assert torch.equal(out, want)
+
+
 # ---------------------------------------------------------------------------
 # block choice
 # ---------------------------------------------------------------------------

@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kThreads, 2) void blocks_split(const T* __restrict_
         auto of = [&](int e) -> Sequence { return few ? mine : entry_of(p, n, e); };
         int* staged = nullptr;
         if (!few) {
-            static_assert(kBlocksSlice * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
+            static_assert(kPagesSlice * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
             staged = reinterpret_cast<int*>(s_ring);
             for (int e = threadIdx.x; e < n.count; e += NWV * kWave) staged[e] = of(e).tokens;
             __syncthreads();

@@ -44,7 +44,6 @@ namespace {
 constexpr int kThreads = kMergeThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBlk = 32;    // tokens per wave step
-constexpr int kStaged = 4096;  // most sequences whose lengths are kept in LDS for the search
 
 // Waves per SIMD that the registers are kept to, and so workgroups per compute
 // unit: four where the registers suffice without spills (8 layers, 4 sequences of
@@ -313,8 +312,8 @@ __global__ __launch_bounds__(NWV * kWave, (kPerSimd<T, D, NH>)) void pages_split
         // many sequences: their lengths are loaded once, by all waves (200 ragged ones of
         // up to 4000 tokens, 8 KV heads: 86 us with every wave loading them, 74 so)
         int* staged = nullptr;
-        if (B > kWave && B <= kStaged) {
-            static_assert(kStaged * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
+        if (B > kWave) {
+            static_assert(kPagesSlice * (int)sizeof(int) <= (int)sizeof(s_ring), "the lengths fit the rings");
             staged = reinterpret_cast<int*>(s_ring);
             for (int e = threadIdx.x; e < B; e += NWV * kWave) staged[e] = sequence_of(p, seq, e, B, max_tokens).tokens;
             __syncthreads();
@@ -483,6 +482,28 @@ hipError_t run(const void* q, const PagePool& p, int B, int Hq, int max_tokens, 
 
 hipError_t launch_decode_pages(const void* q, int dtype, const PagePool& p, int d, int B, int Hq, int max_tokens,
                                const int32_t* seq, float scale, float* out, void* ws, hipStream_t st) {
+    const int slice = decode_pages_plan(p.L, B, Hq, p.Hkv, max_tokens, d).slice;
+    if (slice < B) {  // each layer's slices as calls of their own
+        const size_t row = (size_t)Hq * d, layer = (size_t)p.n_pages * p.Hkv * page_block_bytes(1 << p.shift, d);
+        for (int l = 0; l < p.L; ++l)
+            for (int b = 0; b < B; b += slice) {
+                PagePool part = p;
+                part.L = 1;
+                part.pool += l * layer;
+                if (seq == nullptr) {  // sample b is slot b
+                    part.S -= b;
+                    part.held += b;
+                    part.length += b;
+                    part.table += (size_t)b * p.M;
+                }
+                const size_t at = ((size_t)l * B + b) * row;
+                const hipError_t e = launch_decode_pages(
+                    static_cast<const char*>(q) + at * (dtype == 0 ? 2 : 4), dtype, part, d, B - b < slice ? B - b : slice,
+                    Hq, max_tokens, seq != nullptr ? seq + b : nullptr, scale, out + at, ws, st);
+                if (e != hipSuccess) return e;
+            }
+        return hipSuccess;
+    }
     if (dtype == 0) {
         if (d == 128) return run<__bf16, 128>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);
         return run<__bf16, 64>(q, p, B, Hq, max_tokens, seq, scale, out, ws, st);

@@ -45,15 +45,10 @@ struct BlockView {
 // 15.4, but 2 heads, five quanta to a unit, 12.5 for 11.9).
 constexpr int kBlocksLevel = 1, kBlocksRagged = 4, kBlocksSeveral = 8, kBlocksLong = 8;
 
-// Most entries of one launch that are cut into splits.  Every workgroup finds its split
-// among them by itself, so that more in one launch would cost their square; as many as
-// have their lengths kept in LDS.
-constexpr int kBlocksSlice = 4096;
-
 // Plan of a decode over blocks.  Query tokens of a sample are taken `per` at a time,
 // an entry each: as many as the sixteen columns of a product hold heads for, or one
-// where each has its own blocks.  The entries' tokens are cut as PagesPlan's, a slice of
-// equally many entries after the other.
+// where each has its own blocks.  The entries' tokens are cut as PagesPlan's, up to
+// kPagesSlice entries at a time.
 struct BlocksPlan {
     int pairs, G, per, tiles, entries, R;  // R: query rows of an entry, per * G
     int slice;                             // entries of a launch
@@ -88,7 +83,7 @@ inline BlocksPlan decode_blocks_plan(int L, int B, int Hq, int Hkv, int T, long 
     p.level = splits(d == 64 && segs * quanta >= kBlocksLong * kDecodeUnits ? 2 * kBlocksLevel : kBlocksLevel);
     // chosen blocks are equally many
     p.share = sparse || p.entries < kBlocksSeveral ? p.level : splits(kBlocksRagged);
-    const int slices = p.whole ? 1 : (p.entries + kBlocksSlice - 1) / kBlocksSlice;
+    const int slices = p.whole ? 1 : (p.entries + kPagesSlice - 1) / kPagesSlice;
     p.slice = (p.entries + slices - 1) / slices;
     long long groups = (long long)p.share + p.slice;
     if (groups > p.slice * quanta) groups = p.slice * quanta;

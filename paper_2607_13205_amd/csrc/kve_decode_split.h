@@ -136,8 +136,8 @@ struct Work {
 // costs (64 ragged sequences of up to 16384 tokens, 8 KV heads: 87 us so, 64.5
 // with a share-th; half of it and twice it 63.6 and 73).  Every wave works it out for
 // itself, 64 sequences at a time.  of(b): sequence b, none from B on.  staged: the
-// lengths of all sequences (null: they are loaded; up to 64 once, and more several
-// times).  ranges: where not null, every sequence's range is written there.
+// lengths of all sequences, null for up to 64, which the lanes hold.  ranges: where not
+// null, every sequence's range is written there.
 // level: where not 0, the share for sequences of which none is much longer than the
 // mean.
 template <typename Of>
@@ -148,7 +148,7 @@ __device__ __forceinline__ Work find_work(Of of, int B, int share, int x, const 
     if (staged == nullptr) mine = of(lane);
     auto tokens_at = [&](int b0) -> int {
         if (staged != nullptr) return b0 + lane < B ? staged[b0 + lane] : 0;
-        return b0 == 0 ? mine.tokens : of(b0 + lane).tokens;
+        return mine.tokens;
     };
     // sums over the lanes' shares: up to 2^23 quanta each, any number of sequences
     long long total = 0;
@@ -173,8 +173,8 @@ __device__ __forceinline__ Work find_work(Of of, int B, int share, int x, const 
         if (mask != 0) {
             const int at = __builtin_ctzll(mask);
             w.b = b0 + at;
-            w.slot = b0 == 0 && staged == nullptr ? __builtin_amdgcn_readlane(mine.slot, at)
-                                                  : __builtin_amdgcn_readfirstlane(of(w.b).slot);
+            w.slot = staged == nullptr ? __builtin_amdgcn_readlane(mine.slot, at)
+                                       : __builtin_amdgcn_readfirstlane(of(w.b).slot);
             w.range.first = __builtin_amdgcn_readlane(first, at);
             w.range.count = __builtin_amdgcn_readlane(n, at);
             w.k0 = (x - w.range.first) * per * kDecodeQuantum;

@@ -42,9 +42,11 @@ inline size_t pages_workspace(int n_pages, int n) {
 // is a `share`-th of all sequences' quanta, `share` being one round of resident
 // workgroups over all (layer, KV head) pairs.  That makes at most share + B splits
 // (a sequence's last one may be short).  They are numbered one sequence after the
-// other, and workgroup x of each pair takes split x.
+// other, and workgroup x of each pair takes split x.  More than kPagesSlice sequences that
+// are cut are taken by layers and in slices of equally many, calls of their own.
 struct PagesPlan {
     int pairs, G, groups;  // groups: workgroups per (layer, KV head)
+    int slice;             // sequences of a launch; where not all, the other fields but `total` do not count
     bool whole;            // one split per sequence: nothing to merge
     int per_unit;          // workgroups that share a compute unit: 1, 2 or 4
     size_t off_ml, off_ranges, total;
@@ -63,6 +65,11 @@ struct PagesPlan {
 // and 9.1, 32 of 4000 21.4 and 18.2.
 constexpr int kPagesMostResident = 4 * kDecodeUnits;  // workgroups, at four per compute unit
 constexpr int kPagesWhole = 4;                        // quanta up to which every sequence is one split
+
+// Most sequences of one launch that are cut into splits.  Every workgroup finds its split
+// among them by itself, so that more in one launch would cost their square; as many as
+// have their lengths kept in LDS.
+constexpr int kPagesSlice = 4096;
 
 // Workspace of a decode whose splits leave `parts` partial results.
 inline size_t decode_pages_bytes(size_t parts, int B, int d, PagesPlan* p) {
@@ -84,6 +91,15 @@ inline PagesPlan decode_pages_plan(int L, int B, int Hq, int Hkv, int max_tokens
     if (groups > B * quanta) groups = B * quanta;
     if (p.whole) groups = B;
     p.groups = (int)groups;
+    const int slices = p.whole ? 1 : (B + kPagesSlice - 1) / kPagesSlice;
+    p.slice = (B + slices - 1) / slices;
+    if (slices > 1) {  // a slice that is not the last, and the last
+        const int last = B - (slices - 1) * p.slice;
+        const size_t a = decode_pages_plan(1, p.slice, Hq, Hkv, max_tokens, d).total;
+        const size_t b = decode_pages_plan(1, last, Hq, Hkv, max_tokens, d).total;
+        p.total = a > b ? a : b;
+        return p;
+    }
     p.total = decode_pages_bytes(p.whole ? 0 : (size_t)p.pairs * p.groups * p.G, B, d, &p);
     return p;
 }

@@ -551,6 +551,58 @@ def test_decode_of_thousands_of_samples(K):
             assert not on[0, i].any()
 
 
+@pytest.mark.parametrize("dtype,B,slots", [("bf16", 8194, True), ("f32", 9000, True), ("bf16", 5001, False)])
+def test_decode_of_more_samples_than_a_launch_cuts(K, dtype, B, slots):
+    """Slices of samples one after the other over the same workspace, two layers, rows of several splits in each,
+    captured too."""
+    L, Hkv, G, d, page = 2, 2, 2, 64, 32
+    lengths = [1, 2600, 0, 33, 300]
+    if slots:
+        pages, _, _ = _filled(K, L, Hkv, d, page, lengths)
+    else:                                                       # sample b in slot b: the slots share their pages
+        few, _, _ = _filled(K, L, Hkv, d, page, lengths)
+        which = np.random.default_rng(2).choice([0, 2, 3, 4], B)
+        which[[0, B // 2, B // 2 + 1, B - 1]] = 1
+        at = dev(which).long()
+        pages = K.Pages(few.pool, few.refs, few.table[at].contiguous(), few.held[at].contiguous(),
+                        few.length[at].contiguous(), page, d)
+        rows_in = few
+    r = np.random.default_rng(9)
+    order = r.choice([-1, 0, 2, 3, 4, len(lengths)], B) if slots else which
+    if slots:
+        order[[0, B // 3, B // 3 + 1, 2 * B // 3, 2 * B // 3 + 1, B - 1]] = 1
+        rows_in = pages
+    q = normal((L, B, Hkv * G, d), dtype, 79).cuda()
+    out = torch.full(q.shape, float("nan"), device="cuda")
+    ws = torch.empty(K.decode_pages_workspace_size(L, B, Hkv * G, Hkv, pages.c.M * page, d), dtype=torch.uint8,
+                     device="cuda")
+    ws.fill_(255)
+    seq = dev(order) if slots else None
+    K.decode_pages(q, pages, seq=seq, out=out, workspace=ws)
+    rows = [rows_of(rows_in, s) for s in range(len(lengths))]
+    qn, on = q.double().cpu().numpy(), out.double().cpu().numpy()
+    assert np.isfinite(on).all()
+    ends = [x + e for x in (0, B // 3, B // 2, 2 * B // 3, B - 2) for e in (0, 1)]
+    for i in [*ends, *r.integers(0, B, 100)]:
+        s = order[i]
+        for l in range(L):
+            if 0 <= s < len(lengths):
+                want, mag, top = _decode_ref(qn[l, i], rows[s][0][l], rows[s][1][l], G)
+                check_decode(on[l, i], want, mag, top, f"sample {i} slot {s} layer {l}")
+            else:
+                assert not on[l, i].any()
+    want = out.clone()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        K.decode_pages(q, pages, seq=seq, out=out, workspace=ws)
+    for i in range(3):
+        out.fill_(float("nan"))
+        ws.fill_(i)
+        graph.replay()
+        assert torch.equal(out, want)
+
+
 def test_decode_equals_decode_over_the_rows_read_back(K):
     """The same rows dense in bf16: decode_attention gives the same to float32 rounding."""
     lengths = [700, 64, 0, 333]

@@ -184,6 +184,44 @@ def test_evict_checks_what_goes_into_pages(kve):
         evict(k, None, slots=torch.zeros(1, dtype=torch.int32))
 
 
+PLAN_PROGRAM = """
+#include <cstdio>
+#include <cstdlib>
+#include "kve_pages_plan.h"
+int main(int argc, char** argv) {
+    for (int i = 1; i + 5 < argc; i += 6) {
+        int a[6];
+        for (int j = 0; j < 6; ++j) a[j] = atoi(argv[i + j]);
+        const kve::PagesPlan p = kve::decode_pages_plan(a[0], a[1], a[2], a[3], a[4], a[5]);
+        const int last = (a[1] - 1) % p.slice + 1;
+        printf("%d %d %d %zu %zu %zu\\n", (int)p.whole, p.slice, kve::decode_pages_plan(1, last, a[2], a[3], a[4], a[5]).slice,
+               kve::decode_pages_plan(1, last, a[2], a[3], a[4], a[5]).total, p.total,
+               kve::decode_pages_size(a[0], a[1], a[2], a[3], a[4], a[5]));
+    }
+}
+"""
+
+
+def test_decode_searches_few_samples_at_a_time(tmp_path):
+    """Every workgroup of a launch that is cut into splits searches all of its samples: slices hold at most 4096,
+    cover the call, and fit the workspace."""
+    from tests.test_abi_host import _run_plan
+    cases = [(L, B, G * Hkv, Hkv, most, d) for L, Hkv in ((1, 1), (1, 8), (32, 8)) for G in (1, 4, 16)
+             for B in (1, 64, 4096, 4097, 8193, 20000, 1 << 20) for most in (40, 2048, 2049, 131072, 1 << 30)
+             for d in (64, 128) if L * B * Hkv < 1 << 24]
+    sliced = 0
+    for case, line in zip(cases, _run_plan(tmp_path, PLAN_PROGRAM, cases)):
+        B = case[1]
+        whole, per, last, part, total, size = (int(x) for x in line.split())
+        assert per == B if whole else per <= 4096, case
+        slices = -(-B // per)
+        assert slices == 1 or slices == -(-B // 4096), case            # as few as can be, of one size
+        assert per * slices < B + slices and last == B - (slices - 1) * per, case   # and a slice is one launch
+        assert total <= size and (slices == 1 or part <= total), case
+        sliced += slices > 1
+    assert sliced > 50
+
+
 def test_compact_of_no_rows_checks_the_views(kve):
     """k_cap = 0 launches nothing, but what a call with rows would refuse is refused."""
     call = _calls(kve, _cache(kve))["compact"]

@@ -217,8 +217,7 @@ struct Sums {
             for (int i = 0; i < 8; ++i) bad |= nan_codes(v[e][i]);
         const int turns = __builtin_amdgcn_ballot_w64(bad != 0) == 0 ? 1 : tiles;
         // with one, query token by query token: the rows behind what it sees as zeros, and only
-        // its columns' sums kept.  One loop for both: with a third call of values() for the
-        // first, ROCm 7.2's compiler left den undefined behind it.
+        // its columns' sums kept
 #pragma unroll 1
         for (int t = 0; t < turns; ++t) {
             const bool all = turns == 1;
@@ -528,6 +527,12 @@ hipError_t run_columns(const void* q, const PagePool& p, const Entries& call, co
             launch(blocks_split<T, D, NH, true>);
         else
             launch(blocks_split<T, D, NH, false>);
+        // up to 16 splits of a level entry: one wave per row; more: four, as over four-bit pages.
+        // Ragged ones may have four times as many and leave it open which is better (8 KV heads,
+        // microseconds with one wave and with four: two layers, one sequence of 131072 among 8
+        // of 500 92.8 and 91.5, of 64 channels 51.5 and 50.0, one of 32768 among 16 39.6 and 38.9,
+        // one of 40000 among 64 of 700 40.7 and 42.3, 16 of up to 32768 185.7 and 187.3, eight
+        // layers 662.7 and 665.6; level, 16 of 8192, 84.8 and 85.1).
         const int rows = plan.pairs * n.count * plan.R;
         if (!plan.whole && plan.level > 16)
             hipLaunchKernelGGL((blocks_merge<D, kWaves>), dim3((unsigned)rows), dim3(kThreads), 0, st, p.Hkv, n, plan.R,

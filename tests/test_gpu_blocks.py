@@ -466,6 +466,23 @@ def test_reads_of_more_codes_than_the_caches_hold(K, d, page, dtype):
             assert torch.equal(whole[:, :, :, t:t + m].nan_to_num(3.0), part.nan_to_num(3.0)), t
 
 
+@pytest.mark.parametrize("turned", [False, True])
+def test_append_of_no_tokens(K, turned):
+    """T = 0 writes nothing, with queries and views of empty ranges too."""
+    cache, _, _ = filled(K, 2, 2, 64, 32, [40, 0])
+    pool, length = cache.pool.clone(), cache.length.clone()
+    k = normal((2, 2, 5, 2, 64), "bf16", 1).cuda().permute(0, 1, 3, 2, 4)[:, :, :, 3:3]
+    start, missing = K.pages_extend(cache, dev([0, 0]))
+    kw = {}
+    if turned:
+        cos = torch.ones(4, 16, device="cuda")
+        kw = dict(rotation=K.Rotation(cos, cos), position=dev(np.zeros((2, 0))),
+                  q=torch.zeros((2, 2, 4, 0, 64), dtype=torch.bfloat16, device="cuda"))
+    out = K.blocks_append(k, k, cache, start, **kw)
+    assert out.shape == (2, 2, 4, 0, 64) if turned else out is None
+    assert torch.equal(cache.pool, pool) and torch.equal(cache.length, length) and missing.item() == 0
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
